@@ -90,6 +90,10 @@ typedef enum das_dtype { DAS_F32 = 0, DAS_BF16 = 1 } das_dtype;
 #define DAS_DEVERR_COMMIT 4u     /* num_new[b] outside [0, w_max], or the commit
                                     would run past the sequence's table pages     */
 #define DAS_DEVERR_TESTED 8u     /* tested[b] outside [0, block_len]; clamped      */
+#define DAS_DEVERR_SAMPLE 16u    /* a sampling parameter or random number out of
+                                    range; the row was taken greedily               */
+#define DAS_DEVERR_POOL 32u      /* too few free pages for a sequence, or a free
+                                    list that cannot be right                       */
 
 /*
  * Depth-indexed, paged KV cache (caller-owned device memory).
@@ -341,6 +345,155 @@ das_status das_greedy_accept(int32_t batch, int32_t block_len, const int32_t *pr
                              const int32_t *target_pred, const int32_t *tested,
                              int32_t *accepted, int32_t *num_keep, int32_t *emitted,
                              int32_t *num_emitted, uint32_t *dev_error, hipStream_t stream);
+
+/* -------------------------------------------------------------------------
+ * A cache held in 8 bits
+ * -------------------------------------------------------------------------
+ * The same planes, layers, heads, pages and block tables with every element one
+ * e4m3 code (OCP 8-bit float: 4 exponent bits, 3 mantissa bits, largest 448) and
+ * one power-of-two scale per 8 tokens and KV head ("group": positions 8 G .. 8 G + 7
+ * of a page). Element = code * 2^(byte - 127), byte in 1..254.
+ *
+ *   base.k_pool  [num_k_planes][L][Hkv][num_pages][8][8 * head_dim] codes: in a
+ *                group, token 4 e + n (e < 2, n < 4), dim 32 s + 8 g + i (g < 4,
+ *                i < 8) is byte 256 s + 64 g + 16 n + 8 e + i
+ *   base.v_pool  [num_v_planes][L][Hkv][num_pages][8][head_dim][8] codes
+ *   k_exp        [num_k_planes][L][num_pages][Hkv][8] bytes, one per group
+ *   v_exp        [num_v_planes][L][num_pages][Hkv][8] bytes
+ *
+ * base.dtype is the type of queries, block K/V, outputs and committed K/V; the
+ * other fields of `base` are as in das_cache. Pools are 16-byte aligned, exponent
+ * arrays 4-byte aligned. Half the bytes of a bf16 cache (a 1/128 of them more or
+ * less for the exponents), so half the time of a call that is bound by them.
+ * Places that hold no token of a sequence (behind its length) may hold anything.
+ */
+typedef struct das_cache_q8 {
+  das_cache base;
+  uint8_t *k_exp;
+  uint8_t *v_exp;
+} das_cache_q8;
+
+/*
+ * das_attn_policy over an 8-bit cache: prefix keys at depth kappa and values at
+ * depth nu are the elements above, block keys and values are the caller's in
+ * base.dtype. Arguments, masks, bounds and error words as for das_attn_policy, and
+ * the same limits (w in 1..DAS_MAX_BLOCK, Hq / Hkv <= 8), for any batch size.
+ *
+ * Numerics: elements are exact in the products' types. bf16 calls multiply values
+ * in fp16 with probabilities of 11 bits; a group's values below 2^-24 of the largest
+ * scale's unit met so far round there. fp32 calls multiply in fp32. Accumulation and
+ * softmax statistics are fp32. lse as for das_attn_policy.
+ *
+ * das_attn_q8_workspace_bytes returns 0 for arguments that das_attn_q8 rejects; the
+ * workspace is 256-byte aligned, needs no init, and calls that run concurrently need
+ * separate ones.
+ */
+size_t das_attn_q8_workspace_bytes(const das_cache_q8 *cache, const das_batch *batch,
+                                   int32_t num_q_heads, int32_t block_len);
+das_status das_attn_q8(const das_cache_q8 *cache, const das_batch *batch, int32_t layer,
+                       int32_t kappa, int32_t nu, int32_t num_q_heads, int32_t block_len,
+                       const void *q, const void *k_blk, const void *v_blk, void *out, float *lse,
+                       void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * das_kv_append into an 8-bit cache. Arguments as for das_kv_append, with k_new and
+ * v_new in base.dtype.
+ *
+ * A group without earlier tokens of the sequence gets the smallest exponent e in
+ * -64..119 with |x| <= 448 * 2^e for its new finite elements. A group with earlier
+ * tokens gets the larger of that and its own; when its own grows, the earlier codes
+ * are rounded again (which changes only those that become subnormal). Codes are
+ * x * 2^-e rounded to nearest even; NaN and infinities become the code NaN, finite
+ * values past 448 * 2^119 become that. Places of the group from the sequence's new
+ * length on are left as they were.
+ */
+das_status das_kv_append_q8(const das_cache_q8 *cache, const das_batch *batch, const void *k_new,
+                            const void *v_new, int32_t w_max, const int32_t *num_new,
+                            int32_t *len_out, hipStream_t stream);
+
+/* Largest vocabulary that das_sample takes. */
+#define DAS_MAX_VOCAB (1 << 20)
+
+/*
+ * A token for every position of a batch of blocks, from its logits and a given random
+ * number: the target's predictions for das_greedy_accept. A proposal that equals the
+ * token drawn from the verifier's conditional is accepted, so the emitted tokens are
+ * draws from the verifier's (filtered) distribution whatever the draft proposes, and
+ * with temperature 0 they are its greedy continuation.
+ *
+ * Row (b, i) uses the parameters of sequence b. With z its logits (NaN counts as
+ * -inf), m = max z and weights w_j = exp((z_j - m) / temperature[b]), tokens in the
+ * order (z descending, index ascending):
+ *   top-k  keeps the first top_k[b] tokens (0 or less, or vocab or more: all);
+ *   top-p  keeps, of those, the shortest run from the first whose weights sum to
+ *          top_p[b] of their total or more (1 or more: all; the first is always kept);
+ *   min-p  keeps, of those, the tokens with w_j >= min_p[b] (0 or less: all; over 1
+ *          counts as 1).
+ * The token is the first in index order at which the running sum of kept weights
+ * passes uniform[b][i] times their sum. Sums are exact sums of weights rounded to
+ * 2^-40; a token below 2^-41 of the largest is never drawn. A temperature of 0 takes
+ * the largest logit, lowest index first; so do rows with a NaN, negative or infinite
+ * temperature, a NaN filter or a random number outside [0, 1), which set
+ * DAS_DEVERR_SAMPLE, and a row without any logit above -inf gives token 0.
+ *
+ *   logits       device rows of `vocab` elements of `dtype`, row_stride elements from
+ *                one to the next (>= vocab), in the order [B][w]
+ *   temperature  device [B] fp32, or NULL: 1
+ *   top_k        device [B] int32, or NULL: all
+ *   top_p, min_p device [B] fp32, or NULL: all
+ *   uniform      device [B][w] fp32 in [0, 1)
+ *   tokens       device [B][w] int32, written
+ *   probs        device [B][w] fp32 or NULL, written: the token's share of the kept
+ *                weights (1 where it was taken greedily)
+ *   dev_error    optional device word
+ *
+ * batch in 1..65535, block_len in 1..DAS_MAX_BLOCK, vocab in 1..DAS_MAX_VOCAB. Logits
+ * are aligned to their type, the other arrays to 4 bytes. Results do not depend on
+ * the order of the work: equal calls give equal bits.
+ */
+das_status das_sample(int32_t batch, int32_t block_len, int32_t vocab, int32_t dtype,
+                      const void *logits, int64_t row_stride, const float *temperature,
+                      const int32_t *top_k, const float *top_p, const float *min_p,
+                      const float *uniform, int32_t *tokens, float *probs, uint32_t *dev_error,
+                      hipStream_t stream);
+
+/*
+ * Block tables from the lengths that sequences shall have, on the device: pages for a
+ * step before its commit, their release after a rollback, and a finished sequence's
+ * (length 0).
+ *
+ * Sequence b shall hold ceil(lengths[b] / 64) pages, the first pages_held[b] entries of
+ * its table row. Sequences that hold more give the rest back, their entries become -1;
+ * then sequences that hold less get what they lack, in sequence order: each all of it,
+ * or nothing once the running sum of what was asked for passes the free pages
+ * (DAS_DEVERR_POOL; its row and count stay as they were). Free pages are a stack: a
+ * release undoes the grant before it exactly, so tables do not depend on timing.
+ *
+ *   lengths      device [B], each in 0 .. 64 * max_pages_per_seq; a sequence with
+ *                another length, or a held count out of range, is left alone
+ *                (DAS_DEVERR_PREFIX)
+ *   block_table  device [B][max_pages_per_seq], updated
+ *   pages_held   device [B], updated
+ *   free_pages   device [num_pages], updated: the free page ids are its first *num_free
+ *   num_free     device [1], updated. Where it is out of range or the list could not
+ *                hold what comes back, nothing is moved (DAS_DEVERR_POOL)
+ *   first, slots, block_len
+ *                device [B], device [B][block_len] and the width, or NULL, NULL, 0:
+ *                slots[b][i] receives the slot page * 64 + position % 64 of position
+ *                first[b] + i in the updated table, or -1 where it is not below
+ *                lengths[b] or has no page
+ *   dev_error    optional device word
+ *
+ * batch in 1..65535, max_pages_per_seq in 1..2^24, batch * max_pages_per_seq < 2^31,
+ * num_pages in 1..2^25 - 1, block_len in 1..DAS_MAX_BLOCK where slots are asked for.
+ * The arrays must not overlap. One sequence's entry may be any page id: ids are moved,
+ * not read through.
+ */
+das_status das_pages_update(int32_t batch, int32_t max_pages_per_seq, int32_t num_pages,
+                            const int32_t *lengths, int32_t *block_table, int32_t *pages_held,
+                            int32_t *free_pages, int32_t *num_free, const int32_t *first,
+                            int32_t block_len, int32_t *slots, uint32_t *dev_error,
+                            hipStream_t stream);
 
 /* Static description of a status code; never NULL. */
 const char *das_status_string(das_status status);

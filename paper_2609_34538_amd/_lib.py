@@ -11,7 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_char_p, c_int32, c_size_t, c_uint32, c_void_p
+from ctypes import POINTER, c_char_p, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 from dataclasses import dataclass, field
 from typing import Dict, Optional
 
@@ -33,10 +33,14 @@ STATUS_NAMES = {0: "DAS_OK", -1: "DAS_ERR_NULL", -2: "DAS_ERR_SHAPE", -3: "DAS_E
 DTYPE_CODES = {torch.float32: 0, torch.bfloat16: 1}
 PATHS = {"auto": 0, "valu": 1, "mfma": 2, "balanced": 3}
 DEVERR_PAGE, DEVERR_PREFIX, DEVERR_COMMIT, DEVERR_TESTED = 1, 2, 4, 8
+DEVERR_SAMPLE, DEVERR_POOL = 16, 32
+MAX_VOCAB = 1 << 20
+GROUP_TOKENS = 8  # tokens that share an exponent of the 8-bit cache
 
 EXPORTED = ["das_attn_workspace_bytes", "das_attn_workspace_bytes_ex", "das_attn_draft_maturev",
             "das_attn_verify", "das_attn_policy", "das_attn_policy_noalloc", "das_kv_append",
-            "das_greedy_accept",
+            "das_greedy_accept", "das_attn_q8_workspace_bytes", "das_attn_q8", "das_kv_append_q8",
+            "das_sample", "das_pages_update",
             "das_status_string", "das_version"]
 
 
@@ -61,6 +65,10 @@ class DasBatchC(ctypes.Structure):
 
 class DasOptionsC(ctypes.Structure):
     _fields_ = [("path", c_int32), ("pages_per_split", c_int32)]
+
+
+class DasCacheQ8C(ctypes.Structure):
+    _fields_ = [("base", DasCacheC), ("k_exp", c_void_p), ("v_exp", c_void_p)]
 
 
 def _load() -> ctypes.CDLL:
@@ -91,6 +99,22 @@ def _load() -> ctypes.CDLL:
     lib.das_kv_append.restype = c_int32
     lib.das_greedy_accept.argtypes = [c_int32, c_int32] + [c_void_p] * 8 + [c_void_p]
     lib.das_greedy_accept.restype = c_int32
+    pq = POINTER(DasCacheQ8C)
+    lib.das_attn_q8_workspace_bytes.argtypes = [pq, pb, c_int32, c_int32]
+    lib.das_attn_q8_workspace_bytes.restype = c_size_t
+    lib.das_attn_q8.argtypes = [pq, pb, c_int32, c_int32, c_int32, c_int32, c_int32, c_void_p,
+                                c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t,
+                                c_void_p]
+    lib.das_attn_q8.restype = c_int32
+    lib.das_kv_append_q8.argtypes = [pq, pb, c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
+                                     c_void_p]
+    lib.das_kv_append_q8.restype = c_int32
+    lib.das_sample.argtypes = ([c_int32] * 4 + [c_void_p, c_int64] + [c_void_p] * 8
+                               + [c_void_p])
+    lib.das_sample.restype = c_int32
+    lib.das_pages_update.argtypes = ([c_int32] * 3 + [c_void_p] * 6 + [c_int32] + [c_void_p] * 2
+                                     + [c_void_p])
+    lib.das_pages_update.restype = c_int32
     lib.das_status_string.argtypes = [c_int32]
     lib.das_status_string.restype = c_char_p
     lib.das_version.argtypes = []
@@ -450,3 +474,297 @@ def greedy_accept(proposals: torch.Tensor, target_pred: torch.Tensor,
     if st != DAS_OK:
         raise DasError(st, "das_greedy_accept")
     return accepted, num_keep
+
+
+# ---------------------------------------------------------------------------
+# The 8-bit cache, the sampler and the page tables
+# ---------------------------------------------------------------------------
+def _check(t: torch.Tensor, dtype, shape, device, what: str):
+    """A tensor the call reads or writes: type, shape, layout and device."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{what} must be on {device}")
+    return t.data_ptr()
+
+
+def _check_opt(t: Optional[torch.Tensor], dtype, shape, device, what: str):
+    return None if t is None else _check(t, dtype, shape, device, what)
+
+
+class _Call:
+    """A library call with its arguments marshalled: calling it enqueues it on `stream`
+    (None: the current stream of the tensors' device) with that device current. The
+    tensors are kept alive."""
+
+    def __init__(self, fn, name: str, args, keep, device: torch.device, stream):
+        if stream is not None and device.type == "cuda" and stream.device != device:
+            raise ValueError(f"the stream must be one of {device}")
+        self._fn, self._name, self._keep, self._device = fn, name, keep, device
+        if stream is None and device.type == "cuda":
+            stream = torch.cuda.current_stream(device)
+        self._args = (*args, 0 if stream is None else stream.cuda_stream)
+
+    def __call__(self):
+        if self._device.type == "cuda" and torch.cuda.current_device() != self._device.index:
+            with torch.cuda.device(self._device):
+                st = self._fn(*self._args)
+        else:
+            st = self._fn(*self._args)
+        if st != DAS_OK:
+            raise DasError(st, self._name)
+
+
+@dataclass
+class QuantCache:
+    """Caller-owned depth-indexed paged cache in 8 bits (layouts as in das.h).
+
+    k_pool: float8_e4m3fn [nK, L, Hkv, P, 8, 8 * dh]; v_pool: float8_e4m3fn
+    [nV, L, Hkv, P, 8, dh, 8]; k_exp / v_exp: uint8 [nK|nV, L, P, Hkv, 8]. `dtype` is
+    the type of queries, block K/V, outputs and committed K/V."""
+    k_pool: torch.Tensor
+    v_pool: torch.Tensor
+    k_exp: torch.Tensor
+    v_exp: torch.Tensor
+    num_depths: int
+    k_plane: Dict[int, int]
+    v_plane: Dict[int, int]
+    dtype: torch.dtype = torch.bfloat16
+    _c: DasCacheQ8C = field(default=None, repr=False)
+
+    def __post_init__(self):
+        self.refresh()
+
+    @classmethod
+    def empty(cls, num_layers: int, num_kv_heads: int, num_pages: int, head_dim: int,
+              num_depths: int, k_plane: Dict[int, int], v_plane: Dict[int, int],
+              dtype: torch.dtype = torch.bfloat16, device="cuda") -> "QuantCache":
+        """An empty cache with planes for the depths that k_plane and v_plane name."""
+        nk, nv = max(k_plane.values()) + 1, max(v_plane.values()) + 1
+        code, at = torch.float8_e4m3fn, (num_layers, num_kv_heads, num_pages, GROUP_TOKENS)
+        exps = (num_layers, num_pages, num_kv_heads, GROUP_TOKENS)
+        return cls(torch.zeros((nk, *at, GROUP_TOKENS * head_dim), dtype=code, device=device),
+                   torch.zeros((nv, *at, head_dim, GROUP_TOKENS), dtype=code, device=device),
+                   torch.full((nk, *exps), 127, dtype=torch.uint8, device=device),
+                   torch.full((nv, *exps), 127, dtype=torch.uint8, device=device),
+                   num_depths, k_plane, v_plane, dtype)
+
+    @property
+    def num_layers(self):
+        return self.k_pool.shape[1]
+
+    @property
+    def num_kv_heads(self):
+        return self.k_pool.shape[2]
+
+    @property
+    def num_pages(self):
+        return self.k_pool.shape[3]
+
+    @property
+    def head_dim(self):
+        return self.v_pool.shape[5]
+
+    @property
+    def device(self):
+        return self.k_pool.device
+
+    def refresh(self):
+        k, v = self.k_pool, self.v_pool
+        if k.dim() != 6 or v.dim() != 7:
+            raise ValueError("k_pool must be 6-d and v_pool 7-d")
+        (nk, L, hkv, P), nv, dh = k.shape[:4], v.shape[0], v.shape[5]
+        code, dev = torch.float8_e4m3fn, k.device
+        _check(k, code, (nk, L, hkv, P, PAGE_TOKENS // GROUP_TOKENS, GROUP_TOKENS * dh), dev, "k_pool")
+        _check(v, code, (nv, L, hkv, P, PAGE_TOKENS // GROUP_TOKENS, dh, GROUP_TOKENS), dev, "v_pool")
+        _check(self.k_exp, torch.uint8, (nk, L, P, hkv, PAGE_TOKENS // GROUP_TOKENS), dev, "k_exp")
+        _check(self.v_exp, torch.uint8, (nv, L, P, hkv, PAGE_TOKENS // GROUP_TOKENS), dev, "v_exp")
+        if self.dtype not in DTYPE_CODES:
+            raise ValueError("dtype must be torch.float32 or torch.bfloat16")
+        c = DasCacheQ8C()
+        b = c.base
+        b.dtype, b.num_depths = DTYPE_CODES[self.dtype], self.num_depths
+        b.num_layers, b.num_kv_heads, b.num_pages, b.head_dim = L, hkv, P, dh
+        b.num_k_planes, b.num_v_planes = nk, nv
+        for r in range(MAX_DEPTH + 1):
+            b.k_plane[r] = self.k_plane.get(r, -1)
+            b.v_plane[r] = self.v_plane.get(r, -1)
+        b.k_pool, b.v_pool = k.data_ptr(), v.data_ptr()
+        c.k_exp, c.v_exp = self.k_exp.data_ptr(), self.v_exp.data_ptr()
+        self._c = c
+        return self
+
+    @property
+    def c(self) -> DasCacheQ8C:
+        return self._c
+
+
+def _check_batch_on(batch: Batch, device):
+    for t, what in ((batch.prefix_len, "prefix_len"), (batch.block_table, "block_table")):
+        if t.device != device:
+            raise ValueError(f"{what} must be on {device}")
+    _check_opt(batch.dev_error, torch.int32, (1,), device, "dev_error")
+
+
+def workspace_bytes_q8(cache: QuantCache, batch: Batch, num_q_heads: int, block_len: int) -> int:
+    return LIB.das_attn_q8_workspace_bytes(ctypes.byref(cache.c), ctypes.byref(batch.c),
+                                           num_q_heads, block_len)
+
+
+def alloc_workspace_q8(cache: QuantCache, batch: Batch, num_q_heads: int,
+                       block_len: int) -> torch.Tensor:
+    n = workspace_bytes_q8(cache, batch, num_q_heads, block_len)
+    if n == 0:
+        raise DasError(-2, "workspace query rejected the shapes")
+    return torch.empty(n, dtype=torch.uint8, device=cache.device)
+
+
+class PreparedAttentionQ8(_Call):
+    """das_attn_q8 with its arguments marshalled up front, for loops that issue the same
+    call many times."""
+
+    def __init__(self, cache: QuantCache, batch: Batch, layer: int, kappa: int, nu: int,
+                 q: torch.Tensor, k_blk: torch.Tensor, v_blk: torch.Tensor, out: torch.Tensor,
+                 workspace: torch.Tensor, lse: Optional[torch.Tensor] = None, stream=None):
+        if q.dim() != 4:
+            raise ValueError("q must be [B, w, Hq, dh]")
+        dev, (B, w, hq, dh) = cache.device, q.shape
+        blk = (batch.batch, w, cache.num_kv_heads, cache.head_dim)
+        q_shape = (batch.batch, w, hq, cache.head_dim)
+        _check_batch_on(batch, dev)
+        if workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
+            raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
+        args = (ctypes.byref(cache.c), ctypes.byref(batch.c), layer, kappa, nu, hq, w,
+                _check(q, cache.dtype, q_shape, dev, "q"),
+                _check(k_blk, cache.dtype, blk, dev, "k_blk"),
+                _check(v_blk, cache.dtype, blk, dev, "v_blk"),
+                _check(out, cache.dtype, q_shape, dev, "out"),
+                _check_opt(lse, torch.float32, (B, hq, w), dev, "lse"),
+                workspace.data_ptr(), workspace.numel())
+        super().__init__(LIB.das_attn_q8, "das_attn_q8", args,
+                         (cache, batch, q, k_blk, v_blk, out, workspace, lse), dev, stream)
+
+
+def attn_policy_q8(cache: QuantCache, batch: Batch, layer: int, kappa: int, nu: int,
+                   q: torch.Tensor, k_blk: torch.Tensor, v_blk: torch.Tensor,
+                   out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Eq. (2)-(3) over an 8-bit cache: prefix keys at depth kappa, values at depth nu."""
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        workspace = alloc_workspace_q8(cache, batch, q.shape[2], q.shape[1])
+    PreparedAttentionQ8(cache, batch, layer, kappa, nu, q, k_blk, v_blk, out, workspace, lse,
+                        stream)()
+    return out
+
+
+class PreparedAppendQ8(_Call):
+    """das_kv_append_q8 with its arguments marshalled up front."""
+
+    def __init__(self, cache: QuantCache, batch: Batch, k_new: torch.Tensor, v_new: torch.Tensor,
+                 num_new: torch.Tensor, len_out: Optional[torch.Tensor] = None, stream=None):
+        if k_new.dim() != 6:
+            raise ValueError("k_new must be [nK, L, B, w_max, Hkv, dh]")
+        dev, w_max = cache.device, k_new.shape[3]
+        tail = (cache.num_layers, batch.batch, w_max, cache.num_kv_heads, cache.head_dim)
+        _check_batch_on(batch, dev)
+        args = (ctypes.byref(cache.c), ctypes.byref(batch.c),
+                _check(k_new, cache.dtype, (cache.k_pool.shape[0], *tail), dev, "k_new"),
+                _check(v_new, cache.dtype, (cache.v_pool.shape[0], *tail), dev, "v_new"), w_max,
+                _check(num_new, torch.int32, (batch.batch,), dev, "num_new"),
+                _check_opt(len_out, torch.int32, (batch.batch,), dev, "len_out"))
+        super().__init__(LIB.das_kv_append_q8, "das_kv_append_q8", args,
+                         (cache, batch, k_new, v_new, num_new, len_out), dev, stream)
+
+
+def kv_append_q8(cache: QuantCache, batch: Batch, k_new: torch.Tensor, v_new: torch.Tensor,
+                 num_new: torch.Tensor, len_out: Optional[torch.Tensor] = None, stream=None):
+    """Commit the first num_new[b] block entries of every plane and layer, in 8 bits."""
+    PreparedAppendQ8(cache, batch, k_new, v_new, num_new, len_out, stream)()
+
+
+class PreparedSample(_Call):
+    """das_sample with its arguments marshalled up front; `tokens` and `probs` hold the
+    results."""
+
+    def __init__(self, logits: torch.Tensor, uniform: torch.Tensor,
+                 temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+                 top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+                 tokens: Optional[torch.Tensor] = None, probs: Optional[torch.Tensor] = None,
+                 dev_error: Optional[torch.Tensor] = None, stream=None):
+        if logits.dim() != 3 or logits.dtype not in DTYPE_CODES:
+            raise ValueError("logits must be a float32 or bfloat16 tensor [B, w, V]")
+        B, w, V = logits.shape
+        dev = logits.device
+        stride = logits.stride(1) if w > 1 else logits.stride(0) if B > 1 else V
+        # rows may lie apart, but evenly in the order [B, w]
+        if V > 1 and logits.stride(2) != 1 or stride < V or (
+                B > 1 and w > 1 and logits.stride(0) != w * stride):
+            raise ValueError("logits must have contiguous rows at one even distance")
+        if tokens is None:
+            tokens = torch.empty((B, w), dtype=torch.int32, device=dev)
+        self.tokens, self.probs = tokens, probs
+        f32 = torch.float32
+        args = (B, w, V, DTYPE_CODES[logits.dtype], logits.data_ptr(), stride,
+                _check_opt(temperature, f32, (B,), dev, "temperature"),
+                _check_opt(top_k, torch.int32, (B,), dev, "top_k"),
+                _check_opt(top_p, f32, (B,), dev, "top_p"),
+                _check_opt(min_p, f32, (B,), dev, "min_p"),
+                _check(uniform, f32, (B, w), dev, "uniform"),
+                _check(tokens, torch.int32, (B, w), dev, "tokens"),
+                _check_opt(probs, f32, (B, w), dev, "probs"),
+                _check_opt(dev_error, torch.int32, (1,), dev, "dev_error"))
+        super().__init__(LIB.das_sample, "das_sample", args,
+                         (logits, uniform, temperature, top_k, top_p, min_p, tokens, probs,
+                          dev_error), dev, stream)
+
+
+def sample(logits: torch.Tensor, uniform: torch.Tensor,
+           temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+           top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+           tokens: Optional[torch.Tensor] = None, probs: Optional[torch.Tensor] = None,
+           dev_error: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """A token for every row of logits [B, w, V] from the random numbers `uniform` [B, w];
+    the filters are per sequence. Returns the tokens, greedy_accept's target_pred."""
+    call = PreparedSample(logits, uniform, temperature, top_k, top_p, min_p, tokens, probs,
+                          dev_error, stream)
+    call()
+    return call.tokens
+
+
+class PreparedPages(_Call):
+    """das_pages_update with its arguments marshalled up front."""
+
+    def __init__(self, lengths: torch.Tensor, block_table: torch.Tensor, pages_held: torch.Tensor,
+                 free_pages: torch.Tensor, num_free: torch.Tensor,
+                 first: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+                 dev_error: Optional[torch.Tensor] = None, stream=None):
+        if block_table.dim() != 2 or free_pages.dim() != 1:
+            raise ValueError("block_table must be [B, max_pages] and free_pages [num_pages]")
+        if (first is None) != (slots is None) or (slots is not None and slots.dim() != 2):
+            raise ValueError("first [B] and slots [B, w] go together")
+        B, dev, i32 = block_table.shape[0], block_table.device, torch.int32
+        w = 0 if slots is None else slots.shape[1]
+        args = (B, block_table.shape[1], free_pages.shape[0],
+                _check(lengths, i32, (B,), dev, "lengths"),
+                _check(block_table, i32, block_table.shape, dev, "block_table"),
+                _check(pages_held, i32, (B,), dev, "pages_held"),
+                _check(free_pages, i32, free_pages.shape, dev, "free_pages"),
+                _check(num_free, i32, (1,), dev, "num_free"),
+                _check_opt(first, i32, (B,), dev, "first"), w,
+                _check_opt(slots, i32, (B, w), dev, "slots"),
+                _check_opt(dev_error, i32, (1,), dev, "dev_error"))
+        super().__init__(LIB.das_pages_update, "das_pages_update", args,
+                         (lengths, block_table, pages_held, free_pages, num_free, first, slots,
+                          dev_error), dev, stream)
+
+
+def pages_update(lengths: torch.Tensor, block_table: torch.Tensor, pages_held: torch.Tensor,
+                 free_pages: torch.Tensor, num_free: torch.Tensor,
+                 first: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+                 dev_error: Optional[torch.Tensor] = None, stream=None):
+    """Give every sequence the pages that lengths [B] ask for and take back the rest; with
+    `first` and `slots` also write the slots of positions first[b] .. in the new table."""
+    PreparedPages(lengths, block_table, pages_held, free_pages, num_free, first, slots, dev_error,
+                  stream)()

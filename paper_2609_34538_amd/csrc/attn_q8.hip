@@ -1,0 +1,645 @@
+// Policy attention (Eq. (2)-(3)) over a cache held in 8 bits: e4m3 codes with one
+// power-of-two scale per 8 tokens and KV head (das_attn_q8).
+//
+// A unit is one (sequence, KV head); its 32-token tiles, the draft block's first,
+// then the prefix's, are cut into chunks of chunk_tiles, one workgroup of four
+// waves each. RW of the waves hold different query rows (16 * NQ each), the other
+// 4 / RW take a chunk's tiles in turn, each with its own running maximum, sum and
+// output; they merge through LDS, and where a unit has several chunks these leave
+// records that a second kernel merges.
+//
+// Both products take the key / value tile as the A operand, as in mfma_tile.h:
+//   S^T (tokens x rows) = K . Q^T,   O^T (dh x rows) += V^T . P^T
+// The page layouts give every lane its operands in 16-byte pieces: a key piece is
+// 8 dims of the two tokens 8 G + n % 4 and + 4 that its two S^T tiles want, a value
+// piece the 8 tokens of two neighbouring dims, which become rows of two O^T tiles.
+// A wave's load is four runs of 256 bytes. Codes become bf16 keys and fp16 values
+// in one instruction per two (v_cvt_scalef32_pk_*_fp8) that applies the scale and
+// is exact.
+//
+// P.V of bf16 calls runs in fp16: e4m3 values are exact there and probabilities
+// keep 11 bits instead of 8 (error against 64 bits then is the output's rounding).
+// Probabilities are held times 2^15, so that fp16 is normal down to 2^-29 of the
+// row's largest; values are held relative to the largest exponent that the wave
+// has met (vref, per wave), which like the running maximum rescales the output
+// when it grows, by a power of two. Draft-block values are bf16 with bf16's range:
+// their probabilities enter as a bf16 and its remainder, two products.
+// fp32 calls use v_mfma_f32_16x16x4_f32 for both products; reduction slots may be
+// numbered freely as long as both operands agree, so the same pieces serve: step i
+// takes a lane's i-th dim or token.
+
+#include "mfma_tile.h"
+#include "q8_internal.h"
+
+namespace das {
+namespace {
+
+typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kTile = 32;
+constexpr int kTilesPerPage = kPage / kTile;
+constexpr int kWavesQ8 = 4;
+constexpr float kProbShift = 15.f;  // bf16 calls: probabilities times 2^15
+
+__device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, a),
+                                                __builtin_bit_cast(h16x8, b), c, 0, 0, 0);
+}
+
+// 8 codes (two words) times `scale`, a power of two.
+__device__ __forceinline__ u32x4 codes_to_bf16(uint32_t lo, uint32_t hi, float scale) {
+  return u32x4{
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
+}
+__device__ __forceinline__ u32x4 codes_to_f16(uint32_t lo, uint32_t hi, float scale) {
+  return u32x4{
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, true)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, true))};
+}
+__device__ __forceinline__ void codes_to_f32(uint32_t lo, uint32_t hi, float scale, float (&x)[8]) {
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(lo, scale, false);
+  const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(lo, scale, true);
+  const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, scale, false);
+  const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, scale, true);
+  x[0] = a[0], x[1] = a[1], x[2] = b[0], x[3] = b[1];
+  x[4] = c[0], x[5] = c[1], x[6] = d[0], x[7] = d[1];
+}
+
+// A tile as loaded: pieces of keys and values, and the exponent bytes of its four
+// token groups (the same words in every lane).
+template <int DH>
+struct Raw {
+  u32x4 k[DH / 32], v[DH / 32];
+  uint32_t ke, ve;
+};
+
+// One wave's running result. bf16 calls: o is in units of 2^vref, o and l times
+// 2^15 (kProbShift).
+template <int DH, int NQ>
+struct Acc {
+  float m[NQ], l[NQ];
+  f32x4 o[NQ][DH / 16];
+  int vref;
+};
+
+// The Q operand of a 16-row tile: bf16 one piece per 32 dims, fp32 two.
+template <typename T, int DH>
+struct QFrag {
+  u32x4 x[DH / 32][sizeof(T) / 2];
+};
+
+// Softmax step of a tile: logits x[qt][e][v] (token 8 g + 4 e + v of the tile, row n)
+// become probabilities in place; the running maximum moves, the output is rescaled
+// where it did, the lane's share of the sum is added.
+template <int DH, int NQ>
+__device__ __forceinline__ void softmax_step(Acc<DH, NQ> &st, f32x4 (&s)[NQ][2],
+                                             const int (&cap)[NQ], int limit, bool full, float scale,
+                                             float shift, int lg) {
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt) {
+    if (!full) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const int t = 8 * lg + 4 * e + v;
+          s[qt][e][v] = ((t < limit) & (t <= cap[qt])) ? s[qt][e][v] : kNegInf;
+        }
+    }
+    float mx = kNegInf;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) mx = fmaxf(mx, s[qt][e][v]);
+    const float mnew = fmaxf(st.m[qt], group_max(mx) * scale);
+    const float ref = mnew == kNegInf ? 0.f : mnew;  // nothing visible yet: every p is 0
+    const float alpha = __builtin_amdgcn_exp2f(st.m[qt] - ref);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][e][v], scale, shift - ref));
+        s[qt][e][v] = p;
+        sum += p;
+      }
+    st.l[qt] = st.l[qt] * alpha + sum;
+    st.m[qt] = mnew;
+    // a lane's accumulators of row tile qt all belong to one row
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
+#pragma unroll
+      for (int dt = 0; dt < DH / 16; ++dt) st.o[qt][dt] *= alpha;
+    }
+  }
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const bf16x2 h = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
+  return __builtin_bit_cast(uint32_t, h);
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const h16x2 h = {static_cast<_Float16>(a), static_cast<_Float16>(b)};
+  return __builtin_bit_cast(uint32_t, h);
+}
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// A tile of the prefix through both products. `limit`: visible tokens.
+template <typename T, int DH, int NQ>
+__device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, const Raw<DH> &t,
+                                            const QFrag<T, DH> (&qf)[NQ], int limit, float scale,
+                                            int ln, int lg) {
+  const bool full = limit >= kTile;
+  const float ks = __uint_as_float(__builtin_amdgcn_ubfe(t.ke, 8 * (ln >> 2), 8) << 23);
+  f32x4 s[NQ][2], odd[NQ][2];  // odd: fp32's second chains, half the roundings each
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt)
+    s[qt][0] = s[qt][1] = odd[qt][0] = odd[qt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < DH / 32; ++k) {
+    if constexpr (sizeof(T) == 2) {
+      const u32x4 a0 = codes_to_bf16(t.k[k][0], t.k[k][1], ks);
+      const u32x4 a1 = codes_to_bf16(t.k[k][2], t.k[k][3], ks);
+#pragma unroll
+      for (int qt = 0; qt < NQ; ++qt) {
+        s[qt][0] = mfma16x16x32(a0, qf[qt].x[k][0], s[qt][0]);
+        s[qt][1] = mfma16x16x32(a1, qf[qt].x[k][0], s[qt][1]);
+      }
+    } else {
+      float a0[8], a1[8];
+      codes_to_f32(t.k[k][0], t.k[k][1], ks, a0);
+      codes_to_f32(t.k[k][2], t.k[k][3], ks, a1);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int qt = 0; qt < NQ; ++qt) {
+          const uint32_t b = qf[qt].x[k][i / 4][i % 4];
+          f32x4 &c0 = i % 2 ? odd[qt][0] : s[qt][0], &c1 = i % 2 ? odd[qt][1] : s[qt][1];
+          c0 = mfma16x16x4(__float_as_uint(a0[i]), b, c0);
+          c1 = mfma16x16x4(__float_as_uint(a1[i]), b, c1);
+        }
+    }
+  }
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int qt = 0; qt < NQ; ++qt) s[qt][0] += odd[qt][0], s[qt][1] += odd[qt][1];
+  }
+  int none[NQ];
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt) none[qt] = 0x7fffffff;
+  softmax_step<DH, NQ>(st, s, none, limit, full, scale, sizeof(T) == 2 ? kProbShift : 0.f, lg);
+
+  const uint32_t vexp = __builtin_amdgcn_ubfe(t.ve, 8 * lg, 8);
+  if constexpr (sizeof(T) == 2) {
+    // the largest exponent of the groups with a visible token, as a wave-uniform value
+    uint32_t w = __builtin_amdgcn_readfirstlane(t.ve);
+    if (!full) w &= limit > 24 ? ~0u : limit > 16 ? 0xffffffu : limit > 8 ? 0xffffu : limit > 0 ? 0xffu : 0u;
+    const int most = max(max(static_cast<int>(w & 255), static_cast<int>(w >> 8 & 255)),
+                         max(static_cast<int>(w >> 16 & 255), static_cast<int>(w >> 24))) - 127;
+    if (most > st.vref) {
+#pragma unroll
+      for (int qt = 0; qt < NQ; ++qt)
+#pragma unroll
+        for (int dt = 0; dt < DH / 16; ++dt)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            st.o[qt][dt][v] = __builtin_amdgcn_ldexpf(st.o[qt][dt][v], st.vref - most);
+      st.vref = most;
+    }
+    const float vs = __uint_as_float(static_cast<uint32_t>(max(static_cast<int>(vexp) - st.vref, 0)) << 23);
+    u32x4 pf[NQ];
+#pragma unroll
+    for (int qt = 0; qt < NQ; ++qt)
+      pf[qt] = u32x4{pack_f16(s[qt][0][0], s[qt][0][1]), pack_f16(s[qt][0][2], s[qt][0][3]),
+                     pack_f16(s[qt][1][0], s[qt][1][1]), pack_f16(s[qt][1][2], s[qt][1][3])};
+    // invisible tokens enter with probability 0; their values are zeroed so that
+    // whatever the page holds there adds nothing
+    u32x4 keep = {~0u, ~0u, ~0u, ~0u};
+    if (!full) keep = value_mask<bf16_t>(limit, lg);
+#pragma unroll
+    for (int k = 0; k < DH / 32; ++k)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        u32x4 a = codes_to_f16(t.v[k][2 * i], t.v[k][2 * i + 1], vs);
+        if (!full) a &= keep;
+#pragma unroll
+        for (int qt = 0; qt < NQ; ++qt) st.o[qt][2 * k + i] = mfma_f16(a, pf[qt], st.o[qt][2 * k + i]);
+      }
+  } else {
+    const float vs = __uint_as_float(vexp << 23);
+#pragma unroll
+    for (int k = 0; k < DH / 32; ++k)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float a[8];
+        codes_to_f32(t.v[k][2 * i], t.v[k][2 * i + 1], vs, a);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (!full) a[j] = 8 * lg + j < limit ? a[j] : 0.f;
+#pragma unroll
+          for (int qt = 0; qt < NQ; ++qt)
+            st.o[qt][2 * k + i] = mfma16x16x4(__float_as_uint(a[j]), __float_as_uint(s[qt][j / 4][j % 4]),
+                                              st.o[qt][2 * k + i]);
+        }
+      }
+  }
+}
+
+// Tile u of the draft block: keys and values in the call's type, straight from the
+// token-major rows (rows past the block's last repeat it and are masked).
+template <typename T, int DH, int NQ>
+__device__ __forceinline__ void block_tile(Acc<DH, NQ> &st, const AttnQ8Params &p, int b, int kvh,
+                                           int u, const QFrag<T, DH> (&qf)[NQ],
+                                           const int (&row_pos)[NQ], int ln, int lg) {
+  const size_t row_elems = static_cast<size_t>(p.hkv) * DH;
+  const size_t base = (static_cast<size_t>(b) * p.w * p.hkv + kvh) * DH;
+  const T *kb = static_cast<const T *>(p.kb) + base, *vb = static_cast<const T *>(p.vb) + base;
+  const int limit = p.w - kTile * u;
+  f32x4 s[NQ][2];
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt) s[qt][0] = s[qt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int tok = min(kTile * u + 8 * (ln >> 2) + (ln & 3) + 4 * e, p.w - 1);
+    const T *row = kb + tok * row_elems;
+#pragma unroll
+    for (int k = 0; k < DH / 32; ++k) {
+      const u32x4 *src = reinterpret_cast<const u32x4 *>(row + 32 * k + 8 * lg);
+      if constexpr (sizeof(T) == 2) {
+        const u32x4 a = src[0];
+#pragma unroll
+        for (int qt = 0; qt < NQ; ++qt) s[qt][e] = mfma16x16x32(a, qf[qt].x[k][0], s[qt][e]);
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const u32x4 a = src[h];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int qt = 0; qt < NQ; ++qt) s[qt][e] = mfma16x16x4(a[i], qf[qt].x[k][h][i], s[qt][e]);
+        }
+      }
+    }
+  }
+  int cap[NQ];
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt) cap[qt] = row_pos[qt] - kTile * u;
+  softmax_step<DH, NQ>(st, s, cap, limit, false, p.scale_log2, sizeof(T) == 2 ? kProbShift : 0.f, lg);
+
+  // values: a lane's 8 tokens of dims 32 k + 2 n and + 1
+  if constexpr (sizeof(T) == 2) {
+    u32x4 hi[NQ], lo[NQ];
+#pragma unroll
+    for (int qt = 0; qt < NQ; ++qt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float a = __builtin_amdgcn_ldexpf(s[qt][j / 2][2 * (j % 2)], -st.vref);
+        const float c = __builtin_amdgcn_ldexpf(s[qt][j / 2][2 * (j % 2) + 1], -st.vref);
+        hi[qt][j] = pack_bf16(a, c);
+        lo[qt][j] = pack_bf16(a - bf16_lo(hi[qt][j]), c - bf16_hi(hi[qt][j]));
+      }
+#pragma unroll
+    for (int k = 0; k < DH / 32; ++k) {
+      u32x4 a0, a1;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t w[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int tok = kTile * u + 8 * lg + 2 * j + h;
+          w[h] = *reinterpret_cast<const uint32_t *>(vb + min(tok, p.w - 1) * row_elems + 32 * k + 2 * ln);
+          if (tok >= p.w) w[h] = 0;
+        }
+        a0[j] = (w[0] & 0xffffu) | (w[1] << 16);
+        a1[j] = (w[0] >> 16) | (w[1] & 0xffff0000u);
+      }
+#pragma unroll
+      for (int qt = 0; qt < NQ; ++qt) {
+        st.o[qt][2 * k] = mfma16x16x32(a0, lo[qt], st.o[qt][2 * k]);
+        st.o[qt][2 * k + 1] = mfma16x16x32(a1, lo[qt], st.o[qt][2 * k + 1]);
+        st.o[qt][2 * k] = mfma16x16x32(a0, hi[qt], st.o[qt][2 * k]);
+        st.o[qt][2 * k + 1] = mfma16x16x32(a1, hi[qt], st.o[qt][2 * k + 1]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < DH / 32; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int tok = kTile * u + 8 * lg + j;
+        u32x2 w = *reinterpret_cast<const u32x2 *>(vb + min(tok, p.w - 1) * row_elems + 32 * k + 2 * ln);
+        if (tok >= p.w) w = u32x2{0, 0};
+#pragma unroll
+        for (int qt = 0; qt < NQ; ++qt) {
+          const uint32_t pj = __float_as_uint(s[qt][j / 4][j % 4]);
+          st.o[qt][2 * k] = mfma16x16x4(w[0], pj, st.o[qt][2 * k]);
+          st.o[qt][2 * k + 1] = mfma16x16x4(w[1], pj, st.o[qt][2 * k + 1]);
+        }
+      }
+  }
+}
+
+template <typename T, int DH, int NQ, int RW>
+__global__ __launch_bounds__(64 * kWavesQ8) __attribute__((amdgpu_waves_per_eu(2)))
+void attn_q8_kernel(AttnQ8Params p, int n_rg) {
+  constexpr int IW = kWavesQ8 / RW;   // waves that share a chunk's tiles
+  constexpr int RS = DH + 4;          // row stride of the merge area (floats)
+  constexpr int KS = DH / 32;
+  __shared__ __attribute__((aligned(16))) float part[kWavesQ8][16 * RS];
+  __shared__ float sm[kWavesQ8][16 * NQ], sl[kWavesQ8][16 * NQ], sa[kWavesQ8][16 * NQ];
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int ln = lane & 15, lg = lane >> 4;
+  const int rw = wave % RW, iw = wave / RW;
+  // every unit's first chunk comes before any second one
+  const int units = p.batch * p.hkv;
+  const int rg = blockIdx.x % n_rg, grp = blockIdx.x / n_rg;
+  const int unit = grp % units, chunk = grp / units;
+  const int b = unit / p.hkv, kvh = unit % p.hkv;
+  const int row0 = rg * (16 * NQ * RW) + rw * (16 * NQ);
+  const int nb = (p.w + kTile - 1) / kTile;
+  const int g0 = chunk * p.chunk_tiles + iw;  // this wave's first tile of the unit
+
+  const int s_raw = p.prefix_len[b];
+  QFrag<T, DH> qf[NQ];
+  int row_pos[NQ];
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt) {
+    // rows past the last are clamped; their outputs are never written
+    const int row = min(row0 + qt * 16 + ln, p.rows - 1);
+    const int i = row / p.group, g = row % p.group;
+    row_pos[qt] = i;
+    const T *qrow = static_cast<const T *>(p.q) +
+                    ((static_cast<size_t>(b) * p.w + i) * p.hq + kvh * p.group + g) * DH;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int h = 0; h < static_cast<int>(sizeof(T)) / 2; ++h)
+        qf[qt].x[k][h] = reinterpret_cast<const u32x4 *>(qrow + 32 * k + 8 * lg)[h];
+  }
+  // page ids: lane i holds the page of this wave's (window + i)-th tile
+  auto load_window = [&](int first) {
+    const int pg = (g0 + IW * (first + lane) - nb) / kTilesPerPage;
+    return g0 + IW * (first + lane) >= nb && pg < p.max_pages
+               ? p.block_table[static_cast<size_t>(b) * p.max_pages + pg] : 0;
+  };
+  int window = load_window(0);
+
+  bool bad;
+  const int S = clamp_prefix(s_raw, p.max_pages, &bad);
+  if (bad && kvh == 0 && rg == 0 && chunk == 0 && threadIdx.x == 0)
+    report_error(p.dev_error, DAS_DEVERR_PREFIX);
+  const int ntile = nb + (S + kTile - 1) / kTile;
+  const int nsb = (ntile + p.chunk_tiles - 1) / p.chunk_tiles;  // chunks of this unit
+  if (chunk >= nsb) return;
+  const int g_end = min(ntile, (chunk + 1) * p.chunk_tiles);
+  const int n = g_end > g0 ? (g_end - g0 + IW - 1) / IW : 0;  // this wave's tiles
+
+  Acc<DH, NQ> st;
+  st.vref = kQ8MinExp;
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt) {
+    st.m[qt] = kNegInf;
+    st.l[qt] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DH / 16; ++dt) st.o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const uint32_t lane_k = (ln >> 2) * 8 * DH + lg * 64 + (ln & 3) * 16;
+  const uint32_t lane_v = lg * 8 * DH + ln * 16;
+  // Loads of the wave's i-th tile; the number of its visible tokens comes back. An
+  // out-of-range page id is reported and read as page 0 (its tile is masked out).
+  auto load = [&](int i, Raw<DH> &t) {
+    if (i >= 64 && i % 64 == 0) window = load_window(i);
+    const int page_raw = __builtin_amdgcn_readlane(window, i & 63);
+    const bool ok = page_raw >= 0 && page_raw < p.num_pages;
+    if (!ok) report_error(p.dev_error, DAS_DEVERR_PAGE);
+    const int page = ok ? page_raw : 0;
+    const int tile = g0 + IW * i - nb, half = tile % kTilesPerPage;
+    const size_t off = (static_cast<size_t>(kvh) * p.num_pages + page) * (kPage * DH) + half * kTile * DH;
+    const size_t eoff = (static_cast<size_t>(page) * p.hkv + kvh) * kQ8GroupsPerPage + 4 * half;
+    const auto rk = buffer_of(p.k_layer + off, kTile * DH), rv = buffer_of(p.v_layer + off, kTile * DH);
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+      t.k[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, lane_k, 256 * k, kNonTemporal));
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+      t.v[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, lane_v, 256 * k, kNonTemporal));
+    t.ke = *reinterpret_cast<const uint32_t *>(p.k_exp + eoff);
+    t.ve = *reinterpret_cast<const uint32_t *>(p.v_exp + eoff);
+    return ok ? min(kTile, S - kTile * tile) : 0;
+  };
+
+  // draft-block tiles come first: tiles 0 .. nb - 1 of chunk 0
+  int i = 0;
+  for (; i < n && g0 + IW * i < nb; ++i)
+    block_tile<T, DH, NQ>(st, p, b, kvh, g0 + IW * i, qf, row_pos, ln, lg);
+  // two tiles in flight
+  Raw<DH> ta, tb;
+  int la = 0, lb = 0;
+  if (i < n) la = load(i, ta);
+  if (i + 1 < n) lb = load(i + 1, tb);
+  for (; i < n; i += 2) {
+    prefix_tile<T, DH, NQ>(st, ta, qf, la, p.scale_log2, ln, lg);
+    if (i + 2 < n) la = load(i + 2, ta);
+    if (i + 1 >= n) break;
+    prefix_tile<T, DH, NQ>(st, tb, qf, lb, p.scale_log2, ln, lg);
+    if (i + 3 < n) lb = load(i + 3, tb);
+  }
+
+  // From here on m, l and o are the plain ones: o unnormalised, without shifts.
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt) {
+    st.l[qt] = group_sum(st.l[qt]);
+    if constexpr (sizeof(T) == 2) {
+      st.l[qt] *= 0x1p-15f;
+#pragma unroll
+      for (int dt = 0; dt < DH / 16; ++dt)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          st.o[qt][dt][v] = __builtin_amdgcn_ldexpf(st.o[qt][dt][v], st.vref - 15);
+    }
+  }
+  uint8_t *rec = p.ws + (static_cast<size_t>(unit) * p.nsplit + chunk) * p.piece_stride;
+  // Merge of the waves' results: every row's maxima and sums first, then, one
+  // 16-row tile at a time, the outputs scaled to the common maximum.
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt) {
+    float amax = 0.f;
+    if (sizeof(T) == 2 && nsb > 1) {
+#pragma unroll
+      for (int dt = 0; dt < DH / 16; ++dt)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) amax = fmaxf(amax, fabsf(st.o[qt][dt][v]));
+      amax = group_max(amax);
+    }
+    if (lg == 0) {
+      sm[wave][16 * qt + ln] = st.m[qt];
+      sl[wave][16 * qt + ln] = st.l[qt];
+      sa[wave][16 * qt + ln] = amax;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt) {
+    float mx = kNegInf;
+#pragma unroll
+    for (int k = 0; k < IW; ++k) mx = fmaxf(mx, sm[k * RW + rw][16 * qt + ln]);
+    // no visible position in the whole chunk (an unreadable page): outputs are 0
+    const float ref = mx == kNegInf ? 0.f : mx;
+    const float sc = __builtin_amdgcn_exp2f(st.m[qt] - ref);
+    if (qt > 0) __syncthreads();  // the previous row tile has been summed
+    // tile 2 k + i of a lane holds dims 32 k + 8 g + 2 v + i
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const f32x4 x = st.o[qt][2 * k] * sc, y = st.o[qt][2 * k + 1] * sc;
+      float *dst = &part[wave][ln * RS + 32 * k + 8 * lg];
+      *reinterpret_cast<f32x4 *>(dst) = f32x4{x[0], y[0], x[1], y[1]};
+      *reinterpret_cast<f32x4 *>(dst + 4) = f32x4{x[2], y[2], x[3], y[3]};
+    }
+    __syncthreads();
+    constexpr int CG = DH / 4;
+    for (int item = threadIdx.x; item < RW * 16 * CG; item += 64 * kWavesQ8) {
+      const int wr = item / (16 * CG), r = item / CG % 16, c = 4 * (item % CG);
+      const int row = rg * (16 * NQ * RW) + wr * (16 * NQ) + 16 * qt + r;
+      if (row >= p.rows) continue;
+      float m2 = kNegInf;
+#pragma unroll
+      for (int k = 0; k < IW; ++k) m2 = fmaxf(m2, sm[k * RW + wr][16 * qt + r]);
+      const float ref2 = m2 == kNegInf ? 0.f : m2;
+      float den = 0.f, bound = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < IW; ++k) {
+        const int src = k * RW + wr;
+        const float sck = __builtin_amdgcn_exp2f(sm[src][16 * qt + r] - ref2);
+        den += sck * sl[src][16 * qt + r];
+        bound += sck * sa[src][16 * qt + r];
+        o += *reinterpret_cast<const f32x4 *>(&part[src][r * RS + c]);
+      }
+      if (nsb > 1) {
+        write_piece_item<T, DH>(rec, p.rows, row, c, o, m2, den, bound);
+        continue;
+      }
+      const int pos = row / p.group, h = kvh * p.group + row % p.group;
+      store_out4(static_cast<T *>(p.out) + ((static_cast<size_t>(b) * p.w + pos) * p.hq + h) * DH + c,
+                 o * (1.f / den));
+      if (p.lse && c == 0)
+        p.lse[(static_cast<size_t>(b) * p.hq + h) * p.w + pos] =
+            (m2 + log2f(den)) * 0.69314718055994530942f;
+    }
+  }
+}
+
+// Merge of the chunks of a unit: a thread per (row, 4 columns), the first kEagerQ8
+// records of an item in flight at once.
+constexpr int kEagerQ8 = 8;
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void attn_q8_combine_kernel(AttnQ8Params p) {
+  constexpr int CG = DH / 4, RB = rec_elem_bytes(sizeof(T));
+  typedef typename RecVec<T>::type Ov;
+  const int unit = blockIdx.x, b = unit / p.hkv, kvh = unit % p.hkv;
+  const int item = blockIdx.y * 256 + threadIdx.x;
+  if (item >= p.rows * CG) return;
+  const int row = item / CG, c = 4 * (item % CG);
+  const size_t stride = static_cast<size_t>(p.piece_stride);
+  const uint8_t *rec = p.ws + static_cast<size_t>(unit) * p.nsplit * stride;
+  const uint8_t *orow = rec + (row * DH + c) * RB, *mrow = rec + p.rows * DH * RB + row * 16;
+  const int s_raw = p.prefix_len[b];
+  f32x4 meta[kEagerQ8];
+  Ov ov[kEagerQ8];
+#pragma unroll
+  for (int k = 0; k < kEagerQ8; ++k) {
+    if (k < p.nsplit) {
+      meta[k] = *reinterpret_cast<const f32x4 *>(mrow + k * stride);
+      ov[k] = *reinterpret_cast<const Ov *>(orow + k * stride);
+    }
+  }
+  bool bad;
+  const int S = clamp_prefix(s_raw, p.max_pages, &bad);
+  const int ntile = (p.w + kTile - 1) / kTile + (S + kTile - 1) / kTile;
+  const int ns = (ntile + p.chunk_tiles - 1) / p.chunk_tiles;
+  if (ns <= 1) return;  // written by the attention kernel
+  float mx = kNegInf, den = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < kEagerQ8; ++k) mx = k < ns ? fmaxf(mx, meta[k][0]) : mx;
+  // the first chunk holds the block's diagonal, so mx is finite
+#pragma unroll
+  for (int k = 0; k < kEagerQ8; ++k) {
+    if (k < ns) {
+      const float sc = exp2f(meta[k][0] - mx), wt = sc * meta[k][2];
+      den += sc * meta[k][1];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) o[v] += wt * static_cast<float>(ov[k][v]);
+    }
+  }
+  for (int k = kEagerQ8; k < ns; ++k) {
+    const f32x4 mk = *reinterpret_cast<const f32x4 *>(mrow + k * stride);
+    const Ov x = *reinterpret_cast<const Ov *>(orow + k * stride);
+    const float nm = fmaxf(mx, mk[0]);
+    const float a = exp2f(mx - nm), sc = exp2f(mk[0] - nm), wt = sc * mk[2];
+    den = den * a + sc * mk[1];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) o[v] = o[v] * a + wt * static_cast<float>(x[v]);
+    mx = nm;
+  }
+  const int pos = row / p.group, h = kvh * p.group + row % p.group;
+  store_out4(static_cast<T *>(p.out) + ((static_cast<size_t>(b) * p.w + pos) * p.hq + h) * DH + c,
+             o * (1.f / den));
+  if (p.lse && c == 0)
+    p.lse[(static_cast<size_t>(b) * p.hq + h) * p.w + pos] = (mx + log2f(den)) * 0.69314718055994530942f;
+}
+
+template <typename T, int DH, int NQ>
+hipError_t launch_tiles(const AttnQ8Params &p, int rw, hipStream_t s) {
+  const int gr = 16 * NQ * rw, n_rg = (p.rows + gr - 1) / gr;
+  const dim3 grid(static_cast<unsigned>(p.batch) * p.hkv * p.nsplit * n_rg), block(64 * kWavesQ8);
+  if (rw == 1) return launch_kernel(attn_q8_kernel<T, DH, NQ, 1>, grid, block, s, p, n_rg);
+  if (rw == 2) return launch_kernel(attn_q8_kernel<T, DH, NQ, 2>, grid, block, s, p, n_rg);
+  return launch_kernel(attn_q8_kernel<T, DH, NQ, 4>, grid, block, s, p, n_rg);
+}
+
+template <typename T, int DH>
+hipError_t launch_dh(const AttnQ8Params &p, hipStream_t s) {
+  constexpr int ES = sizeof(T);
+  const int rw = q8_row_waves(p.rows, DH, ES);
+  hipError_t e;
+  if constexpr (ES == 4 && DH == 128) {
+    e = launch_tiles<T, DH, 1>(p, rw, s);
+  } else {  // one row tile: no more than one wave has rows
+    e = q8_row_tiles(p.rows, DH, ES) == 1
+            ? launch_kernel(attn_q8_kernel<T, DH, 1, 1>,
+                            dim3(static_cast<unsigned>(p.batch) * p.hkv * p.nsplit),
+                            dim3(64 * kWavesQ8), s, p, 1)
+            : launch_tiles<T, DH, 2>(p, rw, s);
+  }
+  if (e != hipSuccess || p.nsplit == 1) return e;
+  const dim3 merge(static_cast<unsigned>(p.batch) * p.hkv, (p.rows * (DH / 4) + 255) / 256);
+  return launch_kernel(attn_q8_combine_kernel<T, DH>, merge, dim3(256), s, p);
+}
+
+}  // namespace
+
+hipError_t launch_attn_q8(const AttnQ8Params &p, int dtype, int dh, hipStream_t s) {
+  if (dtype == DAS_F32) {
+    if (dh == 64) return launch_dh<float, 64>(p, s);
+    if (dh == 96) return launch_dh<float, 96>(p, s);
+    return launch_dh<float, 128>(p, s);
+  }
+  if (dh == 64) return launch_dh<bf16_t, 64>(p, s);
+  if (dh == 96) return launch_dh<bf16_t, 96>(p, s);
+  return launch_dh<bf16_t, 128>(p, s);
+}
+
+}  // namespace das
