@@ -253,12 +253,49 @@ __device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, const Raw<DH> &t,
   }
 }
 
+// Two packed bf16 with what is not finite replaced by 0; `odd` collects whether any was.
+__device__ __forceinline__ uint32_t finite_bf16(uint32_t w, bool &odd) {
+  const bool lo = (w & 0x7f80u) == 0x7f80u, hi = (w & 0x7f800000u) == 0x7f800000u;
+  odd |= lo | hi;
+  return (lo ? 0u : w & 0xffffu) | (hi ? 0u : w & 0xffff0000u);
+}
+__device__ __forceinline__ uint32_t finite_f32(uint32_t w, bool &odd) {
+  const bool is = (w & 0x7f800000u) == 0x7f800000u;
+  odd |= is;
+  return is ? 0u : w;
+}
+
+// What finite_* took out of a draft-block tile's values, for the rows that see it: in a
+// product 0 * NaN would reach the rows that do not. probs: the tile's probabilities,
+// [row tile][row][token].
+template <typename T, int DH, int NQ>
+__device__ __forceinline__ void add_not_finite(Acc<DH, NQ> &st, const float *probs, const T *vb,
+                                               size_t row_elems, int t0, int w, const int (&cap)[NQ],
+                                               int ln, int lg) {
+#pragma unroll
+  for (int k = 0; k < DH / 32; ++k) {
+#pragma unroll 1
+    for (int t = 0; t < kTile && t0 + t < w; ++t) {
+      const T *src = vb + (t0 + t) * row_elems + 32 * k + 8 * lg;
+#pragma unroll
+      for (int qt = 0; qt < NQ; ++qt) {
+        const float pt = probs[(16 * qt + ln) * kTile + t];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {  // tile 2 k + i % 2 holds dim 32 k + 8 g + i
+          const float x = to_f32<T>(src[i]);
+          if (!(fabsf(x) < __builtin_huge_valf()) && t <= cap[qt]) st.o[qt][2 * k + i % 2][i / 2] += pt * x;
+        }
+      }
+    }
+  }
+}
+
 // Tile u of the draft block: keys and values in the call's type, straight from the
 // token-major rows (rows past the block's last repeat it and are masked).
 template <typename T, int DH, int NQ>
 __device__ __forceinline__ void block_tile(Acc<DH, NQ> &st, const AttnQ8Params &p, int b, int kvh,
                                            int u, const QFrag<T, DH> (&qf)[NQ],
-                                           const int (&row_pos)[NQ], int ln, int lg) {
+                                           const int (&row_pos)[NQ], float *probs, int ln, int lg) {
   const size_t row_elems = static_cast<size_t>(p.hkv) * DH;
   const size_t base = (static_cast<size_t>(b) * p.w * p.hkv + kvh) * DH;
   const T *kb = static_cast<const T *>(p.kb) + base, *vb = static_cast<const T *>(p.vb) + base;
@@ -294,57 +331,61 @@ __device__ __forceinline__ void block_tile(Acc<DH, NQ> &st, const AttnQ8Params &
   for (int qt = 0; qt < NQ; ++qt) cap[qt] = row_pos[qt] - kTile * u;
   softmax_step<DH, NQ>(st, s, cap, limit, false, p.scale_log2, sizeof(T) == 2 ? kProbShift : 0.f, lg);
 
-  // values: a lane's 8 tokens of dims 32 k + 2 n and + 1
-  if constexpr (sizeof(T) == 2) {
-    u32x4 hi[NQ], lo[NQ];
 #pragma unroll
-    for (int qt = 0; qt < NQ; ++qt)
+  for (int qt = 0; qt < NQ; ++qt) {
+    f32x4 *dst = reinterpret_cast<f32x4 *>(probs + (16 * qt + ln) * kTile + 8 * lg);
+    dst[0] = s[qt][0], dst[1] = s[qt][1];
+  }
+
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+
+  // values: a lane's 8 tokens of dims 32 k + 2 n and + 1; one row tile after the other,
+  // which reads them again but needs fewer registers than the tiles of the prefix
+  bool odd = false;
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt) {
+    asm volatile("" ::: "memory");
+    u32x4 hi, lo;
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float a = __builtin_amdgcn_ldexpf(s[qt][j / 2][2 * (j % 2)], -st.vref);
         const float c = __builtin_amdgcn_ldexpf(s[qt][j / 2][2 * (j % 2) + 1], -st.vref);
-        hi[qt][j] = pack_bf16(a, c);
-        lo[qt][j] = pack_bf16(a - bf16_lo(hi[qt][j]), c - bf16_hi(hi[qt][j]));
+        hi[j] = pack_bf16(a, c);
+        lo[j] = pack_bf16(a - bf16_lo(hi[j]), c - bf16_hi(hi[j]));
       }
+    }
 #pragma unroll
     for (int k = 0; k < DH / 32; ++k) {
       u32x4 a0, a1;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint32_t w[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int tok = kTile * u + 8 * lg + 2 * j + h;
-          w[h] = *reinterpret_cast<const uint32_t *>(vb + min(tok, p.w - 1) * row_elems + 32 * k + 2 * ln);
-          if (tok >= p.w) w[h] = 0;
-        }
-        a0[j] = (w[0] & 0xffffu) | (w[1] << 16);
-        a1[j] = (w[0] >> 16) | (w[1] & 0xffff0000u);
-      }
-#pragma unroll
-      for (int qt = 0; qt < NQ; ++qt) {
-        st.o[qt][2 * k] = mfma16x16x32(a0, lo[qt], st.o[qt][2 * k]);
-        st.o[qt][2 * k + 1] = mfma16x16x32(a1, lo[qt], st.o[qt][2 * k + 1]);
-        st.o[qt][2 * k] = mfma16x16x32(a0, hi[qt], st.o[qt][2 * k]);
-        st.o[qt][2 * k + 1] = mfma16x16x32(a1, hi[qt], st.o[qt][2 * k + 1]);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < DH / 32; ++k)
-#pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int tok = kTile * u + 8 * lg + j;
-        u32x2 w = *reinterpret_cast<const u32x2 *>(vb + min(tok, p.w - 1) * row_elems + 32 * k + 2 * ln);
-        if (tok >= p.w) w = u32x2{0, 0};
-#pragma unroll
-        for (int qt = 0; qt < NQ; ++qt) {
+        const T *src = vb + min(tok, p.w - 1) * row_elems + 32 * k + 2 * ln;
+        if constexpr (sizeof(T) == 2) {
+          uint32_t x = *reinterpret_cast<const uint32_t *>(src);
+          x = tok < p.w ? finite_bf16(x, odd) : 0u;
+          if (j % 2 == 0) a0[j / 2] = x & 0xffffu, a1[j / 2] = x >> 16;
+          else a0[j / 2] |= x << 16, a1[j / 2] |= x & 0xffff0000u;
+        } else {
+          const u32x2 x = *reinterpret_cast<const u32x2 *>(src);
           const uint32_t pj = __float_as_uint(s[qt][j / 4][j % 4]);
-          st.o[qt][2 * k] = mfma16x16x4(w[0], pj, st.o[qt][2 * k]);
-          st.o[qt][2 * k + 1] = mfma16x16x4(w[1], pj, st.o[qt][2 * k + 1]);
+          st.o[qt][2 * k] = mfma16x16x4(tok < p.w ? finite_f32(x[0], odd) : 0u, pj, st.o[qt][2 * k]);
+          st.o[qt][2 * k + 1] = mfma16x16x4(tok < p.w ? finite_f32(x[1], odd) : 0u, pj, st.o[qt][2 * k + 1]);
         }
       }
+      if constexpr (sizeof(T) == 2) {
+        st.o[qt][2 * k] = mfma16x16x32(a0, lo, st.o[qt][2 * k]);
+        st.o[qt][2 * k + 1] = mfma16x16x32(a1, lo, st.o[qt][2 * k + 1]);
+        st.o[qt][2 * k] = mfma16x16x32(a0, hi, st.o[qt][2 * k]);
+        st.o[qt][2 * k + 1] = mfma16x16x32(a1, hi, st.o[qt][2 * k + 1]);
+      }
+    }
   }
+  if (__builtin_amdgcn_ballot_w64(odd) != 0)
+    add_not_finite<T, DH, NQ>(st, probs, vb, row_elems, kTile * u, p.w, cap, ln, lg);
 }
 
 template <typename T, int DH, int NQ, int RW>
@@ -353,7 +394,9 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
   constexpr int IW = kWavesQ8 / RW;   // waves that share a chunk's tiles
   constexpr int RS = DH + 4;          // row stride of the merge area (floats)
   constexpr int KS = DH / 32;
+  // the merge area of one row tile; before that, a draft-block tile's probabilities
   __shared__ __attribute__((aligned(16))) float part[kWavesQ8][16 * RS];
+  static_assert(16 * RS >= 16 * NQ * kTile, "a tile's probabilities fit");
   __shared__ float sm[kWavesQ8][16 * NQ], sl[kWavesQ8][16 * NQ], sa[kWavesQ8][16 * NQ];
 
   const int lane = threadIdx.x & 63;
@@ -442,7 +485,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
   // draft-block tiles come first: tiles 0 .. nb - 1 of chunk 0
   int i = 0;
   for (; i < n && g0 + IW * i < nb; ++i)
-    block_tile<T, DH, NQ>(st, p, b, kvh, g0 + IW * i, qf, row_pos, ln, lg);
+    block_tile<T, DH, NQ>(st, p, b, kvh, g0 + IW * i, qf, row_pos, part[wave], ln, lg);
   // two tiles in flight
   Raw<DH> ta, tb;
   int la = 0, lb = 0;

@@ -1,0 +1,222 @@
+"""Attention over the 8-bit cache against the 64-bit oracle on the decoded cache: types,
+head dims, head layouts, widths, lengths around tiles and pages, unlike exponents, NaN
+codes in every place that holds no token, unreadable pages, streams and graphs."""
+
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_34538_amd import _lib as das
+from q8_ref import HostCache, attention, random_cache, tolerance
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def _block(seed, dtype, B, w, hq, hkv, dh, gain=1.0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    r = lambda h: torch.randn((B, w, h, dh), generator=g, device=DEV)  # noqa: E731
+    return (r(hq) * gain).to(dtype), r(hkv).to(dtype), r(hkv).to(dtype)
+
+
+def _check(cache, batch, table, lens, q, kb, vb, out, lse, seqs=None, layer=0, kappa=1, nu=1):
+    host = HostCache(cache)
+    for b in range(len(lens)) if seqs is None else seqs:
+        ref, rl, a, size = attention(host, table, lens, b, layer, kappa - 1, nu - 1, q, kb, vb)
+        got = out[b].double().cpu().numpy()
+        tol = tolerance(cache.dtype, ref, a, size, lens[b] + q.shape[1], q.shape[3])
+        err = np.abs(got - ref)
+        assert (err <= tol).all(), (b, lens[b], float((err / tol).max()))
+        # the logit's and the sum's share of the bound, in the logarithm, and its fp32 steps
+        lt = 2 * (q.shape[3] + 8) * 2.0 ** -24 * size + 2 * (lens[b] + 80) * 2.0 ** -24 + 2.0 ** -22 * np.abs(rl)
+        le = np.abs(lse[b].double().cpu().numpy() - rl)
+        assert (le <= lt).all(), (b, lens[b], float((le / lt).max()))
+
+
+CASES = [  # dtype, dh, hkv, group, w, lens, spread
+    (BF16, 64, 2, 1, 1, [0, 1, 7, 8, 9], 0),
+    (BF16, 96, 3, 1, 4, [31, 32, 33, 63, 64, 65, 127, 128, 129], 1),
+    (BF16, 128, 2, 4, 8, [300, 0, 95], 2),
+    (BF16, 128, 1, 8, 64, [1000, 77], 0),
+    (BF16, 64, 4, 7, 5, [640, 513], 1),
+    (BF16, 96, 2, 2, 33, [200, 1], 1),
+    (BF16, 96, 55, 1, 16, [700], 0),
+    (BF16, 64, 1, 1, 64, [4097], 1),
+    (BF16, 128, 2, 1, 1, [9000, 3], 0),
+    (F32, 64, 4, 1, 4, [256, 0, 1], 0),
+    (F32, 96, 2, 1, 17, [65, 500], 2),
+    (F32, 96, 1, 8, 11, [129], 1),
+    (F32, 128, 2, 4, 32, [333, 64], 1),
+    (F32, 128, 1, 1, 1, [2500, 8], 0),
+    (F32, 64, 1, 8, 64, [50], 0),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{str(c[0])[6:]}-dh{c[1]}-h{c[2]}x{c[3]}-w{c[4]}-{c[5][0]}")
+def test_matches_the_oracle(case):
+    dtype, dh, hkv, G, w, lens, spread = case
+    B = len(lens)
+    cache, batch, table = random_cache(7, dtype, B, hkv, dh, lens, spread=spread)
+    q, kb, vb = _block(11, dtype, B, w, hkv * G, hkv, dh)
+    lse = torch.full((B, hkv * G, w), float("nan"), device=DEV)
+    out = das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb,
+                             out=torch.full_like(q, float("nan")), lse=lse)
+    _check(cache, batch, table, lens, q, kb, vb, out, lse)
+    assert int(batch.dev_error) == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_plane_layer_and_policy(dtype):
+    """Keys of depth 2 and values of depth 3 at layer 1 are the ones that are read."""
+    lens = [130, 40]
+    cache, batch, table = random_cache(3, dtype, 2, 2, 64, lens, layers=2, nk=2, nv=3)
+    q, kb, vb = _block(4, dtype, 2, 6, 4, 2, 64)
+    lse = torch.empty((2, 4, 6), device=DEV)
+    out = das.attn_policy_q8(cache, batch, 1, 2, 3, q, kb, vb, lse=lse)
+    _check(cache, batch, table, lens, q, kb, vb, out, lse, layer=1, kappa=2, nu=3)
+
+
+def test_many_long_units_one_chunk_each():
+    """More units than workgroups, row tiles on every wave: a wave takes over 64 tiles of
+    one chunk (a second window of page ids)."""
+    B, hkv, dh, lens = 70, 16, 64, [5000] * 70
+    cache = das.QuantCache.empty(1, hkv, 80, dh, 1, {1: 0}, {1: 0})
+    g = torch.Generator(device=DEV).manual_seed(1)
+    for pool in (cache.k_pool, cache.v_pool):
+        pool.copy_((torch.randn(pool.shape, generator=g, device=DEV)).to(torch.float8_e4m3fn))
+    table = np.stack([np.random.default_rng(b).permutation(80)[:79] for b in range(B)]).astype(np.int32)
+    batch = das.Batch(torch.full((B,), 5000, dtype=torch.int32, device=DEV),
+                      torch.as_tensor(table, device=DEV))
+    q, kb, vb = _block(2, BF16, B, 10, 8 * hkv, hkv, dh)
+    lse = torch.empty((B, 8 * hkv, 10), device=DEV)
+    out = das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb, lse=lse)
+    _check(cache, batch, table, lens, q, kb, vb, out, lse, seqs=[0, 69])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_unlike_exponents(dtype):
+    """Scales of a unit's groups over 2^-30 .. 2^30: values far below the largest count
+    by their share of the sum only."""
+    lens = [257, 700]
+    cache, batch, table = random_cache(5, dtype, 2, 2, 96, lens)
+    rng = np.random.default_rng(0)
+    e = rng.integers(97, 158, size=cache.v_exp.shape).astype(np.uint8)
+    cache.v_exp.copy_(torch.where(cache.v_exp == 255, cache.v_exp, torch.as_tensor(e, device=DEV)))
+    q, kb, vb = _block(6, dtype, 2, 9, 2, 2, 96)
+    lse = torch.empty((2, 2, 9), device=DEV)
+    out = das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb, lse=lse)
+    _check(cache, batch, table, lens, q, kb, vb, out, lse)
+
+
+def test_small_scales_are_kept():
+    """A cache whose values are all tiny gives outputs of that size to full precision where
+    the block adds nothing."""
+    lens = [500]
+    cache, batch, table = random_cache(5, BF16, 1, 1, 64, lens)
+    cache.v_exp.sub_(50)  # values about 2^-50; bytes of empty groups are still garbage
+    q, kb, vb = _block(6, BF16, 1, 3, 1, 1, 64)
+    vb.zero_()
+    lse = torch.empty((1, 1, 3), device=DEV)
+    out = das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb, lse=lse)
+    _check(cache, batch, table, lens, q, kb, vb, out, lse)
+
+
+def test_large_logits():
+    lens = [900, 65]
+    cache, batch, table = random_cache(9, BF16, 2, 2, 128, lens)
+    cache.k_exp.copy_(torch.where(cache.k_exp == 255, 255, 127 - 7 + 2))
+    q, kb, vb = _block(3, BF16, 2, 7, 4, 2, 128, gain=4.0)
+    lse = torch.empty((2, 4, 7), device=DEV)
+    out = das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb, lse=lse)
+    _check(cache, batch, table, lens, q, kb, vb, out, lse)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_unreadable_pages_are_skipped_and_reported(dtype):
+    lens = [700, 130]
+    cache, batch, table = random_cache(8, dtype, 2, 2, 96, lens)
+    bad = table.copy()
+    bad[0, 3], bad[0, 4], bad[1, 0] = cache.num_pages, -5, 2 ** 31 - 1
+    batch = das.Batch(batch.prefix_len, torch.as_tensor(bad, device=DEV), batch.dev_error)
+    q, kb, vb = _block(3, dtype, 2, 8, 2, 2, 96)
+    out = das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb)
+    assert int(batch.dev_error) == das.DEVERR_PAGE
+    host = HostCache(cache)
+    for b in range(2):
+        keep = np.array([bad[b, i // 64] == table[b, i // 64] for i in range(lens[b])])
+        ref, _, a, size = attention(host, table, lens, b, 0, 0, 0, q, kb, vb, keep=keep)
+        tol = tolerance(dtype, ref, a, size, lens[b] + 8, 96)
+        assert (np.abs(out[b].double().cpu().numpy() - ref) <= tol).all()
+
+
+def test_bad_prefix_length_is_clamped_and_reported():
+    cache, batch, table = random_cache(8, BF16, 2, 1, 64, [128, 64])
+    batch = das.Batch(torch.tensor([1000, -3], dtype=torch.int32, device=DEV), batch.block_table,
+                      batch.dev_error)
+    q, kb, vb = _block(3, BF16, 2, 2, 1, 1, 64)
+    lse = torch.empty((2, 1, 2), device=DEV)
+    out = das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb, lse=lse)
+    assert int(batch.dev_error) == das.DEVERR_PREFIX
+    _check(cache, batch, table, [128, 0], q, kb, vb, out, lse)
+
+
+def test_a_visible_nan_stays_in_its_sequence_and_head():
+    lens = [100, 100]
+    cache, batch, table = random_cache(8, BF16, 2, 2, 64, lens)
+    clean = das.attn_policy_q8(cache, batch, 0, 1, 1, *_block(3, BF16, 2, 3, 2, 2, 64))
+    cache.v_pool.view(torch.uint8)[0, 0, 1, int(table[0, 1]), 2, 5, 3] = 0x7f
+    out = das.attn_policy_q8(cache, batch, 0, 1, 1, *_block(3, BF16, 2, 3, 2, 2, 64))
+    assert torch.isnan(out[0, :, 1, 5]).all()
+    hit = torch.zeros_like(out, dtype=torch.bool)
+    hit[0, :, 1, 5] = True
+    assert torch.equal(out[~hit], clean[~hit])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_what_later_block_positions_hold_does_not_reach_earlier_rows(dtype):
+    """Infinities and NaN in block keys and values that a row does not see."""
+    lens = [70]
+    cache, batch, _ = random_cache(8, dtype, 1, 2, 64, lens)
+    q, kb, vb = _block(3, dtype, 1, 40, 4, 2, 64)
+    clean = das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb)
+    kb[:, 20:], vb[:, 20] = float("nan"), float("inf")
+    vb[:, 35] = float("nan")
+    out = das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb)
+    assert torch.equal(out[:, :20], clean[:, :20])
+    assert not torch.isfinite(out[:, 20:]).any()
+
+
+def test_repeats_streams_and_graphs_agree():
+    """Equal calls give equal bits: again, on two streams at once, captured, and in two
+    graphs that share a workspace and are replayed in turn."""
+    lens = [2000, 333]
+    cache, batch, table = random_cache(8, BF16, 2, 2, 96, lens)
+    blocks = [_block(s, BF16, 2, 5, 4, 2, 96) for s in (1, 2)]
+    want = [das.attn_policy_q8(cache, batch, 0, 1, 1, *x) for x in blocks]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in blocks]
+    got = []
+    for _ in range(3):
+        for x, s in zip(blocks, streams):
+            with torch.cuda.stream(s):
+                got.append(das.attn_policy_q8(cache, batch, 0, 1, 1, *x))
+    torch.cuda.synchronize()
+    for i, o in enumerate(got):
+        assert torch.equal(o, want[i % 2])
+    ws = das.alloc_workspace_q8(cache, batch, 4, 5)
+    outs, graphs = [torch.empty_like(w) for w in want], []
+    for x, o in zip(blocks, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            das.attn_policy_q8(cache, batch, 0, 1, 1, *x, out=o, workspace=ws)
+        graphs.append(g)
+    for rep in range(4):
+        for g, o, w in zip(graphs, outs, want):
+            o.fill_(7)
+            das.attn_policy_q8(cache, batch, 0, 1, 1, *blocks[1])  # eager work between
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(o, w), rep

@@ -1,0 +1,201 @@
+"""das_sample against its definition in 64 bits, on rows of every length and kind, and
+against its bounds: equal logits, infinities, NaN, one token, the largest vocabulary."""
+
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_34538_amd import _lib as das
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def reference(z, u, T=1.0, k=0, p=1.0, low=0.0):
+    """(token, probability) of one row, in 64 bits."""
+    z = np.where(np.isnan(z), -np.inf, z.astype(np.float64))
+    order = np.lexsort((np.arange(len(z)), -z))
+    best = z[order[0]]
+    if T == 0 or best == -np.inf:
+        return (int(order[0]) if best > -np.inf else 0), 1.0
+    with np.errstate(invalid="ignore"):
+        w = np.where(z == best, 1.0, np.exp((z - best) / T))
+    kept = order[:k] if 0 < k < len(z) else order
+    if p < 1:
+        c = np.cumsum(w[kept])
+        kept = kept[:int(np.searchsorted(c, p * c[-1])) + 1]
+    if low > 0:
+        kept = kept[w[kept] >= min(low, 1.0)]
+    ids = np.sort(kept)
+    c = np.cumsum(w[ids])
+    at = min(int(np.searchsorted(c, u * c[-1], side="right")), len(ids) - 1)
+    return int(ids[at]), w[ids[at]] / c[-1]
+
+
+def check(logits, u, T=None, k=None, p=None, low=None, error=0):
+    B, w, _ = logits.shape
+    up = lambda x, dt: None if x is None else torch.tensor(x, dtype=dt, device=DEV)  # noqa: E731
+    probs = torch.full((B, w), float("nan"), device=DEV)
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    tokens = das.sample(logits, u, up(T, F32), up(k, torch.int32), up(p, F32), up(low, F32),
+                        probs=probs, dev_error=err)
+    z, uu = logits.float().cpu().numpy(), u.double().cpu().numpy()
+    pick = lambda x, b, d: d if x is None else float(np.float32(x[b]))  # noqa: E731
+    for b in range(B):
+        for i in range(w):
+            t, pr = reference(z[b, i], uu[b, i], pick(T, b, 1.0), 0 if k is None else k[b],
+                              pick(p, b, 1.0), pick(low, b, 0.0))
+            assert int(tokens[b, i]) == t, (b, i)
+            # an fp32 step, and weights that are whole multiples of 2^-40
+            assert abs(float(probs[b, i]) - pr) <= 2.0 ** -24 * pr + 2.0 ** -38, (b, i)
+    assert int(err) == error
+    return tokens
+
+
+def _logits(seed, B, w, V, dtype, kind="normal"):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    z = torch.randn((B, w, V), generator=g, device=DEV) * (0.5 if kind == "flat" else 2.5)
+    if kind == "peaked":
+        z[..., : max(1, V // 50)] += 9
+        z = z[..., torch.randperm(V, generator=g, device=DEV)]
+    return z.to(dtype).contiguous(), torch.rand((B, w), generator=g, device=DEV)
+
+
+FILTERS = dict(T=[1.0, 0.7, 1.5, 0.0, 0.9, 1.0], k=[0, 20, 3, 5, 0, 1], p=[1.0, 1.0, 0.9, 0.5, 0.95, 0.3],
+               low=[0.0, 0.05, 0.0, 0.1, 0.02, 0.0])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("V", [1, 2, 7, 8, 511, 512, 513, 1000, 4097, 8192, 32001, 65536, 100003, 262147])
+def test_vocabularies(dtype, V):
+    check(*_logits(V, 6, 2, V, dtype, "peaked"), **FILTERS)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_largest_vocabulary(dtype):
+    check(*_logits(1, 3, 1, das.MAX_VOCAB, dtype), T=[1.0, 0.8, 2.0], k=[0, 100, 0], p=[1.0, 0.9, 0.6])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", ["flat", "normal", "peaked"])
+@pytest.mark.parametrize("name,filt", [
+    ("none", {}), ("cold", dict(T=[0.05] * 4)), ("hot", dict(T=[30.0] * 4)),
+    ("top_k", dict(k=[1, 2, 3000, 19999])), ("all", dict(k=[20000, 30000, -1, 0])),
+    ("top_p", dict(p=[0.0, 1e-6, 0.5, 0.999])), ("min_p", dict(low=[1e-9, 0.3, 1.0, 5.0])),
+    ("both", dict(T=[0.6] * 4, k=[50, 5000, 400, 7], p=[0.99, 0.5, 0.9, 0.01], low=[0.01, 0.0, 0.2, 0.9])),
+])
+def test_filters(dtype, kind, name, filt):
+    check(*_logits(5, 4, 3, 20000, dtype, kind), **filt)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("V", [100, 5000, 70001])
+def test_equal_logits(dtype, V):
+    """Every token equal, or two values only: cuts go through ties, lowest index first."""
+    z, u = _logits(2, 6, 2, V, dtype)
+    z[:3] = 0.25
+    z[3:] = torch.where(z[3:] > 1.0, 1.0, -1.0).to(dtype)
+    f = dict(T=[1.0, 0.5, 1.0, 1.0, 0.7, 1.3], k=[0, 17, 0, V // 2, 5, 0], p=[0.5, 1.0, 0.9, 0.8, 1.0, 0.3])
+    check(z, u, **f)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_outliers(dtype):
+    """A single huge logit squeezes the rest into one bin; the cut lies among them."""
+    z, u = _logits(4, 4, 1, 30000, dtype)
+    z[:, :, 123] = 3000.0
+    check(z, u, k=[50, 5000, 29999, 0], p=[1.0, 0.9, 1.0, 0.9], T=[1.0, 1.0, 2000.0, 900.0])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_infinities_and_nan(dtype):
+    z, u = _logits(3, 6, 1, 3001, dtype)
+    z[0, 0, ::2] = float("nan")
+    z[1] = float("-inf")
+    z[2] = float("nan")
+    z[3, 0, [5, 700, 2999]] = float("inf")
+    z[4, 0, 1:] = float("-inf")
+    z[5, 0, 10:] = torch.finfo(dtype).min
+    f = dict(T=[1.0] * 6, k=[10, 0, 4, 2, 7, 20], p=[0.9, 0.9, 1.0, 1.0, 0.5, 0.99], low=[0.1] * 6)
+    check(z, u, **f)
+    check(z, u)
+    check(z, u, T=[0.0] * 6)
+
+
+def test_greedy_takes_the_lowest_of_equal_largest():
+    z = torch.zeros((2, 3, 9000), device=DEV)
+    z[0, 1, [8999, 4000, 70]] = 2.0
+    z[1, 2, [513, 512]] = 1.0
+    z[1, 0, 100] = -0.0
+    t = check(z, torch.rand((2, 3), device=DEV), T=[0.0, 0.0])
+    assert t.tolist() == [[0, 70, 0], [0, 0, 512]]
+
+
+def test_random_numbers_at_the_ends():
+    z, _ = _logits(3, 2, 4, 700, F32)
+    last = float(np.nextafter(np.float32(1), np.float32(0)))
+    u = torch.tensor([[0.0, last, 2.0 ** -30, 0.5]] * 2, device=DEV)
+    check(z, u, T=[1.0, 3.0], p=[1.0, 0.7])
+
+
+def test_parameters_out_of_range_are_reported_and_taken_greedily():
+    z, u = _logits(3, 7, 1, 700, F32)
+    nan, inf = float("nan"), float("inf")
+    u[6] = 1.0
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    up = lambda x: torch.tensor(x, device=DEV)  # noqa: E731
+    probs = torch.zeros((7, 1), device=DEV)
+    t = das.sample(z, u, up([-1.0, nan, inf, 1.0, 1.0, 1.0, 1.0]), None, up([1.0] * 3 + [nan, 1.0, 1.0, 1.0]),
+                   up([0.0] * 4 + [nan, 0.0, 0.0]), probs=probs, dev_error=err)
+    assert int(err) == das.DEVERR_SAMPLE
+    greedy = z.argmax(-1)
+    for b in range(7):
+        want = int(greedy[b]) if b != 5 else reference(z[5, 0].cpu().numpy(), float(u[5]))[0]
+        assert int(t[b]) == want
+        if b != 5:
+            assert float(probs[b]) == 1.0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_apart_and_unaligned(dtype):
+    """Rows of a wider buffer, from an odd element on: any distance, any alignment."""
+    big = torch.full((3, 4, 1003), 50.0, device=DEV).to(dtype)
+    z, u = _logits(3, 3, 4, 1000, dtype)
+    big[..., 1:1001] = z
+    view = big[..., 1:1001]
+    f = dict(T=[1.0, 0.7, 1.0], k=[0, 20, 0], p=[1.0, 1.0, 0.9])
+    assert torch.equal(check(view, u, **f), check(z, u, **f))
+
+
+def test_the_share_of_random_numbers_is_the_probability():
+    """Random numbers on an even grid: a token's count is its probability's share of it,
+    to one grid step on each side."""
+    n = 64 * 200
+    z = torch.randn((1, 1, 300), device=DEV).expand(200, 64, 300).contiguous()
+    u = (torch.arange(n, device=DEV).float() / n).view(200, 64)
+    t = das.sample(z, u, torch.full((200,), 0.8, device=DEV)).view(-1).cpu().numpy()
+    p = np.exp((z[0, 0].double().cpu().numpy()) / np.float64(np.float32(0.8)))
+    p /= p.sum()
+    assert (np.diff(t) >= 0).all()  # index order
+    assert (np.abs(np.bincount(t, minlength=300) - p * n) <= 1.001).all()
+
+
+def test_repeats_and_graphs_agree():
+    z, u = _logits(3, 4, 2, 30000, BF16)
+    par = [torch.tensor(x, device=DEV) for x in ([1.0, 0.7, 0.0, 1.2], [0, 50, 0, 0], [0.9, 0.95, 1.0, 1.0])]
+    par[1] = par[1].int()
+    want = das.sample(z, u, *par).clone()
+    tokens = torch.empty_like(want)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        das.sample(z, u, *par, tokens=tokens)
+    for _ in range(4):
+        tokens.fill_(-1)
+        assert torch.equal(das.sample(z, u, *par), want)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(tokens, want)
