@@ -23,10 +23,9 @@
 namespace das {
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWavesS = kThreads / 64;
-constexpr int kBlock = 512;                     // tokens of a wave's step
-constexpr int kMaxBlocks = DAS_MAX_VOCAB / kBlock;
+constexpr int kMaxThreads = 1024;
+constexpr int kStep = 512;                      // tokens of a wave's step
+constexpr int kMaxBlocks = 256;                 // blocks of a row, kStep << row_shift tokens each
 constexpr int kBins = 2048;
 constexpr int kList = 2048;                     // tokens that are compared with each other
 constexpr float kNegInf = -__builtin_huge_valf();
@@ -42,20 +41,47 @@ __device__ __forceinline__ float of_key(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-// 8 logits from index i of a row of n (-inf past its end).
+// 8 logits of a row as they lie in memory.
 template <typename T>
-__device__ __forceinline__ void load8(const T *row, int i, int n, float (&z)[8]) {
-  T raw[8];
+struct Raw8 {
+  uint32_t w[8 * sizeof(T) / 4];
+};
+// ... from index i of a row of n, -inf past its end.
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const T *row, int i, int n) {
+  Raw8<T> r;
   if (i + 8 <= n) {
-    __builtin_memcpy(raw, row + i, sizeof(raw));
-#pragma unroll
-    for (int j = 0; j < 8; ++j) z[j] = to_f32<T>(raw[j]);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) z[j] = i + j < n ? to_f32<T>(row[i + j]) : kNegInf;
+    __builtin_memcpy(&r, row + i, sizeof(r));
+    return r;
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) z[j] = z[j] == z[j] ? z[j] + 0.f : kNegInf;
+  for (int k = 0; k < static_cast<int>(sizeof(r) / 4); ++k) r.w[k] = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+#pragma unroll 1
+  for (int j = 0; j < 8 && i < n; ++j) {  // in at the top, one after the other
+    constexpr int N = sizeof(r) / 4;
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t v = i + j < n ? row[i + j] : 0xff80u;
+#pragma unroll
+      for (int k = 0; k < N - 1; ++k) r.w[k] = r.w[k] >> 16 | r.w[k + 1] << 16;
+      r.w[N - 1] = r.w[N - 1] >> 16 | v << 16;
+    } else {
+      const uint32_t v = i + j < n ? __float_as_uint(row[i + j]) : 0xff800000u;
+#pragma unroll
+      for (int k = 0; k < N - 1; ++k) r.w[k] = r.w[k + 1];
+      r.w[N - 1] = v;
+    }
+  }
+  return r;
+}
+// Logit j of the eight, NaN as -inf and -0 as 0.
+template <typename T>
+__device__ __forceinline__ float logit(const Raw8<T> &r, int j) {
+  float z;
+  if constexpr (sizeof(T) == 2)
+    z = __uint_as_float(j % 2 ? r.w[j / 2] & 0xffff0000u : r.w[j / 2] << 16);
+  else
+    z = __uint_as_float(r.w[j]);
+  return z == z ? z + 0.f : kNegInf;
 }
 
 // 2^x for x <= 0 as round(2^40 2^x): 2^x = 2^n 2^f with |f| <= 1/2 and the series of
@@ -79,6 +105,15 @@ __device__ __forceinline__ uint64_t weight_of(double x) {
   return __builtin_bit_cast(uint64_t, w + 0x1p52) & 0xfffffffffffffull;
 }
 
+// The next of the eight to place 0.
+template <typename T>
+__device__ __forceinline__ void pop(Raw8<T> &r) {
+  constexpr int N = sizeof(r.w) / 4;
+#pragma unroll
+  for (int k = 0; k < N - 1; ++k) r.w[k] = sizeof(T) == 2 ? r.w[k] >> 16 | r.w[k + 1] << 16 : r.w[k + 1];
+  if (sizeof(T) == 2) r.w[N - 1] >>= 16;
+}
+
 struct Row {
   float best;      // largest logit
   double c;        // log2(e) / T
@@ -92,6 +127,18 @@ struct Row {
   }
 };
 
+// The bins of a bf16 row, one for each value of 2^-9 <= |z| < 2^7, larger logits in
+// lower bins: 0 for larger ones, kCentre for those around 0, kBottom for the rest.
+constexpr int kSmall = 0x3b00, kLarge = 0x4300;  // bits of 2^-9 and 2^7
+constexpr float kLowest = -128.f;
+constexpr int kCentre = kLarge - kSmall + 1, kBottom = 2 * kCentre;
+constexpr int kValues = kBottom + 1;
+constexpr int kAround = 512;                     // tokens around 0 that a row may have
+
+struct Blocks {
+  unsigned long long above[kMaxBlocks];  // kept weights above the cut, per block
+  uint32_t ties[kMaxBlocks];             // tokens at the cut
+};
 struct Shared {
   union {
     struct {
@@ -103,59 +150,140 @@ struct Shared {
       uint64_t list_weight[kList];
     } cut;
     struct {
-      uint64_t above[kMaxBlocks];  // kept weights above the cut key, per block
-      uint32_t ties[kMaxBlocks];   // tokens at the cut key
-    } last;
+      uint64_t weight[kValues];  // of a kept token of each bin
+      union {
+        uint32_t count[kValues];
+        Blocks last;
+      };
+      int32_t centre[kAround];   // the tokens around 0, and their bits
+      uint16_t centre_bits[kAround];
+    } value;
+    Blocks last;
   };
-  uint64_t part[kWavesS];
-  uint32_t part32[kWavesS];
+  uint64_t part[kMaxThreads / 64];
+  uint32_t part32[kMaxThreads / 64];
   uint64_t answer64;
   uint32_t answer32, answer_ties, n_list;
   int at;
 };
 
-__device__ __forceinline__ uint64_t shfl_up64(uint64_t x, int d) {
-  return static_cast<uint64_t>(__shfl_up(static_cast<unsigned long long>(x), d, 64));
+__device__ __forceinline__ uint64_t join(uint32_t lo, uint32_t hi) {
+  return static_cast<uint64_t>(hi) << 32 | lo;
 }
-__device__ __forceinline__ uint64_t wave_scan(uint64_t x, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t y = shfl_up64(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
+// x plus what CTRL brings from another lane, 0 where it brings nothing (and in the rows
+// of 16 lanes outside ROWS).
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint64_t plus_dpp(uint64_t x) {
+  const uint32_t lo = static_cast<uint32_t>(x), hi = static_cast<uint32_t>(x >> 32);
+  return x + join(__builtin_amdgcn_update_dpp(0, lo, CTRL, ROWS, 0xf, false),
+                  __builtin_amdgcn_update_dpp(0, hi, CTRL, ROWS, 0xf, false));
 }
+// Inclusive prefix sum over the wave: within rows of 16 lanes (shifts), then the row's
+// last lane into the next row, and lane 31 into the upper half.
+__device__ __forceinline__ uint64_t wave_scan(uint64_t x) {
+  x = plus_dpp<0x111>(x);
+  x = plus_dpp<0x112>(x);
+  x = plus_dpp<0x114>(x);
+  x = plus_dpp<0x118>(x);
+  x = plus_dpp<0x142, 0xa>(x);
+  return plus_dpp<0x143, 0xc>(x);
+}
+// Sum over the wave, in every lane: lanes 1 and 2 apart, mirrored in 8 and 16, then the
+// swaps of 16 and 32 lanes.
 __device__ __forceinline__ uint64_t wave_sum(uint64_t x) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1)
-    x += static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(x), d, 64));
-  return x;
+  x = plus_dpp<0xB1>(x);
+  x = plus_dpp<0x4E>(x);
+  x = plus_dpp<0x141>(x);
+  x = plus_dpp<0x140>(x);
+  uint32_t lo = static_cast<uint32_t>(x), hi = static_cast<uint32_t>(x >> 32);
+  auto a = __builtin_amdgcn_permlane16_swap(lo, lo, false, false);
+  auto b = __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+  x = join(a[0], b[0]) + join(a[1], b[1]);
+  lo = static_cast<uint32_t>(x), hi = static_cast<uint32_t>(x >> 32);
+  a = __builtin_amdgcn_permlane32_swap(lo, lo, false, false);
+  b = __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+  return join(a[0], b[0]) + join(a[1], b[1]);
 }
 // Exclusive prefix sum over the workgroup; *total is the sum.
+template <int THREADS>
 __device__ __forceinline__ uint64_t block_scan(uint64_t x, Shared &sh, uint64_t *total) {
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const uint64_t incl = wave_scan(x, lane);
+  const uint64_t incl = wave_scan(x);
   __syncthreads();  // the previous call's parts have been read
   if (lane == 63) sh.part[wave] = incl;
   __syncthreads();
-  uint64_t before = 0, all = 0;
-#pragma unroll
-  for (int k = 0; k < kWavesS; ++k) {
-    const uint64_t v = sh.part[k];
-    if (k < wave) before += v;
-    all += v;
-  }
-  *total = all;
-  return before + incl - x;
+  // the waves' sums, scanned in a row of 16 lanes
+  uint64_t v = lane < THREADS / 64 ? sh.part[lane] : 0;
+  v = plus_dpp<0x111>(v);
+  v = plus_dpp<0x112>(v);
+  v = plus_dpp<0x114>(v);
+  v = plus_dpp<0x118>(v);
+  auto at = [&](int l) {
+    return join(__builtin_amdgcn_readlane(static_cast<uint32_t>(v), l),
+                __builtin_amdgcn_readlane(static_cast<uint32_t>(v >> 32), l));
+  };
+  *total = at(THREADS / 64 - 1);
+  const int w = __builtin_amdgcn_readfirstlane(wave);
+  return (w > 0 ? at(w - 1) : 0) + incl - x;
 }
 
-// fn(first index, 8 logits) over the whole row, a wave on 512 neighbouring tokens.
-template <typename T, typename Fn>
+// fn(first index, 8 logits) over the whole row, a wave on 512 neighbouring tokens, the
+// last of which may be past the end (-inf: no weight, and after every token in the order).
+// The loads of a thread's next 16 or 8 tokens (bf16, fp32) are under way while it works
+// on the ones before.
+template <int THREADS, typename T, typename Fn>
 __device__ __forceinline__ void for_row(const T *row, int n, Fn &&fn) {
-  for (int i = threadIdx.x * 8; i < (n + kBlock - 1) / kBlock * kBlock; i += kThreads * 8) {
-    float z[8];
-    load8<T>(row, i, n, z);
-    fn(i, z);
+  constexpr int GROUP = 4 / sizeof(T), STEP = THREADS * 8;
+  const int lane8 = threadIdx.x % 64 * 8;
+  Raw8<T> r[GROUP], next[GROUP];
+  auto load = [&](int i0, Raw8<T> (&to)[GROUP]) {
+#pragma unroll
+    for (int c = 0; c < GROUP; ++c)
+      if (i0 + c * STEP < n) to[c] = load8<T>(row, i0 + lane8 + c * STEP, n);
+  };
+  int i0 = threadIdx.x / 64 * kStep;  // uniform in the wave
+  load(i0, r);
+  for (; i0 < n; i0 += GROUP * STEP) {
+    load(i0 + GROUP * STEP, next);
+#pragma unroll
+    for (int c = 0; c < GROUP; ++c)
+      if (i0 + c * STEP < n) fn(i0 + lane8 + c * STEP, r[c]);
+#pragma unroll
+    for (int c = 0; c < GROUP; ++c) r[c] = next[c];
+  }
+}
+
+// fn(index, logit) one token a lane at a time, for work that is long against a load (an
+// exponential each); tokens past the end come as -inf. Two loads are ahead.
+template <typename T, typename Fn>
+__device__ __forceinline__ void for_each(const T *row, int n, int begin, int tokens, Fn &&fn) {
+  const int i0 = begin + threadIdx.x % 64;
+  auto load = [&](int i) {
+    const float z = i < n ? to_f32<T>(row[i]) : kNegInf;
+    return z == z ? z + 0.f : kNegInf;
+  };
+  float z0 = load(i0), z1 = load(i0 + 64);
+#pragma unroll 1
+  for (int i = i0; i < i0 + tokens; i += 64) {
+    const float z2 = i + 128 < i0 + tokens ? load(i + 128) : 0.f;
+    fn(i, z0);
+    z0 = z1;
+    z1 = z2;
+  }
+}
+
+// fn(index, logit) for every token: eight at a time, or in fp32's place the compact loop
+// for bf16 rows, which come here only when sample_values does not take them.
+template <int THREADS, typename T, typename Fn>
+__device__ __forceinline__ void for_tokens(const T *row, int n, Fn &&fn) {
+  if constexpr (sizeof(T) == 2) {
+    for (int i = threadIdx.x / 64 * kStep; i < n; i += THREADS / 64 * kStep)
+      for_each<T>(row, n, i, kStep, fn);
+  } else {
+    for_row<THREADS, T>(row, n, [&](int i, const Raw8<T> &z8) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) fn(i + j, logit<T>(z8, j));
+    });
   }
 }
 
@@ -163,7 +291,7 @@ __device__ __forceinline__ void for_row(const T *row, int n, Fn &&fn) {
 // with key >= row.key (at row.key itself only row.ties of them), the largest key t such
 // that the f of the keys >= t reach `target` (0 < target <= their sum; WEIGH: share of
 // the sum), and how many tokens at t that takes. Moves row.key and row.ties there.
-template <bool WEIGH, typename T>
+template <int THREADS, bool WEIGH, typename T>
 __device__ void find_cut(const T *row, int n, Row &r, uint32_t count, float share, Shared &sh) {
   const int tid = threadIdx.x, lane = tid % 64;
   // bins of equal width below the maximum; weights further down than the last are 0
@@ -172,39 +300,38 @@ __device__ void find_cut(const T *row, int n, Row &r, uint32_t count, float shar
     const float d = (r.best - z) * width;  // NaN where both are infinite: bin 0
     return d < kBins - 1 ? static_cast<int>(d) : d >= kBins - 1 ? kBins - 1 : 0;
   };
-  for (int i = tid; i < kBins; i += kThreads) {
+  for (int i = tid; i < kBins; i += THREADS) {
     if (WEIGH) sh.cut.bin.weight[i] = 0;
     else sh.cut.bin.count[i] = 0;
   }
   if (tid == 0) sh.n_list = 0;
   __syncthreads();
-  for_row<T>(row, n, [&](int i, const float (&z)[8]) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (i + j >= n || key_of(z[j]) < r.key) continue;
-      if (WEIGH) {
-        if (key_of(z[j]) == r.key) continue;  // added below, as many as count
-        const uint64_t w = r.weight(z[j]);
-        if (w) atomicAdd(reinterpret_cast<unsigned long long *>(&sh.cut.bin.weight[bin_of(z[j])]),
-                         static_cast<unsigned long long>(w));
-      } else {
-        atomicAdd(&sh.cut.bin.count[bin_of(z[j])], 1u);
-      }
-    }
-  });
+  const int wave = tid / 64;
+  if constexpr (WEIGH) {
+    for_tokens<THREADS, T>(row, n, [&](int, float z) {
+      if (key_of(z) <= r.key) return;  // those equal are added below, as many as count
+      const uint64_t w = r.weight(z);
+      if (w) atomicAdd(reinterpret_cast<unsigned long long *>(&sh.cut.bin.weight[bin_of(z)]),
+                       static_cast<unsigned long long>(w));
+    });
+  } else {
+    for_tokens<THREADS, T>(row, n, [&](int, float z) {
+      if (key_of(z) >= r.key) atomicAdd(&sh.cut.bin.count[bin_of(z)], 1u);
+    });
+  }
   __syncthreads();
   const uint64_t tie_weight = WEIGH && r.ties ? r.weight(of_key(r.key)) : 0;
   if (WEIGH && tid == 0 && r.ties) sh.cut.bin.weight[bin_of(of_key(r.key))] += tie_weight * r.ties;
   __syncthreads();
   // the bin that reaches the target
-  uint64_t a[kBins / kThreads], mine = 0, total;
+  uint64_t a[kBins / THREADS], mine = 0, total;
 #pragma unroll
-  for (int k = 0; k < kBins / kThreads; ++k) {
-    const int i = tid * (kBins / kThreads) + k;
+  for (int k = 0; k < kBins / THREADS; ++k) {
+    const int i = tid * (kBins / THREADS) + k;
     a[k] = WEIGH ? sh.cut.bin.weight[i] : sh.cut.bin.count[i];
     mine += a[k];
   }
-  uint64_t before = block_scan(mine, sh, &total);
+  uint64_t before = block_scan<THREADS>(mine, sh, &total);
   uint64_t target = count;
   if (WEIGH) {
     const double q = __builtin_ceil(static_cast<double>(share) * static_cast<double>(total));
@@ -212,9 +339,9 @@ __device__ void find_cut(const T *row, int n, Row &r, uint32_t count, float shar
   }
   if (target > total) target = total;
 #pragma unroll
-  for (int k = 0; k < kBins / kThreads; ++k) {
+  for (int k = 0; k < kBins / THREADS; ++k) {
     if (before < target && before + a[k] >= target) {
-      sh.at = tid * (kBins / kThreads) + k;
+      sh.at = tid * (kBins / THREADS) + k;
       sh.answer64 = target - before;
     }
     before += a[k];
@@ -223,23 +350,17 @@ __device__ void find_cut(const T *row, int n, Row &r, uint32_t count, float shar
   const int bin = sh.at;
   uint64_t rest = sh.answer64;  // to be reached within the bin, >= 1
   // its tokens
-  for_row<T>(row, n, [&](int i, const float (&z)[8]) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t key = key_of(z[j]);
-      if (i + j >= n || key < r.key || bin_of(z[j]) != bin) continue;
-      if (WEIGH && key == r.key) continue;
-      const uint32_t at = atomicAdd(&sh.n_list, 1u);
-      if (at < kList) {
-        sh.cut.list_key[at] = key;
-        sh.cut.list_weight[at] = WEIGH ? r.weight(z[j]) : 1;
-      }
-    }
+  for_tokens<THREADS, T>(row, n, [&](int, float z) {
+    const uint32_t key = key_of(z);
+    if (key < r.key || bin_of(z) != bin || (WEIGH && key == r.key)) return;
+    const uint32_t at = atomicAdd(&sh.n_list, 1u);
+    if (at < kList) sh.cut.list_key[at] = key;
   });
   __syncthreads();
   const uint32_t listed = sh.n_list;
-  __syncthreads();
   if (listed <= kList) {
+    for (uint32_t i = tid; i < listed; i += THREADS)
+      sh.cut.list_weight[i] = WEIGH ? r.weight(of_key(sh.cut.list_key[i])) : 1;
     if (tid == 0) {
       // reached by none of the list: by the ties of the cut that was there
       sh.answer32 = r.key;
@@ -248,7 +369,7 @@ __device__ void find_cut(const T *row, int n, Row &r, uint32_t count, float shar
     }
     __syncthreads();
     uint64_t all = 0;
-    for (uint32_t i = tid; i < listed; i += kThreads) {
+    for (uint32_t i = tid; i < listed; i += THREADS) {
       const uint32_t key = sh.cut.list_key[i];
       uint64_t above = 0, equal = 0;
       all = 0;
@@ -281,30 +402,29 @@ __device__ void find_cut(const T *row, int n, Row &r, uint32_t count, float shar
   uint32_t prefix = 0;
 #pragma unroll 1
   for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += kThreads) sh.cut.bin.weight[i] = 0;
+    for (int i = tid; i < 256; i += THREADS) sh.cut.bin.weight[i] = 0;
     __syncthreads();
-    for_row<T>(row, n, [&](int i, const float (&z)[8]) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t key = key_of(z[j]);
-        bool in = i + j < n && key >= r.key && bin_of(z[j]) == bin;
+    for (int i0 = wave * kStep; i0 < n; i0 += THREADS / 64 * kStep) {
+      for_each<T>(row, n, i0, kStep, [&](int, float z) {
+        const uint32_t key = key_of(z);
+        bool in = key >= r.key && bin_of(z) == bin;
         if (WEIGH) in = in && key != r.key;
         if (shift < 24) in = in && (key >> (shift + 8)) == prefix;
         const uint32_t digit = key >> shift & 255;
         const uint64_t voters = __builtin_amdgcn_ballot_w64(in);
-        if (!voters) continue;
+        if (!voters) return;
         // equal logits are what leads here: one addition for lanes with the same key
         const uint32_t lead = __builtin_amdgcn_readlane(key, __builtin_ctzll(voters));
         const uint64_t same = __builtin_amdgcn_ballot_w64(in && key == lead);
         if (in) {
-          const uint64_t w = WEIGH ? r.weight(z[j]) : 1;
+          const uint64_t w = WEIGH ? r.weight(z) : 1;
           const bool first = lane == __builtin_ctzll(same);
           if (key != lead || first)
             atomicAdd(reinterpret_cast<unsigned long long *>(&sh.cut.bin.weight[digit]),
                       static_cast<unsigned long long>(key != lead ? w : w * __builtin_popcountll(same)));
         }
-      }
-    });
+      });
+    }
     __syncthreads();
     if (WEIGH && tid == 0 && r.ties && bin_of(of_key(r.key)) == bin &&
         (shift == 24 || (r.key >> (shift + 8)) == prefix))
@@ -312,7 +432,7 @@ __device__ void find_cut(const T *row, int n, Row &r, uint32_t count, float shar
     __syncthreads();
     const uint64_t w = tid < 256 ? sh.cut.bin.weight[255 - tid] : 0;  // from the top
     uint64_t all;
-    const uint64_t over = block_scan(w, sh, &all);
+    const uint64_t over = block_scan<THREADS>(w, sh, &all);
     if (over < rest && over + w >= rest) {
       sh.at = 255 - tid;
       sh.answer64 = rest - over;
@@ -327,8 +447,312 @@ __device__ void find_cut(const T *row, int n, Row &r, uint32_t count, float shar
   r.ties = static_cast<uint32_t>((rest + w - 1) / w);
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p) {
+// Tokens of a block: the fewest doublings of a step that leave kMaxBlocks of them.
+__device__ __forceinline__ int row_shift(int n) {
+  int s = 9;
+  static_assert(kStep == 1 << 9 && (DAS_MAX_VOCAB >> 9) / kMaxBlocks <= 32, "few doublings");
+  while ((n - 1) >> s >= kMaxBlocks) ++s;
+  return s;
+}
+template <int THREADS>
+__device__ __forceinline__ void clear(Blocks &blk) {
+  for (int i = threadIdx.x; i < kMaxBlocks; i += THREADS) blk.above[i] = 0, blk.ties[i] = 0;
+  __syncthreads();
+}
+// A wave's step of block b: its weights and ties.
+__device__ __forceinline__ void add_step(Blocks &blk, int b, uint64_t sum, uint32_t ties) {
+  const bool lead = threadIdx.x % 64 == 0;
+  if (__builtin_amdgcn_ballot_w64(sum != 0)) {
+    sum = wave_sum(sum);
+    if (lead) atomicAdd(&blk.above[b], static_cast<unsigned long long>(sum));
+  }
+  if (__builtin_amdgcn_ballot_w64(ties != 0)) {
+    ties = static_cast<uint32_t>(wave_sum(ties));
+    if (lead) atomicAdd(&blk.ties[b], ties);
+  }
+}
+
+// The drawn token from the sums of the blocks: `above(z)` is the weight of a token that is
+// kept whatever its index (else 0), the tokens with `tie(z)` weigh tie_weight each, the
+// first `limit` of them are kept. The block that passes the target is gone through once
+// more by one wave.
+template <int THREADS, typename T, typename Above, typename Tie>
+__device__ __forceinline__ void pick(const SampleParams &p, const T *row, int row_id, float u, bool greedy,
+                                     uint64_t tie_weight, uint32_t limit, const Blocks &blk, Shared &sh,
+                                     Above &&above, Tie &&tie) {
+  const int tid = threadIdx.x, lane = tid % 64, n = p.vocab, shift = row_shift(n);
+  static_assert(kMaxBlocks <= THREADS, "a block a thread");
+  __syncthreads();
+  const uint64_t ab = tid < kMaxBlocks ? blk.above[tid] : 0, ti = tid < kMaxBlocks ? blk.ties[tid] : 0;
+  uint64_t all_above, all_ties = 0, ti_before = 0;
+  const uint64_t ab_before = block_scan<THREADS>(ab, sh, &all_above);
+  if (limit) ti_before = block_scan<THREADS>(ti, sh, &all_ties);
+  const uint64_t most = limit;
+  const uint64_t total = all_above + min(all_ties, most) * tie_weight;
+  uint64_t target = static_cast<uint64_t>(static_cast<double>(u) * static_cast<double>(total));
+  if (target >= total) target = total - 1;
+  const uint64_t lo = ab_before + min(ti_before, most) * tie_weight;
+  const uint64_t hi = ab_before + ab + min(ti_before + ti, most) * tie_weight;
+  if (lo <= target && target < hi) {
+    sh.at = tid;
+    sh.answer64 = lo;
+    sh.answer32 = static_cast<uint32_t>(ti_before);
+  }
+  __syncthreads();
+  if (tid >= 64) return;
+  uint64_t run = sh.answer64;
+  uint32_t rank = sh.answer32;
+  // 8 tokens a lane: their sums, and in the step that passes the target each of them
+#pragma unroll 1
+  for (int i0 = sh.at << shift; i0 < n; i0 += kStep) {
+    const int i = i0 + 8 * lane;
+    const Raw8<T> z8 = load8<T>(row, i, n);
+    uint64_t sum = 0;
+    uint32_t ties = 0;
+    Raw8<T> z = z8;
+#pragma unroll 1
+    for (int j = 0; j < 8; ++j, pop(z)) {
+      const float x = logit<T>(z, 0);
+      if (limit && tie(x)) ++ties;
+      else if (i + j < n) sum += above(x);
+    }
+    const uint32_t ties_before = rank + static_cast<uint32_t>(wave_scan(ties)) - ties;
+    const uint32_t ties_kept = min(ties_before + ties, limit) - min(ties_before, limit);
+    sum += ties_kept * tie_weight;
+    uint64_t w_run = run + wave_scan(sum) - sum;
+    const uint64_t end = run + wave_sum(sum);
+    if (target < end) {
+      uint32_t own = ties_before;
+      z = z8;
+#pragma unroll 1
+      for (int j = 0; j < 8; ++j, pop(z)) {
+        const float x = logit<T>(z, 0);
+        uint64_t w = 0;
+        if (limit && tie(x)) w = own++ < limit ? tie_weight : 0;
+        else if (i + j < n) w = above(x);
+        if (w_run <= target && target < w_run + w) {
+          p.tokens[row_id] = i + j;
+          if (p.probs)
+            p.probs[row_id] = greedy ? 1.f : static_cast<float>(static_cast<double>(w) / static_cast<double>(total));
+        }
+        w_run += w;
+      }
+      return;
+    }
+    run = end;
+    rank += static_cast<uint32_t>(wave_sum(ties));
+  }
+}
+
+// The bin of a bf16 logit; a positive NaN counts as a large logit, a negative one as a
+// small one (rows with large logits are left to the other way).
+__device__ __forceinline__ int value_bin(uint32_t h) {
+  const int t = min(max(static_cast<int>(h & 0x7fffu), kSmall - 1), kLarge) - (kSmall - 1);
+  return h & 0x8000u ? kCentre + t : kCentre - t;
+}
+// The same for two logits in a word, and |z| - 2^-9 in steps, 0 for the tokens around 0.
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ i16x2 value_bins(uint32_t w, i16x2 &steps) {
+  const i16x2 z = __builtin_bit_cast(i16x2, w);
+  i16x2 flip = ~z >> 15;                 // -1 for positive ones
+  asm("" : "+v"(flip));                  // packed arithmetic, no selections by sign
+  i16x2 a = z & static_cast<int16_t>(0x7fff);
+  const i16x2 low = {kSmall - 1, kSmall - 1}, high = {kLarge, kLarge};
+  a = __builtin_elementwise_min(__builtin_elementwise_max(a, low), high) - low;
+  steps = a;
+  return (a ^ flip) + (static_cast<int16_t>(kCentre) - flip);  // centre -+ a
+}
+// Two bf16 as signed integers in their order.
+__device__ __forceinline__ i16x2 ordered(uint32_t w) {
+  const i16x2 z = __builtin_bit_cast(i16x2, w);
+  return z ^ ((z >> 15) & static_cast<int16_t>(0x7fff));
+}
+__device__ __forceinline__ float bin_value(int bin) {
+  const uint32_t h = kSmall - 1 + (bin < kCentre ? kCentre - bin : (bin - kCentre) | 0x8000);
+  return __uint_as_float(h << 16);
+}
+
+// A bf16 row by the counts of its values: there are few thousand of them in the range
+// that logits have, so one pass of counting holds the order, every cut and, with one
+// exponential per value, every sum; the last pass looks its weights up. Returns false
+// (having done nothing) for rows out of that range: a largest logit of 2^7 or more, or
+// within 2^-9 of 0, weights that matter below -2^7, many tokens within 2^-9 of 0, or a
+// cut there.
+template <int THREADS>
+__device__ bool sample_values(const SampleParams &p, const bf16_t *row, int row_id, float temperature, int k,
+                              float top_p, float min_p, float u, bool greedy, Shared &sh) {
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, n = p.vocab;
+  constexpr int PER = (kValues + THREADS - 1) / THREADS;
+  for (int i = tid; i < kValues; i += THREADS) sh.value.count[i] = 0;
+  if (tid == 0) sh.n_list = 0;
+  __syncthreads();
+  for_row<THREADS, bf16_t>(row, n, [&](int i, const Raw8<bf16_t> &z8) {
+    i16x2 steps[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const i16x2 bins = value_bins(z8.w[k], steps[k]);
+      atomicAdd(&sh.value.count[bins[0]], 1u);
+      atomicAdd(&sh.value.count[bins[1]], 1u);
+    }
+    const i16x2 least = __builtin_elementwise_min(__builtin_elementwise_min(steps[0], steps[1]),
+                                                  __builtin_elementwise_min(steps[2], steps[3]));
+    if (least[0] == 0 || least[1] == 0) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (steps[j / 2][j % 2] != 0) continue;
+        const uint32_t at = atomicAdd(&sh.n_list, 1u);
+        if (at < kAround) {
+          sh.value.centre[at] = i + j;
+          sh.value.centre_bits[at] = static_cast<uint16_t>(z8.w[j / 2] >> (16 * (j % 2)));
+        }
+      }
+    }
+  });
+  __syncthreads();
+  // a thread's bins, from the largest logits down
+  const int bin0 = tid * PER, bin1 = min(bin0 + PER, kValues);
+  int first = kBottom;
+  for (int i = bin1 - 1; i >= bin0; --i)
+    if (sh.value.count[i]) first = i;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) first = min(first, __shfl_xor(first, d, 64));
+  if (lane == 0) sh.part32[wave] = first;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < (THREADS / 64); ++i) first = min(first, static_cast<int>(sh.part32[i]));
+  const uint32_t centre = sh.n_list;
+  if (first == 0 || first == kCentre || first == kBottom || centre > kAround) return false;
+  Row r;
+  r.best = bin_value(first);
+  r.c = 1.4426950408889634074 / static_cast<double>(greedy ? 1.f : temperature);
+  r.least = 1;
+  if (min_p > 0.f && !greedy) r.least = static_cast<uint64_t>(__builtin_ceil(fmin(min_p, 1.f) * kOne));
+  if (!greedy && r.weight(kLowest) != 0) return false;
+
+  int cut = kBottom;       // bins above it are kept, of the cut the first `ties` tokens
+  uint32_t ties = 0;
+  uint64_t tie_weight = 1;
+  if (greedy) {
+    cut = first;
+    ties = 1;
+  } else {
+    uint64_t mine = 0;     // the tokens around 0, whatever their filter
+    for (uint32_t i = tid; i < centre; i += THREADS)
+      mine += r.weight(bf16_to_f32(sh.value.centre_bits[i]));
+    uint64_t centre_sum;
+    block_scan<THREADS>(mine, sh, &centre_sum);
+    uint64_t counts = 0, sums = 0, all, unused;
+#pragma unroll 1
+    for (int i = bin0; i < bin1; ++i) {
+      const uint32_t c = sh.value.count[i];
+      const uint64_t w = c && i != kCentre && i < kBottom ? r.weight(bin_value(i)) : 0;
+      sh.value.weight[i] = w;
+      counts += c;
+      sums += i == kCentre ? centre_sum : w * c;
+    }
+    const uint64_t sums_before = block_scan<THREADS>(sums, sh, &all);
+    uint64_t limit = all;  // weight that top-k leaves
+    if (k > 0 && k < n) {
+      uint64_t before = block_scan<THREADS>(counts, sh, &unused), sum = sums_before;
+      const uint64_t want = static_cast<uint32_t>(k);
+#pragma unroll 1
+      for (int i = bin0; i < bin1; ++i) {
+        const uint32_t c = sh.value.count[i];
+        const uint64_t w = sh.value.weight[i];
+        if (before < want && before + c >= want) {
+          sh.at = i;
+          sh.answer_ties = static_cast<uint32_t>(want - before);
+          sh.answer64 = sum + w * (want - before);
+          sh.answer32 = c;
+        }
+        before += c;
+        sum += i == kCentre ? centre_sum : w * c;
+      }
+      __syncthreads();
+      cut = sh.at;
+      ties = sh.answer_ties;
+      limit = sh.answer64;
+      if (cut == kCentre) {
+        if (ties != sh.answer32) return false;
+        ++cut;             // all of it
+        ties = 0;
+        limit += centre_sum;
+      }
+      __syncthreads();
+    }
+    if (top_p < 1.f) {
+      const double share = __builtin_ceil(static_cast<double>(top_p) * static_cast<double>(limit));
+      uint64_t target = share < 1.0 ? 1 : static_cast<uint64_t>(share);
+      if (target > limit) target = limit;
+      uint64_t sum = sums_before;
+#pragma unroll 1
+      for (int i = bin0; i < bin1; ++i) {
+        const uint64_t w = sh.value.weight[i];
+        const uint64_t own = i == kCentre ? centre_sum : w * sh.value.count[i];
+        if (sum < target && sum + own >= target) {
+          sh.at = i;
+          sh.answer_ties = i == kCentre ? 0 : static_cast<uint32_t>((target - sum + w - 1) / w);
+        }
+        sum += own;
+      }
+      __syncthreads();
+      if (sh.at == kCentre) return false;
+      cut = sh.at;
+      ties = sh.answer_ties;
+    }
+    tie_weight = cut < kBottom && cut != kCentre ? sh.value.weight[cut] : 0;
+    if (tie_weight < r.least) ties = 0;
+  }
+  __syncthreads();  // counts and weights have been read
+#pragma unroll 1
+  for (int i = bin0; i < bin1; ++i) {
+    const uint64_t w = i < cut && !greedy ? sh.value.weight[i] : 0;
+    sh.value.weight[i] = w >= r.least ? w : 0;
+  }
+  __syncthreads();
+  // kept weights and ties of the blocks; a step whose largest logit lies below the cut
+  // (all but a few, where a filter is on) has none
+  clear<THREADS>(sh.value.last);
+  const int shift = row_shift(n);
+  const int lowest = cut == kBottom ? -32768 : ordered(__float_as_uint(bin_value(cut)) >> 16)[0];
+  for_row<THREADS, bf16_t>(row, n, [&](int i, const Raw8<bf16_t> &z8) {
+    const i16x2 most = __builtin_elementwise_max(__builtin_elementwise_max(ordered(z8.w[0]), ordered(z8.w[1])),
+                                                 __builtin_elementwise_max(ordered(z8.w[2]), ordered(z8.w[3])));
+    if (__builtin_amdgcn_ballot_w64(max(most[0], most[1]) >= lowest) == 0) return;
+    i16x2 bins[4], steps;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) bins[k] = value_bins(z8.w[k], steps);
+    uint64_t sum = 0;
+    uint32_t at_cut = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += sh.value.weight[bins[j / 2][j % 2]];
+    if (ties) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) at_cut += bins[j / 2][j % 2] == cut;
+    }
+    add_step(sh.value.last, i >> shift, sum, at_cut);
+  });
+  if (!greedy && kCentre < cut) {
+    for (uint32_t i = tid; i < centre; i += THREADS) {
+      const uint64_t w = r.weight(bf16_to_f32(sh.value.centre_bits[i]));
+      if (w >= r.least)
+        atomicAdd(&sh.value.last.above[sh.value.centre[i] >> shift], static_cast<unsigned long long>(w));
+    }
+  }
+  pick<THREADS, bf16_t>(p, row, row_id, greedy ? 0.f : u, greedy, tie_weight, ties, sh.value.last, sh,
+                        [&](float z) -> uint64_t {
+                          const int bin = value_bin(__float_as_uint(z) >> 16);
+                          if (bin != kCentre) return sh.value.weight[bin];
+                          if (greedy || kCentre >= cut) return 0;
+                          const uint64_t w = r.weight(z);
+                          return w >= r.least ? w : 0;
+                        },
+                        [&](float z) { return value_bin(__float_as_uint(z) >> 16) == cut; });
+  return true;
+}
+
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) void sample_kernel(SampleParams p) {
   __shared__ Shared sh;
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   const int row_id = blockIdx.x, b = row_id / p.w, n = p.vocab;
@@ -341,13 +765,17 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p) {
                     min_p == min_p && u >= 0.f && u < 1.f;
   if (!fine && tid == 0) report_error(p.dev_error, DAS_DEVERR_SAMPLE);
 
+  const bool greedy = T_raw == 0.f || !fine;
+  if constexpr (sizeof(T) == 2) {
+    if (sample_values<THREADS>(p, row, row_id, T_raw, k, top_p, min_p, u, greedy, sh)) return;
+    __syncthreads();  // its last reads of the shared memory
+  }
+
   // the largest logit and its lowest index
   float best = kNegInf;
   int best_at = 0;
-  for_row<T>(row, n, [&](int i, const float (&z)[8]) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (z[j] > best) best = z[j], best_at = i + j;
+  for_tokens<THREADS, T>(row, n, [&](int i, float z) {
+    if (z > best) best = z, best_at = i;
   });
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) {
@@ -359,12 +787,12 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p) {
   __syncthreads();
   uint64_t top = 0;
 #pragma unroll
-  for (int i = 0; i < kWavesS; ++i) top = sh.part[i] > top ? sh.part[i] : top;
+  for (int i = 0; i < (THREADS / 64); ++i) top = sh.part[i] > top ? sh.part[i] : top;
   best = of_key(static_cast<uint32_t>(top >> 32));
   best_at = static_cast<int>(0xffffffffu - static_cast<uint32_t>(top));
   if (best == kNegInf) best_at = 0;  // nothing to choose from
   // greedy; numbers out of range, and rows without a finite or infinite logit, too
-  if (T_raw == 0.f || !fine || best == kNegInf) {
+  if (greedy || best == kNegInf) {
     if (tid == 0) {
       p.tokens[row_id] = best_at;
       if (p.probs) p.probs[row_id] = 1.f;
@@ -379,103 +807,58 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p) {
   if (min_p > 0.f) r.least = static_cast<uint64_t>(__builtin_ceil(fmin(min_p, 1.f) * kOne));
   r.key = 0;
   r.ties = 0;
-  if (k > 0 && k < n) find_cut<false, T>(row, n, r, k, 0.f, sh);
-  if (top_p < 1.f) find_cut<true, T>(row, n, r, 0, top_p, sh);
+  if (k > 0 && k < n) find_cut<THREADS, false, T>(row, n, r, k, 0.f, sh);
+  if (top_p < 1.f) find_cut<THREADS, true, T>(row, n, r, 0, top_p, sh);
   const uint64_t cut_weight = r.weight(of_key(r.key));
   if (cut_weight < r.least) r.ties = 0;
   __syncthreads();
-
-  // kept weights of every block of 512
-  for_row<T>(row, n, [&](int i, const float (&z)[8]) {
-    uint64_t sum = 0;
-    uint32_t ties = 0;
+  clear<THREADS>(sh.last);
+  const int shift = row_shift(n);
+  auto above = [&](float z) -> uint64_t {
+    if (key_of(z) <= r.key) return 0;
+    const uint64_t w = r.weight(z);
+    return w >= r.least ? w : 0;
+  };
+  auto tie = [&](float z) { return key_of(z) == r.key; };
+  if constexpr (sizeof(T) == 4) {
+    for_row<THREADS, T>(row, n, [&](int i, const Raw8<T> &z8) {
+      uint64_t sum = 0;
+      uint32_t ties = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t key = key_of(z[j]);
-      if (i + j < n && key > r.key) {
-        const uint64_t w = r.weight(z[j]);
-        sum += w >= r.least ? w : 0;
+      for (int j = 0; j < 8; ++j) {
+        const float z = logit<T>(z8, j);
+        sum += above(z);
+        ties += tie(z);
       }
-      ties += i + j < n && key == r.key;
+      add_step(sh.last, i >> shift, sum, r.ties ? ties : 0);
+    });
+  } else {
+    for (int i0 = wave * kStep; i0 < n; i0 += THREADS / 64 * kStep) {
+      uint64_t sum = 0;
+      uint32_t ties = 0;
+      for_each<T>(row, n, i0, kStep, [&](int, float z) {
+        sum += above(z);
+        ties += tie(z);
+      });
+      add_step(sh.last, i0 >> shift, sum, r.ties ? ties : 0);
     }
-    sum = wave_sum(sum);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) ties += __shfl_xor(ties, d, 64);
-    if (lane == 0) {
-      sh.last.above[i / kBlock] = sum;
-      sh.last.ties[i / kBlock] = ties;
-    }
-  });
-  __syncthreads();
-  // their prefix sums: two blocks a thread
-  const int blocks = (n + kBlock - 1) / kBlock;
-  constexpr int PER = kMaxBlocks / kThreads;
-  uint64_t ab[PER], ab_mine = 0;
-  uint64_t ti[PER], ti_mine = 0;
-#pragma unroll
-  for (int q = 0; q < PER; ++q) {
-    const int i = tid * PER + q;
-    ab[q] = i < blocks ? sh.last.above[i] : 0;
-    ti[q] = i < blocks ? sh.last.ties[i] : 0;
-    ab_mine += ab[q];
-    ti_mine += ti[q];
   }
-  uint64_t all_above, all_ties;
-  uint64_t ab_before = block_scan(ab_mine, sh, &all_above);
-  uint64_t ti_before = block_scan(ti_mine, sh, &all_ties);
-  const uint64_t limit = r.ties;  // ties that are kept, at most all there are
-  const uint64_t total = all_above + min(all_ties, limit) * cut_weight;
-  uint64_t target = static_cast<uint64_t>(static_cast<double>(u) * static_cast<double>(total));
-  if (target >= total) target = total - 1;
-#pragma unroll
-  for (int q = 0; q < PER; ++q) {
-    const uint64_t lo = ab_before + min(ti_before, limit) * cut_weight;
-    const uint64_t hi = ab_before + ab[q] + min(ti_before + ti[q], limit) * cut_weight;
-    if (lo <= target && target < hi) {
-      sh.at = tid * PER + q;
-      sh.answer64 = lo;
-      sh.answer32 = static_cast<uint32_t>(ti_before);
-    }
-    ab_before += ab[q];
-    ti_before += ti[q];
-  }
-  __syncthreads();
-  if (wave != 0) return;
-  // the block that passes the target, by one wave
-  const int i = sh.at * kBlock + lane * 8;
-  float z[8];
-  load8<T>(row, i, n, z);
-  uint64_t w[8], mine = 0;
-  uint32_t ties = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) ties += i + j < n && key_of(z[j]) == r.key;
-  uint32_t rank = static_cast<uint32_t>(wave_scan(ties, lane)) - ties + sh.answer32;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t key = key_of(z[j]);
-    w[j] = 0;
-    if (i + j < n && key > r.key) w[j] = r.weight(z[j]);
-    if (i + j < n && key == r.key) w[j] = rank++ < limit ? cut_weight : 0;
-    if (w[j] < r.least) w[j] = 0;
-    mine += w[j];
-  }
-  uint64_t run = sh.answer64 + wave_scan(mine, lane) - mine;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    if (run <= target && target < run + w[j]) {
-      p.tokens[row_id] = i + j;
-      if (p.probs) p.probs[row_id] = static_cast<float>(static_cast<double>(w[j]) / static_cast<double>(total));
-    }
-    run += w[j];
-  }
+  pick<THREADS, T>(p, row, row_id, u, false, cut_weight, r.ties, sh.last, sh, above, tie);
 }
 
 }  // namespace
 
+// Up to a row for every compute unit: 1024 threads, a CU's waves; more rows: 512, two
+// rows to a CU, one of which works while the other waits at a barrier.
 hipError_t launch_sample(const SampleParams &p, int dtype, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(p.batch) * p.w), block(kThreads);
-  if (dtype == DAS_F32) return launch_kernel(sample_kernel<float>, grid, block, s, p);
-  return launch_kernel(sample_kernel<bf16_t>, grid, block, s, p);
+  const int rows = p.batch * p.w;
+  const dim3 grid(static_cast<unsigned>(rows));
+  if (rows <= kNumCUs) {
+    if (dtype == DAS_F32) return launch_kernel(sample_kernel<float, 1024>, grid, dim3(1024), s, p);
+    return launch_kernel(sample_kernel<bf16_t, 1024>, grid, dim3(1024), s, p);
+  }
+  if (dtype == DAS_F32) return launch_kernel(sample_kernel<float, 512>, grid, dim3(512), s, p);
+  return launch_kernel(sample_kernel<bf16_t, 512>, grid, dim3(512), s, p);
 }
 
 }  // namespace das
