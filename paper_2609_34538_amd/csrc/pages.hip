@@ -11,8 +11,10 @@
 // sum is at most F + R.
 //
 // One workgroup: the prefix sums run over the batch 1024 sequences at a time, and the
-// entries that change are few (a step of w tokens moves about w / 64 pages a sequence).
-// Bound by the launch and its dependent round trips.
+// entries that change are few (a step of w tokens moves about w / 64 pages a sequence; a
+// sequence with many is moved by its wave). Slots of few positions are written by the same
+// workgroup, others by a grid of their own. Bound by the launch and its dependent round
+// trips.
 
 #include "q8_internal.h"
 
@@ -21,25 +23,49 @@ namespace {
 
 constexpr int kThreads = 1024;
 
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int plus_dpp(int x) {
+  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+// Inclusive prefix sums: in rows of 16 lanes, then from row to row.
+__device__ __forceinline__ int row_scan(int x) {
+  x = plus_dpp<0x111>(x);
+  x = plus_dpp<0x112>(x);
+  x = plus_dpp<0x114>(x);
+  return plus_dpp<0x118>(x);
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  return plus_dpp<0x143, 0xc>(plus_dpp<0x142, 0xa>(row_scan(x)));
+}
 // Inclusive prefix sum over the workgroup; *total is the sum. `part`: 16 words.
 __device__ __forceinline__ int block_scan(int x, int *part, int *total) {
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d, 64);
-    if (lane >= d) x += y;
-  }
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  x = wave_scan(x);
   __syncthreads();  // the previous call's parts have been read
   if (lane == 63) part[wave] = x;
   __syncthreads();
-  int before = 0, all = 0;
-#pragma unroll
-  for (int k = 0; k < kThreads / 64; ++k) {
-    if (k < wave) before += part[k];
-    all += part[k];
+  const int v = row_scan(lane < kThreads / 64 ? part[lane] : 0);
+  *total = __builtin_amdgcn_readlane(v, kThreads / 64 - 1);
+  return x + (wave > 0 ? __builtin_amdgcn_readlane(v, wave - 1) : 0);
+}
+
+// fn(table entry, item) for `count` entries from `column` and `item` of
+// every lane's sequence b: a lane by itself up to kOwn, else the whole wave.
+constexpr int kOwn = 4;
+constexpr int kOwnSlots = 8192;  // slots that the bookkeeping's workgroup writes itself
+template <typename Fn>
+__device__ __forceinline__ void for_entries(const PagesParams &p, int b, int count, int column, int item, Fn &&fn) {
+  const int lane = threadIdx.x % 64;
+  auto row = [&](int seq) { return p.block_table + static_cast<size_t>(seq) * p.max_pages; };
+  for (int k = 0; k < (count <= kOwn ? count : 0); ++k) fn(row(b)[column + k], item + k);
+  uint64_t many = __builtin_amdgcn_ballot_w64(count > kOwn);
+  while (many) {
+    const int l = __builtin_ctzll(many);
+    many &= many - 1;
+    const int n = __builtin_amdgcn_readlane(count, l), c = __builtin_amdgcn_readlane(column, l);
+    const int first = __builtin_amdgcn_readlane(item, l), seq = __builtin_amdgcn_readlane(b, l);
+    for (int k = lane; k < n; k += 64) fn(row(seq)[c + k], first + k);
   }
-  *total = all;
-  return x + before;
 }
 
 struct Seq {
@@ -56,83 +82,83 @@ __device__ __forceinline__ Seq read_seq(const PagesParams &p, int b) {
   return s;
 }
 
+__device__ __forceinline__ int slot_of(const PagesParams &p, int b, int i) {
+  const long pos = static_cast<long>(p.first[b]) + i;
+  const int held = p.pages_held[b];
+  if (pos < 0 || pos >= p.lengths[b] || held > p.max_pages || pos / kPage >= held) return -1;
+  const int page = p.block_table[static_cast<size_t>(b) * p.max_pages + pos / kPage];
+  return page >= 0 && page < p.num_pages ? page * kPage + static_cast<int>(pos % kPage) : -1;
+}
+
+__global__ __launch_bounds__(256) void page_slots_kernel(PagesParams p) {
+  const int it = blockIdx.x * 256 + threadIdx.x;
+  if (it < p.batch * p.w) p.slots[it] = slot_of(p, it / p.w, it % p.w);
+}
+
 __global__ __launch_bounds__(kThreads) void pages_update_kernel(PagesParams p) {
   __shared__ int part[kThreads / 64];
+  __shared__ int s_back, s_taken;
   const int tid = threadIdx.x;
+  if (tid == 0) s_back = s_taken = 0;
   const int F = *p.num_free;
-  // what is given back, in all
-  int R = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
-    const Seq s = read_seq(p, b0 + tid);
-    if (b0 + tid < p.batch && !s.ok) report_error(p.dev_error, DAS_DEVERR_PREFIX);
-    int total;
-    block_scan(s.ok ? max(s.held - s.need, 0) : 0, part, &total);
-    R += total;
+  // what is given back, in all (at most batch * max_pages, which fits)
+  int mine = 0;
+  for (int b = tid; b < p.batch; b += kThreads) {
+    const Seq s = read_seq(p, b);
+    if (!s.ok) report_error(p.dev_error, DAS_DEVERR_PREFIX);
+    else mine += max(s.held - s.need, 0);
   }
+  __syncthreads();
+  mine = wave_scan(mine);
+  if (tid % 64 == 63 && mine) atomicAdd(&s_back, mine);
+  __syncthreads();
+  const int R = s_back;
   // a stack that cannot hold them all: nothing is moved
-  const bool broken = F < 0 || F > p.num_pages || R > p.num_pages - F;
-  if (broken) {
+  if (F < 0 || F > p.num_pages || R > p.num_pages - F) {
     if (tid == 0) report_error(p.dev_error, DAS_DEVERR_POOL);
   } else {
     const int top = F + R;
-    int r0 = 0;
-    if (R > 0) {
-      for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
-        const int b = b0 + tid;
-        const Seq s = read_seq(p, b);
-        const int back = s.ok ? max(s.held - s.need, 0) : 0;
-        int total;
-        int r = r0 + block_scan(back, part, &total) - back;
-        r0 += total;
-        int32_t *row = p.block_table + static_cast<size_t>(b) * p.max_pages;
-        for (int c = s.need; back > 0 && c < s.held; ++c, ++r) {
-          p.free_pages[top - 1 - r] = row[c];
-          row[c] = -1;
-        }
-      }
+    for (int b0 = 0, r0 = 0; R > 0 && b0 < p.batch; b0 += kThreads) {
+      const Seq s = read_seq(p, b0 + tid);
+      const int back = s.ok ? max(s.held - s.need, 0) : 0;
+      int total;
+      const int r = r0 + block_scan(back, part, &total) - back;
+      r0 += total;
+      for_entries(p, b0 + tid, back, s.need, r, [&](int32_t &entry, int item) {
+        p.free_pages[top - 1 - item] = entry;
+        entry = -1;
+      });
     }
     __syncthreads();  // released pages are on the stack
-    int j0 = 0, taken = 0;
-    for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
+    for (int b0 = 0, j0 = 0; b0 < p.batch; b0 += kThreads) {
       const int b = b0 + tid;
       const Seq s = read_seq(p, b);
       const int more = s.ok ? max(s.need - s.held, 0) : 0;
       int total;
-      const int upto = block_scan(more, part, &total);
-      const int incl = j0 + upto;  // at most batch * max_pages, which fits
-      const bool served = incl <= top;
-      int32_t *row = p.block_table + static_cast<size_t>(b) * p.max_pages;
-      if (more > 0 && served)
-        for (int c = s.held, j = incl - more; c < s.need; ++c, ++j) row[c] = p.free_pages[top - 1 - j];
-      if (more > 0 && !served) report_error(p.dev_error, DAS_DEVERR_POOL);
-      if (b < p.batch && s.ok && (more == 0 || served)) p.pages_held[b] = s.need;
-      int given;
-      block_scan(served ? more : 0, part, &given);
-      taken += given;
+      const int incl = j0 + block_scan(more, part, &total);
       j0 += total;
+      const bool served = incl <= top;
+      if (more > 0 && !served) report_error(p.dev_error, DAS_DEVERR_POOL);
+      for_entries(p, b, served ? more : 0, s.held, incl - more,
+                  [&](int32_t &entry, int item) { entry = p.free_pages[top - 1 - item]; });
+      // sums grow along the batch, so the last served one's is what was taken
+      if (served && more > 0) atomicMax(&s_taken, incl);
+      if (b < p.batch && s.ok && (more == 0 || served)) p.pages_held[b] = s.need;
     }
-    if (tid == 0) *p.num_free = top - taken;
+    __syncthreads();
+    if (tid == 0) *p.num_free = top - s_taken;
   }
-  if (!p.slots) return;
+  if (!p.slots || p.batch * p.w > kOwnSlots) return;
   __syncthreads();  // tables and counts are written
-  const int items = p.batch * p.w;
-  for (int it = tid; it < items; it += kThreads) {
-    const int b = it / p.w;
-    const long pos = static_cast<long>(p.first[b]) + it % p.w;
-    const int held = p.pages_held[b];
-    int slot = -1;
-    if (pos >= 0 && pos < p.lengths[b] && held <= p.max_pages && pos / kPage < held) {
-      const int page = p.block_table[static_cast<size_t>(b) * p.max_pages + pos / kPage];
-      if (page >= 0 && page < p.num_pages) slot = page * kPage + static_cast<int>(pos % kPage);
-    }
-    p.slots[it] = slot;
-  }
+  for (int it = tid; it < p.batch * p.w; it += kThreads) p.slots[it] = slot_of(p, it / p.w, it % p.w);
 }
 
 }  // namespace
 
 hipError_t launch_pages_update(const PagesParams &p, hipStream_t s) {
-  return launch_kernel(pages_update_kernel, dim3(1), dim3(kThreads), s, p);
+  const hipError_t e = launch_kernel(pages_update_kernel, dim3(1), dim3(kThreads), s, p);
+  if (e != hipSuccess || !p.slots || p.batch * p.w <= kOwnSlots) return e;
+  return launch_kernel(page_slots_kernel, dim3((p.batch * p.w + 255) / 256), dim3(256), s, p);
 }
 
 }  // namespace das
