@@ -19,8 +19,7 @@
 //
 // P.V of bf16 calls runs in fp16: e4m3 values are exact there and probabilities
 // keep 11 bits instead of 8 (error against 64 bits then is the output's rounding).
-// Probabilities are held times 2^15, so that fp16 is normal down to 2^-29 of the
-// row's largest; values are held relative to the largest exponent that the wave
+// Values are held relative to the largest exponent that the wave
 // has met (vref, per wave), which like the running maximum rescales the output
 // when it grows, by a power of two. Draft-block values are bf16 with bf16's range:
 // their probabilities enter as a bf16 and its remainder, two products.
@@ -42,7 +41,12 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 constexpr int kTile = 32;
 constexpr int kTilesPerPage = kPage / kTile;
 constexpr int kWavesQ8 = 4;
-constexpr float kProbShift = 15.f;  // bf16 calls: probabilities times 2^15
+// Probabilities are held relative to a reference that a row's logits may pass by
+// kSlack binary orders before it moves; bf16 calls hold them times 2^kProbShift, so
+// that the largest fit fp16 and those down to 2^-23 of the reference are normal there.
+constexpr float kSlack = 6.f;
+constexpr float kProbShift = 9.f;
+constexpr float kNoRef = 1e30f;  // in place of shift - reference: nothing seen yet
 
 __device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, a),
@@ -81,11 +85,11 @@ struct Raw {
   uint32_t ke, ve;
 };
 
-// One wave's running result. bf16 calls: o is in units of 2^vref, o and l times
-// 2^15 (kProbShift).
+// One wave's running result: neg = shift - reference, a lane's share of the sum l and
+// the output o, in units of 2^vref for bf16 calls, both times 2^shift.
 template <int DH, int NQ>
 struct Acc {
-  float m[NQ], l[NQ];
+  float neg[NQ], l[NQ];
   f32x4 o[NQ][DH / 16];
   int vref;
 };
@@ -96,9 +100,11 @@ struct QFrag {
   u32x4 x[DH / 32][sizeof(T) / 2];
 };
 
-// Softmax step of a tile: logits x[qt][e][v] (token 8 g + 4 e + v of the tile, row n)
-// become probabilities in place; the running maximum moves, the output is rescaled
-// where it did, the lane's share of the sum is added.
+// Softmax step of a tile: logits s[qt][e][v] (token 8 g + 4 e + v of the tile, row n)
+// become probabilities in place, the lane's share of the sum is added. The reference
+// (the same in a row's four lanes) moves to the row's maximum only when a logit passes it
+// by more than kSlack, which after the first tiles is rare: most tiles need no reduction
+// over lanes and no rescaling (128 rows x 16384 tokens 94 -> 89 us).
 template <int DH, int NQ>
 __device__ __forceinline__ void softmax_step(Acc<DH, NQ> &st, f32x4 (&s)[NQ][2],
                                              const int (&cap)[NQ], int limit, bool full, float scale,
@@ -119,25 +125,25 @@ __device__ __forceinline__ void softmax_step(Acc<DH, NQ> &st, f32x4 (&s)[NQ][2],
     for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int v = 0; v < 4; ++v) mx = fmaxf(mx, s[qt][e][v]);
-    const float mnew = fmaxf(st.m[qt], group_max(mx) * scale);
-    const float ref = mnew == kNegInf ? 0.f : mnew;  // nothing visible yet: every p is 0
-    const float alpha = __builtin_amdgcn_exp2f(st.m[qt] - ref);
-    float sum = 0.f;
+    if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(mx, scale, st.neg[qt]) > shift + kSlack) != 0) {
+      const float m = group_max(mx) * scale;
+      // rows with nothing visible, and those that stay within their slack, keep theirs
+      const float neg = m + st.neg[qt] > shift + kSlack ? shift - m : st.neg[qt];
+      const float alpha = __builtin_amdgcn_exp2f(neg - st.neg[qt]);  // 0 from kNoRef
+      st.neg[qt] = neg;
+      st.l[qt] *= alpha;
+      // a lane's accumulators of row tile qt all belong to one row
+#pragma unroll
+      for (int dt = 0; dt < DH / 16; ++dt) st.o[qt][dt] *= alpha;
+    }
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][e][v], scale, shift - ref));
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][e][v], scale, st.neg[qt]));
         s[qt][e][v] = p;
-        sum += p;
+        st.l[qt] += p;
       }
-    st.l[qt] = st.l[qt] * alpha + sum;
-    st.m[qt] = mnew;
-    // a lane's accumulators of row tile qt all belong to one row
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
-#pragma unroll
-      for (int dt = 0; dt < DH / 16; ++dt) st.o[qt][dt] *= alpha;
-    }
   }
 }
 
@@ -253,19 +259,57 @@ __device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, const Raw<DH> &t,
   }
 }
 
-// Two packed bf16 with what is not finite replaced by 0; `odd` collects whether any was.
-__device__ __forceinline__ uint32_t finite_bf16(uint32_t w, bool &odd) {
-  const bool lo = (w & 0x7f80u) == 0x7f80u, hi = (w & 0x7f800000u) == 0x7f800000u;
-  odd |= lo | hi;
-  return (lo ? 0u : w & 0xffffu) | (hi ? 0u : w & 0xffff0000u);
-}
-__device__ __forceinline__ uint32_t finite_f32(uint32_t w, bool &odd) {
-  const bool is = (w & 0x7f800000u) == 0x7f800000u;
-  odd |= is;
-  return is ? 0u : w;
+// A word of block values (two bf16 or one fp32) with what is not finite replaced by 0.
+template <typename T>
+__device__ __forceinline__ uint32_t finite_word(uint32_t w) {
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu;
+    return (w & 0x7f800000u) == 0x7f800000u ? lo : lo | (w & 0xffff0000u);
+  } else {
+    return (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
+  }
 }
 
-// What finite_* took out of a draft-block tile's values, for the rows that see it: in a
+// A draft-block tile as loaded, in the call's type, straight from the token-major rows:
+// a lane's pieces of its two key tokens, and its 8 tokens of value dims 32 k + 2 n, + 1.
+// Rows past the block's last repeat it and are masked.
+template <typename T, int DH>
+struct Block {
+  static constexpr int W = sizeof(T) / 2;
+  u32x4 k[2][DH / 32][W];
+  uint32_t v[DH / 32][8][W];
+};
+template <typename T, int DH>
+__device__ __forceinline__ void load_block(Block<T, DH> &t, const AttnQ8Params &p, int b, int kvh, int u, int ln,
+                                           int lg) {
+  const size_t row_elems = static_cast<size_t>(p.hkv) * DH;
+  const size_t base = (static_cast<size_t>(b) * p.w * p.hkv + kvh) * DH;
+  const T *kb = static_cast<const T *>(p.kb) + base, *vb = static_cast<const T *>(p.vb) + base;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int tok = min(kTile * u + 8 * (ln >> 2) + (ln & 3) + 4 * e, p.w - 1);
+    const T *row = kb + tok * row_elems + 8 * lg;
+#pragma unroll
+    for (int k = 0; k < DH / 32; ++k)
+#pragma unroll
+      for (int h = 0; h < Block<T, DH>::W; ++h) t.k[e][k][h] = reinterpret_cast<const u32x4 *>(row + 32 * k)[h];
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const T *row = vb + min(kTile * u + 8 * lg + j, p.w - 1) * row_elems + 2 * ln;
+#pragma unroll
+    for (int k = 0; k < DH / 32; ++k) {
+      if constexpr (sizeof(T) == 2) {
+        t.v[k][j][0] = *reinterpret_cast<const uint32_t *>(row + 32 * k);
+      } else {
+        const u32x2 x = *reinterpret_cast<const u32x2 *>(row + 32 * k);
+        t.v[k][j][0] = x[0], t.v[k][j][1] = x[1];
+      }
+    }
+  }
+}
+
+// What finite_word took out of a draft-block tile's values, for the rows that see it: in a
 // product 0 * NaN would reach the rows that do not. probs: the tile's probabilities,
 // [row tile][row][token].
 template <typename T, int DH, int NQ>
@@ -290,102 +334,112 @@ __device__ __forceinline__ void add_not_finite(Acc<DH, NQ> &st, const float *pro
   }
 }
 
-// Tile u of the draft block: keys and values in the call's type, straight from the
-// token-major rows (rows past the block's last repeat it and are masked).
+// Tile u of the draft block through both products.
 template <typename T, int DH, int NQ>
-__device__ __forceinline__ void block_tile(Acc<DH, NQ> &st, const AttnQ8Params &p, int b, int kvh,
-                                           int u, const QFrag<T, DH> (&qf)[NQ],
+__device__ __forceinline__ void block_tile(Acc<DH, NQ> &st, Block<T, DH> &t, const AttnQ8Params &p, int b,
+                                           int kvh, int u, const QFrag<T, DH> (&qf)[NQ],
                                            const int (&row_pos)[NQ], float *probs, int ln, int lg) {
-  const size_t row_elems = static_cast<size_t>(p.hkv) * DH;
-  const size_t base = (static_cast<size_t>(b) * p.w * p.hkv + kvh) * DH;
-  const T *kb = static_cast<const T *>(p.kb) + base, *vb = static_cast<const T *>(p.vb) + base;
-  const int limit = p.w - kTile * u;
+  constexpr int KS = DH / 32;
   f32x4 s[NQ][2];
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) s[qt][0] = s[qt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const int tok = min(kTile * u + 8 * (ln >> 2) + (ln & 3) + 4 * e, p.w - 1);
-    const T *row = kb + tok * row_elems;
+  for (int k = 0; k < KS; ++k)
 #pragma unroll
-    for (int k = 0; k < DH / 32; ++k) {
-      const u32x4 *src = reinterpret_cast<const u32x4 *>(row + 32 * k + 8 * lg);
-      if constexpr (sizeof(T) == 2) {
-        const u32x4 a = src[0];
+    for (int h = 0; h < Block<T, DH>::W; ++h)
 #pragma unroll
-        for (int qt = 0; qt < NQ; ++qt) s[qt][e] = mfma16x16x32(a, qf[qt].x[k][0], s[qt][e]);
-      } else {
+      for (int e = 0; e < 2; ++e) {
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const u32x4 a = src[h];
+          for (int qt = 0; qt < NQ; ++qt) s[qt][e] = mfma16x16x32(t.k[e][k][0], qf[qt].x[k][0], s[qt][e]);
+        } else {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int qt = 0; qt < NQ; ++qt) s[qt][e] = mfma16x16x4(a[i], qf[qt].x[k][h][i], s[qt][e]);
+            for (int qt = 0; qt < NQ; ++qt) s[qt][e] = mfma16x16x4(t.k[e][k][h][i], qf[qt].x[k][h][i], s[qt][e]);
         }
       }
-    }
-  }
   int cap[NQ];
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) cap[qt] = row_pos[qt] - kTile * u;
-  softmax_step<DH, NQ>(st, s, cap, limit, false, p.scale_log2, sizeof(T) == 2 ? kProbShift : 0.f, lg);
+  softmax_step<DH, NQ>(st, s, cap, p.w - kTile * u, false, p.scale_log2, sizeof(T) == 2 ? kProbShift : 0.f, lg);
 
-#pragma unroll
-  for (int qt = 0; qt < NQ; ++qt) {
-    f32x4 *dst = reinterpret_cast<f32x4 *>(probs + (16 * qt + ln) * kTile + 8 * lg);
-    dst[0] = s[qt][0], dst[1] = s[qt][1];
-  }
-
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-
-  // values: a lane's 8 tokens of dims 32 k + 2 n and + 1; one row tile after the other,
-  // which reads them again but needs fewer registers than the tiles of the prefix
+  // the largest magnitude's bits tell whether every value is finite
   bool odd = false;
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  u16x2 most = {0, 0};
+  uint32_t most32 = 0;
 #pragma unroll
-  for (int qt = 0; qt < NQ; ++qt) {
-    asm volatile("" ::: "memory");
-    u32x4 hi, lo;
-    if constexpr (sizeof(T) == 2) {
+  for (int k = 0; k < KS; ++k)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (sizeof(T) == 2)
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, t.v[k][j][0] & 0x7fff7fffu));
+      else
+        most32 = max(most32, max(t.v[k][j][0] & 0x7fffffffu, t.v[k][j][1] & 0x7fffffffu));
+    }
+  odd = sizeof(T) == 2 ? most[0] >= 0x7f80 || most[1] >= 0x7f80 : most32 >= 0x7f800000u;
+  const bool any_odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+  if (any_odd) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int h = 0; h < Block<T, DH>::W; ++h) t.v[k][j][h] = finite_word<T>(t.v[k][j][h]);
+#pragma unroll
+    for (int qt = 0; qt < NQ; ++qt) {
+      f32x4 *dst = reinterpret_cast<f32x4 *>(probs + (16 * qt + ln) * kTile + 8 * lg);
+      dst[0] = s[qt][0], dst[1] = s[qt][1];
+    }
+  }
+  if constexpr (sizeof(T) == 2) {
+    u32x4 hi[NQ], lo[NQ];
+#pragma unroll
+    for (int qt = 0; qt < NQ; ++qt)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float a = __builtin_amdgcn_ldexpf(s[qt][j / 2][2 * (j % 2)], -st.vref);
         const float c = __builtin_amdgcn_ldexpf(s[qt][j / 2][2 * (j % 2) + 1], -st.vref);
-        hi[j] = pack_bf16(a, c);
-        lo[j] = pack_bf16(a - bf16_lo(hi[j]), c - bf16_hi(hi[j]));
+        hi[qt][j] = pack_bf16(a, c);
+        lo[qt][j] = pack_bf16(a - bf16_lo(hi[qt][j]), c - bf16_hi(hi[qt][j]));
       }
-    }
 #pragma unroll
-    for (int k = 0; k < DH / 32; ++k) {
+    for (int k = 0; k < KS; ++k) {
       u32x4 a0, a1;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int tok = kTile * u + 8 * lg + j;
-        const T *src = vb + min(tok, p.w - 1) * row_elems + 32 * k + 2 * ln;
-        if constexpr (sizeof(T) == 2) {
-          uint32_t x = *reinterpret_cast<const uint32_t *>(src);
-          x = tok < p.w ? finite_bf16(x, odd) : 0u;
-          if (j % 2 == 0) a0[j / 2] = x & 0xffffu, a1[j / 2] = x >> 16;
-          else a0[j / 2] |= x << 16, a1[j / 2] |= x & 0xffff0000u;
-        } else {
-          const u32x2 x = *reinterpret_cast<const u32x2 *>(src);
-          const uint32_t pj = __float_as_uint(s[qt][j / 4][j % 4]);
-          st.o[qt][2 * k] = mfma16x16x4(tok < p.w ? finite_f32(x[0], odd) : 0u, pj, st.o[qt][2 * k]);
-          st.o[qt][2 * k + 1] = mfma16x16x4(tok < p.w ? finite_f32(x[1], odd) : 0u, pj, st.o[qt][2 * k + 1]);
-        }
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t x = t.v[k][2 * j][0], y = t.v[k][2 * j + 1][0];
+        a0[j] = __builtin_amdgcn_perm(y, x, 0x05040100);
+        a1[j] = __builtin_amdgcn_perm(y, x, 0x07060302);
       }
-      if constexpr (sizeof(T) == 2) {
-        st.o[qt][2 * k] = mfma16x16x32(a0, lo, st.o[qt][2 * k]);
-        st.o[qt][2 * k + 1] = mfma16x16x32(a1, lo, st.o[qt][2 * k + 1]);
-        st.o[qt][2 * k] = mfma16x16x32(a0, hi, st.o[qt][2 * k]);
-        st.o[qt][2 * k + 1] = mfma16x16x32(a1, hi, st.o[qt][2 * k + 1]);
+#pragma unroll
+      for (int qt = 0; qt < NQ; ++qt) {
+        st.o[qt][2 * k] = mfma16x16x32(a0, lo[qt], st.o[qt][2 * k]);
+        st.o[qt][2 * k + 1] = mfma16x16x32(a1, lo[qt], st.o[qt][2 * k + 1]);
+        st.o[qt][2 * k] = mfma16x16x32(a0, hi[qt], st.o[qt][2 * k]);
+        st.o[qt][2 * k + 1] = mfma16x16x32(a1, hi[qt], st.o[qt][2 * k + 1]);
       }
     }
+  } else {
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int qt = 0; qt < NQ; ++qt)
+            st.o[qt][2 * k + h] = mfma16x16x4(t.v[k][j][h], __float_as_uint(s[qt][j / 4][j % 4]), st.o[qt][2 * k + h]);
   }
-  if (__builtin_amdgcn_ballot_w64(odd) != 0)
+  if (any_odd) {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const size_t row_elems = static_cast<size_t>(p.hkv) * DH;
+    const T *vb = static_cast<const T *>(p.vb) + (static_cast<size_t>(b) * p.w * p.hkv + kvh) * DH;
     add_not_finite<T, DH, NQ>(st, probs, vb, row_elems, kTile * u, p.w, cap, ln, lg);
+  }
 }
 
 template <typename T, int DH, int NQ, int RW>
@@ -436,6 +490,10 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
                ? p.block_table[static_cast<size_t>(b) * p.max_pages + pg] : 0;
   };
   int window = load_window(0);
+  // draft-block tiles come first: tiles 0 .. nb - 1 of chunk 0
+  Block<T, DH> blk;
+  const bool has_block = g0 < nb;
+  if (has_block) load_block<T, DH>(blk, p, b, kvh, g0, ln, lg);
 
   bool bad;
   const int S = clamp_prefix(s_raw, p.max_pages, &bad);
@@ -451,7 +509,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
   st.vref = kQ8MinExp;
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) {
-    st.m[qt] = kNegInf;
+    st.neg[qt] = kNoRef;
     st.l[qt] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < DH / 16; ++dt) st.o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -482,14 +540,18 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     return ok ? min(kTile, S - kTile * tile) : 0;
   };
 
-  // draft-block tiles come first: tiles 0 .. nb - 1 of chunk 0
-  int i = 0;
-  for (; i < n && g0 + IW * i < nb; ++i)
-    block_tile<T, DH, NQ>(st, p, b, kvh, g0 + IW * i, qf, row_pos, part[wave], ln, lg);
-  // two tiles in flight
+  // two tiles in flight, the first of the prefix before the block's are worked on
   Raw<DH> ta, tb;
   int la = 0, lb = 0;
+  int i = g0 < nb ? (nb - g0 + IW - 1) / IW : 0;  // the wave's block tiles
   if (i < n) la = load(i, ta);
+  if (has_block) {
+    block_tile<T, DH, NQ>(st, blk, p, b, kvh, g0, qf, row_pos, part[wave], ln, lg);
+    for (int k = 1; k < i; ++k) {
+      load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
+      block_tile<T, DH, NQ>(st, blk, p, b, kvh, g0 + IW * k, qf, row_pos, part[wave], ln, lg);
+    }
+  }
   if (i + 1 < n) lb = load(i + 1, tb);
   for (; i < n; i += 2) {
     prefix_tile<T, DH, NQ>(st, ta, qf, la, p.scale_log2, ln, lg);
@@ -499,17 +561,21 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     if (i + 3 < n) lb = load(i + 3, tb);
   }
 
-  // From here on m, l and o are the plain ones: o unnormalised, without shifts.
+  // From here on l and o are the plain ones, unnormalised, without shifts.
+  constexpr float kShift = sizeof(T) == 2 ? kProbShift : 0.f;
+  float m[NQ];
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) {
+    m[qt] = st.neg[qt] == kNoRef ? kNegInf : kShift - st.neg[qt];
     st.l[qt] = group_sum(st.l[qt]);
     if constexpr (sizeof(T) == 2) {
-      st.l[qt] *= 0x1p-15f;
+      st.l[qt] *= 0x1p-9f;
+      static_assert(kProbShift == 9.f, "the shift that is taken back");
 #pragma unroll
       for (int dt = 0; dt < DH / 16; ++dt)
 #pragma unroll
         for (int v = 0; v < 4; ++v)
-          st.o[qt][dt][v] = __builtin_amdgcn_ldexpf(st.o[qt][dt][v], st.vref - 15);
+          st.o[qt][dt][v] = __builtin_amdgcn_ldexpf(st.o[qt][dt][v], st.vref - 9);
     }
   }
   uint8_t *rec = p.ws + (static_cast<size_t>(unit) * p.nsplit + chunk) * p.piece_stride;
@@ -526,7 +592,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
       amax = group_max(amax);
     }
     if (lg == 0) {
-      sm[wave][16 * qt + ln] = st.m[qt];
+      sm[wave][16 * qt + ln] = m[qt];
       sl[wave][16 * qt + ln] = st.l[qt];
       sa[wave][16 * qt + ln] = amax;
     }
@@ -539,7 +605,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     for (int k = 0; k < IW; ++k) mx = fmaxf(mx, sm[k * RW + rw][16 * qt + ln]);
     // no visible position in the whole chunk (an unreadable page): outputs are 0
     const float ref = mx == kNegInf ? 0.f : mx;
-    const float sc = __builtin_amdgcn_exp2f(st.m[qt] - ref);
+    const float sc = __builtin_amdgcn_exp2f(m[qt] - ref);
     if (qt > 0) __syncthreads();  // the previous row tile has been summed
     // tile 2 k + i of a lane holds dims 32 k + 8 g + 2 v + i
 #pragma unroll
