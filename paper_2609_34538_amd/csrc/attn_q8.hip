@@ -442,15 +442,33 @@ __device__ __forceinline__ void block_tile(Acc<DH, NQ> &st, Block<T, DH> &t, con
   }
 }
 
+// Shared memory of a workgroup. RW > 1: the tiles that waves with different rows share, a
+// ring of NB steps of IW tiles, their exponents per wave, and room for a block tile's
+// probabilities; afterwards the merge area of one row tile. RW == 1: the merge area, before
+// that the probabilities.
+template <int DH, int NQ, int RW>
+struct Lds {
+  static constexpr int IW = kWavesQ8 / RW;             // waves that share a chunk's tiles
+  static constexpr int NB = RW == 1 ? 0 : RW == 2 ? 3 : 4;
+  static constexpr int TILE = 2 * kTile * DH;          // bytes of a tile
+  static constexpr int RS = DH + 4;                    // row stride of the merge area (floats)
+  static constexpr int EXPS = NB * IW * TILE;
+  static constexpr int PROBS = EXPS + NB * kWavesQ8 * 8;
+  static constexpr int PROB_STRIDE = RW == 1 ? 16 * RS * 4 : 16 * NQ * kTile * 4;
+  static constexpr int MERGE = kWavesQ8 * 16 * RS * 4;
+  static constexpr int BYTES = PROBS + kWavesQ8 * PROB_STRIDE > MERGE ? PROBS + kWavesQ8 * PROB_STRIDE : MERGE;
+  static_assert(PROB_STRIDE >= 16 * NQ * kTile * 4 && PROBS % 16 == 0, "a tile's probabilities fit");
+};
+
 template <typename T, int DH, int NQ, int RW>
 __global__ __launch_bounds__(64 * kWavesQ8) __attribute__((amdgpu_waves_per_eu(2)))
 void attn_q8_kernel(AttnQ8Params p, int n_rg) {
-  constexpr int IW = kWavesQ8 / RW;   // waves that share a chunk's tiles
-  constexpr int RS = DH + 4;          // row stride of the merge area (floats)
+  using L = Lds<DH, NQ, RW>;
+  constexpr int IW = L::IW;
+  constexpr int RS = L::RS;
   constexpr int KS = DH / 32;
-  // the merge area of one row tile; before that, a draft-block tile's probabilities
-  __shared__ __attribute__((aligned(16))) float part[kWavesQ8][16 * RS];
-  static_assert(16 * RS >= 16 * NQ * kTile, "a tile's probabilities fit");
+  __shared__ __attribute__((aligned(16))) uint8_t smem[L::BYTES];
+  float(*part)[16 * RS] = reinterpret_cast<float(*)[16 * RS]>(smem);
   __shared__ float sm[kWavesQ8][16 * NQ], sl[kWavesQ8][16 * NQ], sa[kWavesQ8][16 * NQ];
 
   const int lane = threadIdx.x & 63;
@@ -515,50 +533,115 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     for (int dt = 0; dt < DH / 16; ++dt) st.o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  float *probs = reinterpret_cast<float *>(smem + L::PROBS + wave * L::PROB_STRIDE);
   const uint32_t lane_k = (ln >> 2) * 8 * DH + lg * 64 + (ln & 3) * 16;
   const uint32_t lane_v = lg * 8 * DH + ln * 16;
-  // Loads of the wave's i-th tile; the number of its visible tokens comes back. An
-  // out-of-range page id is reported and read as page 0 (its tile is masked out).
-  auto load = [&](int i, Raw<DH> &t) {
-    if (i >= 64 && i % 64 == 0) window = load_window(i);
+  // Where the wave's i-th tile lies, and the number of its visible tokens. An out-of-range
+  // page id is reported and read as page 0 (its tile is masked out).
+  auto locate = [&](int i, size_t &off, size_t &eoff) {
+    if (i >= 64 && i % 64 == 0) {
+      window = load_window(i);
+      wait_vmcnt<0>();  // here: otherwise every use of it waits for all loads under way
+    }
     const int page_raw = __builtin_amdgcn_readlane(window, i & 63);
     const bool ok = page_raw >= 0 && page_raw < p.num_pages;
-    if (!ok) report_error(p.dev_error, DAS_DEVERR_PAGE);
+    if (!ok && i < n) report_error(p.dev_error, DAS_DEVERR_PAGE);
     const int page = ok ? page_raw : 0;
     const int tile = g0 + IW * i - nb, half = tile % kTilesPerPage;
-    const size_t off = (static_cast<size_t>(kvh) * p.num_pages + page) * (kPage * DH) + half * kTile * DH;
-    const size_t eoff = (static_cast<size_t>(page) * p.hkv + kvh) * kQ8GroupsPerPage + 4 * half;
-    const auto rk = buffer_of(p.k_layer + off, kTile * DH), rv = buffer_of(p.v_layer + off, kTile * DH);
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-      t.k[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, lane_k, 256 * k, kNonTemporal));
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-      t.v[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, lane_v, 256 * k, kNonTemporal));
-    t.ke = *reinterpret_cast<const uint32_t *>(p.k_exp + eoff);
-    t.ve = *reinterpret_cast<const uint32_t *>(p.v_exp + eoff);
+    off = (static_cast<size_t>(kvh) * p.num_pages + page) * (kPage * DH) + half * kTile * DH;
+    eoff = (static_cast<size_t>(page) * p.hkv + kvh) * kQ8GroupsPerPage + 4 * half;
     return ok ? min(kTile, S - kTile * tile) : 0;
   };
+  const int n_block = g0 < nb ? (nb - g0 + IW - 1) / IW : 0;  // the wave's block tiles
 
-  // two tiles in flight, the first of the prefix before the block's are worked on
-  Raw<DH> ta, tb;
-  int la = 0, lb = 0;
-  int i = g0 < nb ? (nb - g0 + IW - 1) / IW : 0;  // the wave's block tiles
-  if (i < n) la = load(i, ta);
-  if (has_block) {
-    block_tile<T, DH, NQ>(st, blk, p, b, kvh, g0, qf, row_pos, part[wave], ln, lg);
-    for (int k = 1; k < i; ++k) {
-      load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
-      block_tile<T, DH, NQ>(st, blk, p, b, kvh, g0 + IW * k, qf, row_pos, part[wave], ln, lg);
+  if constexpr (RW == 1) {
+    // Past the last tile the loads go to empty buffers: they are always issued, so that
+    // the compiler can count them, and waits for one tile leave the next under way.
+    auto load = [&](int i, Raw<DH> &t) {
+      size_t off, eoff;
+      const int visible = locate(i, off, eoff);
+      const int bytes = i < n ? kTile * DH : 0;
+      const auto rk = buffer_of(p.k_layer + off, bytes), rv = buffer_of(p.v_layer + off, bytes);
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+        t.k[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, lane_k, 256 * k, kNonTemporal));
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+        t.v[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, lane_v, 256 * k, kNonTemporal));
+      t.ke = __builtin_amdgcn_raw_buffer_load_b32(buffer_of(p.k_exp + eoff, bytes ? 4 : 0), 0, 0, kCached);
+      t.ve = __builtin_amdgcn_raw_buffer_load_b32(buffer_of(p.v_exp + eoff, bytes ? 4 : 0), 0, 0, kCached);
+      return visible;
+    };
+    // two tiles in flight, the first of the prefix before the block's are worked on
+    Raw<DH> ta, tb;
+    int i = n_block;
+    int la = load(i, ta);
+    if (has_block) {
+      block_tile<T, DH, NQ>(st, blk, p, b, kvh, g0, qf, row_pos, probs, ln, lg);
+      for (int k = 1; k < n_block; ++k) {
+        load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
+        block_tile<T, DH, NQ>(st, blk, p, b, kvh, g0 + IW * k, qf, row_pos, probs, ln, lg);
+      }
     }
-  }
-  if (i + 1 < n) lb = load(i + 1, tb);
-  for (; i < n; i += 2) {
-    prefix_tile<T, DH, NQ>(st, ta, qf, la, p.scale_log2, ln, lg);
-    if (i + 2 < n) la = load(i + 2, ta);
-    if (i + 1 >= n) break;
-    prefix_tile<T, DH, NQ>(st, tb, qf, lb, p.scale_log2, ln, lg);
-    if (i + 3 < n) lb = load(i + 3, tb);
+    int lb = load(i + 1, tb);
+    for (; i < n; i += 2) {
+      prefix_tile<T, DH, NQ>(st, ta, qf, la, p.scale_log2, ln, lg);
+      la = load(i + 2, ta);
+      if (i + 1 < n) prefix_tile<T, DH, NQ>(st, tb, qf, lb, p.scale_log2, ln, lg);
+      lb = load(i + 3, tb);
+    }
+  } else {
+    // Step s: every wave's s-th tile, all from the ring. A wave fetches its share of the
+    // tile that it works on with the other row waves (whole fragments, straight into LDS),
+    // and for itself the tile's exponents; one barrier a step publishes step s and frees
+    // the slot of step s - 1, which step s - 1 + NB takes. Reading tiles from the L2 once
+    // per row wave instead held 128 rows x 16384 tokens at 77 us of loads.
+    constexpr int NB = L::NB, LPW = (2 * KS + RW - 1) / RW;
+    const int steps = (g_end - chunk * p.chunk_tiles + IW - 1) / IW;  // of every wave
+    uint32_t visible = 0;  // of the last four issued steps, 8 bits each
+    auto issue = [&](int s) {
+      visible <<= 8;
+      if (s < n_block || s >= n) return;
+      size_t off, eoff;
+      visible |= locate(s, off, eoff);
+      const auto rk = buffer_of(p.k_layer + off, kTile * DH), rv = buffer_of(p.v_layer + off, kTile * DH);
+      uint8_t *slot = smem + ((s % NB) * IW + iw) * L::TILE;
+#pragma unroll
+      for (int c = 0; c < LPW; ++c) {
+        const int f = (rw * LPW + c) % (2 * KS);  // the last wave's may come twice
+        if (f < KS) dma16<kNonTemporal>(rk, lane_k, 256 * f, slot + f * kFragBytes);
+        else dma16<kNonTemporal>(rv, lane_v, 256 * (f - KS), slot + f * kFragBytes);
+      }
+      if (lane < 2)
+        __builtin_amdgcn_global_load_lds(
+            (__attribute__((address_space(1))) void *)(lane == 0 ? p.k_exp + eoff : p.v_exp + eoff),
+            (__attribute__((address_space(3))) void *)(smem + L::EXPS + ((s % NB) * kWavesQ8 + wave) * 8), 4, 0, 0);
+    };
+    // steps of block tiles need no ring: they are done while its first loads are under way
+    for (int s = 0; s < NB - 1; ++s) issue(s);
+    for (int s = 0; s < n_block; ++s) {
+      if (s > 0) load_block<T, DH>(blk, p, b, kvh, g0 + IW * s, ln, lg);
+      block_tile<T, DH, NQ>(st, blk, p, b, kvh, g0 + IW * s, qf, row_pos, probs, ln, lg);
+    }
+    for (int s = 0; s < steps; ++s) {
+      const bool mine = s >= n_block && s < n;
+      if (mine) wait_tiles<LPW + 1>(min(NB - 2, n - 1 - s));
+      __syncthreads();
+      issue(s + NB - 1);
+      if (mine) {
+        const uint8_t *slot = smem + ((s % NB) * IW + iw) * L::TILE + 16 * lane;
+        Raw<DH> t;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) t.k[k] = *reinterpret_cast<const u32x4 *>(slot + k * kFragBytes);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) t.v[k] = *reinterpret_cast<const u32x4 *>(slot + (KS + k) * kFragBytes);
+        const u32x2 e = *reinterpret_cast<const u32x2 *>(smem + L::EXPS + ((s % NB) * kWavesQ8 + wave) * 8);
+        t.ke = e[0];
+        t.ve = e[1];
+        prefix_tile<T, DH, NQ>(st, t, qf, visible >> (8 * (NB - 1)) & 255, p.scale_log2, ln, lg);
+      }
+    }
+    __syncthreads();  // the ring has been read
   }
 
   // From here on l and o are the plain ones, unnormalised, without shifts.
@@ -710,28 +793,31 @@ __global__ __launch_bounds__(256) void attn_q8_combine_kernel(AttnQ8Params p) {
     p.lse[(static_cast<size_t>(b) * p.hq + h) * p.w + pos] = (mx + log2f(den)) * 0.69314718055994530942f;
 }
 
-template <typename T, int DH, int NQ>
-hipError_t launch_tiles(const AttnQ8Params &p, int rw, hipStream_t s) {
-  const int gr = 16 * NQ * rw, n_rg = (p.rows + gr - 1) / gr;
-  const dim3 grid(static_cast<unsigned>(p.batch) * p.hkv * p.nsplit * n_rg), block(64 * kWavesQ8);
-  if (rw == 1) return launch_kernel(attn_q8_kernel<T, DH, NQ, 1>, grid, block, s, p, n_rg);
-  if (rw == 2) return launch_kernel(attn_q8_kernel<T, DH, NQ, 2>, grid, block, s, p, n_rg);
-  return launch_kernel(attn_q8_kernel<T, DH, NQ, 4>, grid, block, s, p, n_rg);
+template <typename T, int DH, int NQ, int RW>
+hipError_t launch_shape(const AttnQ8Params &p, hipStream_t s) {
+  constexpr int GR = 16 * NQ * RW;
+  const int n_rg = (p.rows + GR - 1) / GR;
+  const dim3 grid(static_cast<unsigned>(p.batch) * p.hkv * p.nsplit * n_rg);
+  return launch_kernel(attn_q8_kernel<T, DH, NQ, RW>, grid, dim3(64 * kWavesQ8), s, p, n_rg);
 }
 
 template <typename T, int DH>
 hipError_t launch_dh(const AttnQ8Params &p, hipStream_t s) {
   constexpr int ES = sizeof(T);
-  const int rw = q8_row_waves(p.rows, DH, ES);
-  hipError_t e;
+  const int nq = q8_row_tiles(p.rows, DH, ES), rw = q8_row_waves(p.rows, DH, ES);
+  hipError_t e = hipErrorInvalidValue;
+  if (nq == 1 && rw == 1) e = launch_shape<T, DH, 1, 1>(p, s);
   if constexpr (ES == 4 && DH == 128) {
-    e = launch_tiles<T, DH, 1>(p, rw, s);
-  } else {  // one row tile: no more than one wave has rows
-    e = q8_row_tiles(p.rows, DH, ES) == 1
-            ? launch_kernel(attn_q8_kernel<T, DH, 1, 1>,
-                            dim3(static_cast<unsigned>(p.batch) * p.hkv * p.nsplit),
-                            dim3(64 * kWavesQ8), s, p, 1)
-            : launch_tiles<T, DH, 2>(p, rw, s);
+    if (rw == 2) e = launch_shape<T, DH, 1, 2>(p, s);
+    if (rw == 4) e = launch_shape<T, DH, 1, 4>(p, s);
+  } else {
+    if (nq == 2 && rw == 1) e = launch_shape<T, DH, 2, 1>(p, s);
+    if constexpr (ES == 4 && DH == 96) {
+      if (rw == 4) e = launch_shape<T, DH, 1, 4>(p, s);
+    } else {
+      if (rw == 2) e = launch_shape<T, DH, 2, 2>(p, s);
+      if (rw == 4) e = launch_shape<T, DH, 2, 4>(p, s);
+    }
   }
   if (e != hipSuccess || p.nsplit == 1) return e;
   const dim3 merge(static_cast<unsigned>(p.batch) * p.hkv, (p.rows * (DH / 4) + 255) / 256);

@@ -67,8 +67,8 @@ das_status plan_attn(const das_cache_q8 *cache, const das_batch *b, int hq, int 
   const long long n_rg = (plan->rows + gr - 1) / gr;
   const long long units = static_cast<long long>(b->batch) * c->num_kv_heads;
   const long long tiles = 2LL * b->max_pages_per_seq + (w + 31) / 32;
-  // about four workgroups per compute unit, of at least 8 tiles
-  long long ns = std::max<long long>(1, 4 * kNumCUs / (units * n_rg));
+  // about two workgroups per compute unit, of at least 8 tiles
+  long long ns = std::max<long long>(1, 2 * kNumCUs / (units * n_rg));
   long long ct = std::max<long long>((tiles + ns - 1) / ns, 8);
   ns = (tiles + ct - 1) / ct;
   if (units * n_rg * ns * 256 > 0xffffffffLL) return DAS_ERR_SHAPE;

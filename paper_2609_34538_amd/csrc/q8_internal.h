@@ -38,10 +38,10 @@ struct AttnQ8Params {
 hipError_t launch_attn_q8(const AttnQ8Params &p, int dtype, int dh, hipStream_t s);
 
 // Launch shape of the attention kernel: 16-row tiles of a wave (two fp32 ones do not
-// fit its registers at head dim 128) and waves with different rows, and with them the
-// rows of a workgroup.
+// fit its registers at head dim 128, nor at 96 where waves share tiles) and waves with
+// different rows, and with them the rows of a workgroup.
 __host__ __device__ constexpr int q8_row_tiles(int rows, int dh, int es) {
-  return rows <= 16 || (es == 4 && dh == 128) ? 1 : 2;
+  return rows <= 16 || (es == 4 && (dh == 128 || (dh == 96 && rows > 32))) ? 1 : 2;
 }
 __host__ __device__ constexpr int q8_row_waves(int rows, int dh, int es) {
   return rows <= 16 * q8_row_tiles(rows, dh, es) ? 1 : rows <= 32 * q8_row_tiles(rows, dh, es) ? 2 : 4;
