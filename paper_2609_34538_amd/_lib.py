@@ -480,12 +480,13 @@ def greedy_accept(proposals: torch.Tensor, target_pred: torch.Tensor,
 # The 8-bit cache, the sampler and the page tables
 # ---------------------------------------------------------------------------
 def _check(t: torch.Tensor, dtype, shape, device, what: str):
-    """A tensor the call reads or writes: type, shape, layout and device."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    """The address of a tensor that the call reads or writes, of this type, shape (a
+    tuple), layout and device."""
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
     if t.device != device:
         raise ValueError(f"{what} must be on {device}")
-    return t.data_ptr()
+    raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
 
 
 def _check_opt(t: Optional[torch.Tensor], dtype, shape, device, what: str):
@@ -498,16 +499,20 @@ class _Call:
     tensors are kept alive."""
 
     def __init__(self, fn, name: str, args, keep, device: torch.device, stream):
-        if stream is not None and device.type == "cuda" and stream.device != device:
-            raise ValueError(f"the stream must be one of {device}")
-        self._fn, self._name, self._keep, self._device = fn, name, keep, device
-        if stream is None and device.type == "cuda":
-            stream = torch.cuda.current_stream(device)
-        self._args = (*args, 0 if stream is None else stream.cuda_stream)
+        self._fn, self._name, self._keep = fn, name, keep
+        self._index = device.index if device.type == "cuda" else None
+        handle = 0
+        if self._index is not None:
+            if stream is None:
+                stream = torch.cuda.current_stream(device)
+            elif stream.device != device:
+                raise ValueError(f"the stream must be one of {device}")
+            handle = stream.cuda_stream
+        self._args = (*args, handle)
 
     def __call__(self):
-        if self._device.type == "cuda" and torch.cuda.current_device() != self._device.index:
-            with torch.cuda.device(self._device):
+        if self._index is not None and torch.cuda.current_device() != self._index:
+            with torch.cuda.device(self._index):
                 st = self._fn(*self._args)
         else:
             st = self._fn(*self._args)
@@ -591,7 +596,8 @@ class QuantCache:
             b.v_plane[r] = self.v_plane.get(r, -1)
         b.k_pool, b.v_pool = k.data_ptr(), v.data_ptr()
         c.k_exp, c.v_exp = self.k_exp.data_ptr(), self.v_exp.data_ptr()
-        self._c = c
+        self._c, self._ref = c, ctypes.byref(c)
+        self._dev, self._hkv, self._dh = dev, hkv, dh
         return self
 
     @property
@@ -600,9 +606,8 @@ class QuantCache:
 
 
 def _check_batch_on(batch: Batch, device):
-    for t, what in ((batch.prefix_len, "prefix_len"), (batch.block_table, "block_table")):
-        if t.device != device:
-            raise ValueError(f"{what} must be on {device}")
+    if batch.prefix_len.device != device or batch.block_table.device != device:
+        raise ValueError(f"prefix_len and block_table must be on {device}")
     _check_opt(batch.dev_error, torch.int32, (1,), device, "dev_error")
 
 
@@ -628,17 +633,15 @@ class PreparedAttentionQ8(_Call):
                  workspace: torch.Tensor, lse: Optional[torch.Tensor] = None, stream=None):
         if q.dim() != 4:
             raise ValueError("q must be [B, w, Hq, dh]")
-        dev, (B, w, hq, dh) = cache.device, q.shape
-        blk = (batch.batch, w, cache.num_kv_heads, cache.head_dim)
-        q_shape = (batch.batch, w, hq, cache.head_dim)
+        dev, dtype, B, (_, w, hq, _) = cache._dev, cache.dtype, batch.batch, q.shape
+        blk, q_shape = (B, w, cache._hkv, cache._dh), (B, w, hq, cache._dh)
         _check_batch_on(batch, dev)
-        if workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
+        if (workspace.dtype is not torch.uint8 or workspace.device != dev
+                or not workspace.is_contiguous()):
             raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
-        args = (ctypes.byref(cache.c), ctypes.byref(batch.c), layer, kappa, nu, hq, w,
-                _check(q, cache.dtype, q_shape, dev, "q"),
-                _check(k_blk, cache.dtype, blk, dev, "k_blk"),
-                _check(v_blk, cache.dtype, blk, dev, "v_blk"),
-                _check(out, cache.dtype, q_shape, dev, "out"),
+        args = (cache._ref, ctypes.byref(batch.c), layer, kappa, nu, hq, w,
+                _check(q, dtype, q_shape, dev, "q"), _check(k_blk, dtype, blk, dev, "k_blk"),
+                _check(v_blk, dtype, blk, dev, "v_blk"), _check(out, dtype, q_shape, dev, "out"),
                 _check_opt(lse, torch.float32, (B, hq, w), dev, "lse"),
                 workspace.data_ptr(), workspace.numel())
         super().__init__(LIB.das_attn_q8, "das_attn_q8", args,

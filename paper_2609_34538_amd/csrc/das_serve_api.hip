@@ -54,7 +54,22 @@ struct PlanQ8 {
   size_t total;
 };
 
-// Cuts the units (sequence, KV head) of a call into chunks of equal length.
+// Cuts the units (sequence, KV head) of a call into chunks of equal length, one workgroup
+// each, by the table's width. A chunk costs its start (three dependent round trips) and a
+// record, and a second chunk of any unit the merge's launch, about 4 us in all, so
+// - few tiles are one chunk (55 heads x 700 tokens, 22 tiles: 7.8 us against 9.5 in three;
+//   fp32 tiles take several times the matrix-core time, and half as many of them),
+// - and so are units that fill three quarters of the compute units (4 x 55 heads x
+//   512-2048 tokens 15.6 against 19.7 us in two; 16 x 55 x 512-4096 77 against 84; 24 x 8
+//   x 1-4099, dh 128, 26.6 against 25.3-27.8);
+// - others are cut for a workgroup per CU, two for batches, whose lengths fill part of the
+//   table (16 x 8 x 512-8192, 258 tiles: 2 chunks 89, 4 to 8 66, 16 74 us; 30011 tokens x
+//   8: 20 to 30 chunks 17.5, 59 18.9), but for 16 tiles at least, 8 where there are few
+//   (8 x 4000 tokens, 126 tiles: 8 tiles 9.7 us, 4 10.5, 16 11.1).
+// - Waves with different rows share a chunk's tiles instead of taking them in turn: two
+//   workgroups per CU, which is what is resident (4 x 8 x 16384 x 128 rows: 33 tiles 71
+//   us, 20 91, 43 84), of 8 tiles at least, 4 with two such waves (96 rows, 81 tiles: 8
+//   26 us, 4 34; 64 rows, 127 tiles: 4 15.3, 8 16.6).
 das_status plan_attn(const das_cache_q8 *cache, const das_batch *b, int hq, int w, PlanQ8 *plan) {
   const das_cache *c = &cache->base;
   if (hq < 1 || hq % c->num_kv_heads != 0) return DAS_ERR_SHAPE;
@@ -67,9 +82,13 @@ das_status plan_attn(const das_cache_q8 *cache, const das_batch *b, int hq, int 
   const long long n_rg = (plan->rows + gr - 1) / gr;
   const long long units = static_cast<long long>(b->batch) * c->num_kv_heads;
   const long long tiles = 2LL * b->max_pages_per_seq + (w + 31) / 32;
-  // about two workgroups per compute unit, of at least 8 tiles
-  long long ns = std::max<long long>(1, 2 * kNumCUs / (units * n_rg));
-  long long ct = std::max<long long>((tiles + ns - 1) / ns, 8);
+  const int rw = q8_row_waves(plan->rows, c->head_dim, es);
+  const long long wgs = units * n_rg;  // of one chunk per unit
+  const bool one = rw == 1 && (tiles <= (es == 2 ? 32 : 16) || 4 * wgs >= 3 * kNumCUs);
+  const long long target = rw == 1 && b->batch == 1 ? kNumCUs : 2 * kNumCUs;
+  const long long least = rw == 1 ? (wgs * ((tiles + 7) / 8) <= kNumCUs ? 8 : 16) : rw == 2 ? 4 : 8;
+  long long ns = one ? 1 : std::max<long long>(1, target / wgs);
+  const long long ct = std::max<long long>((tiles + ns - 1) / ns, least);
   ns = (tiles + ct - 1) / ct;
   if (units * n_rg * ns * 256 > 0xffffffffLL) return DAS_ERR_SHAPE;
   plan->chunk_tiles = static_cast<int>(ct);

@@ -68,6 +68,47 @@ def test_matches_the_oracle(case):
     assert int(batch.dev_error) == 0
 
 
+RAGGED = [  # dtype, dh, hkv, group, w, lens: many units of unlike lengths
+    (BF16, 96, 55, 1, 16, [2000, 0, 1300, 4100, 64, 1]),
+    (BF16, 64, 40, 1, 20, [1500, 3000, 33]),
+    (BF16, 128, 16, 4, 1, [1, 4099, 700, 2048]),
+    (BF16, 128, 16, 4, 33, [3001, 100]),
+    (BF16, 96, 24, 8, 7, [500, 4000, 0]),
+    (BF16, 64, 16, 8, 40, [4000, 1111]),
+    (F32, 96, 30, 1, 9, [3500, 0, 129]),
+    (F32, 64, 40, 2, 12, [2600, 1000]),
+    (F32, 128, 16, 4, 11, [4000, 555]),
+    (F32, 128, 16, 7, 64, [3900]),
+]
+
+
+@pytest.mark.parametrize("case", RAGGED, ids=lambda c: f"{str(c[0])[6:]}-dh{c[1]}-h{c[2]}x{c[3]}-w{c[4]}-{c[5][0]}")
+def test_ragged_batches_match_the_oracle(case):
+    """Units of one chunk, of several and of the block only; a wider table; equal bits
+    again; and an unreadable page among them."""
+    dtype, dh, hkv, G, w, lens = case
+    B = len(lens)
+    cache, batch, table = random_cache(7, dtype, B, hkv, dh, lens, spread=1)
+    wide = torch.nn.functional.pad(batch.block_table, (0, 5), value=-1).contiguous()
+    batch = das.Batch(batch.prefix_len, wide, batch.dev_error)
+    q, kb, vb = _block(11, dtype, B, w, hkv * G, hkv, dh)
+    lse = torch.full((B, hkv * G, w), float("nan"), device=DEV)
+    out = das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb,
+                             out=torch.full_like(q, float("nan")), lse=lse)
+    _check(cache, batch, table, lens, q, kb, vb, out, lse)
+    assert int(batch.dev_error) == 0
+    assert torch.equal(out, das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb))
+    # an unreadable page of the longest sequence
+    b = int(np.argmax(lens))
+    wide[b, 2] = -7
+    keep = np.arange(lens[b]) // 64 != 2
+    out = das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb)
+    assert int(batch.dev_error) == das.DEVERR_PAGE
+    ref, _, a, size = attention(HostCache(cache), table, lens, b, 0, 0, 0, q, kb, vb, keep=keep)
+    tol = tolerance(dtype, ref, a, size, lens[b] + w, dh)
+    assert (np.abs(out[b].double().cpu().numpy() - ref) <= tol).all()
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_plane_layer_and_policy(dtype):
     """Keys of depth 2 and values of depth 3 at layer 1 are the ones that are read."""
