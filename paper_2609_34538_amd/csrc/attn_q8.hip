@@ -160,7 +160,7 @@ __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w 
 
 // A tile of the prefix through both products. `limit`: visible tokens.
 template <typename T, int DH, int NQ>
-__device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, const Raw<DH> &t,
+__device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, Raw<DH> &t,
                                             const QFrag<T, DH> (&qf)[NQ], int limit, float scale,
                                             int ln, int lg) {
   const bool full = limit >= kTile;
@@ -203,7 +203,19 @@ __device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, const Raw<DH> &t,
   for (int qt = 0; qt < NQ; ++qt) none[qt] = 0x7fffffff;
   softmax_step<DH, NQ>(st, s, none, limit, full, scale, sizeof(T) == 2 ? kProbShift : 0.f, lg);
 
-  const uint32_t vexp = __builtin_amdgcn_ubfe(t.ve, 8 * lg, 8);
+  uint32_t vexp = __builtin_amdgcn_ubfe(t.ve, 8 * lg, 8);
+  if (!full) {
+    // Invisible tokens enter with probability 0; their codes are cleared, and the exponent
+    // of a group without visible ones too, so that whatever the page holds adds nothing.
+    // On the codes and in a branch: masks on the converted values took 32 of the 235 vector
+    // instructions of every tile.
+    const int seen = min(max(limit - 8 * lg, 0), 8);
+    const uint32_t lo = seen >= 4 ? ~0u : (1u << 8 * seen) - 1;
+    const uint32_t hi = seen >= 8 ? ~0u : seen <= 4 ? 0u : (1u << 8 * (seen - 4)) - 1;
+#pragma unroll
+    for (int k = 0; k < DH / 32; ++k) t.v[k] &= u32x4{lo, hi, lo, hi};
+    if (seen == 0) vexp = 1;
+  }
   if constexpr (sizeof(T) == 2) {
     // the largest exponent of the groups with a visible token, as a wave-uniform value
     uint32_t w = __builtin_amdgcn_readfirstlane(t.ve);
@@ -226,16 +238,11 @@ __device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, const Raw<DH> &t,
     for (int qt = 0; qt < NQ; ++qt)
       pf[qt] = u32x4{pack_f16(s[qt][0][0], s[qt][0][1]), pack_f16(s[qt][0][2], s[qt][0][3]),
                      pack_f16(s[qt][1][0], s[qt][1][1]), pack_f16(s[qt][1][2], s[qt][1][3])};
-    // invisible tokens enter with probability 0; their values are zeroed so that
-    // whatever the page holds there adds nothing
-    u32x4 keep = {~0u, ~0u, ~0u, ~0u};
-    if (!full) keep = value_mask<bf16_t>(limit, lg);
 #pragma unroll
     for (int k = 0; k < DH / 32; ++k)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        u32x4 a = codes_to_f16(t.v[k][2 * i], t.v[k][2 * i + 1], vs);
-        if (!full) a &= keep;
+        const u32x4 a = codes_to_f16(t.v[k][2 * i], t.v[k][2 * i + 1], vs);
 #pragma unroll
         for (int qt = 0; qt < NQ; ++qt) st.o[qt][2 * k + i] = mfma_f16(a, pf[qt], st.o[qt][2 * k + i]);
       }
@@ -249,7 +256,6 @@ __device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, const Raw<DH> &t,
         codes_to_f32(t.v[k][2 * i], t.v[k][2 * i + 1], vs, a);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          if (!full) a[j] = 8 * lg + j < limit ? a[j] : 0.f;
 #pragma unroll
           for (int qt = 0; qt < NQ; ++qt)
             st.o[qt][2 * k + i] = mfma16x16x4(__float_as_uint(a[j]), __float_as_uint(s[qt][j / 4][j % 4]),
@@ -442,6 +448,64 @@ __device__ __forceinline__ void block_tile(Acc<DH, NQ> &st, Block<T, DH> &t, con
   }
 }
 
+// Eight neighbouring results of a lane: tiles 2 k and 2 k + 1 hold dims 32 k + 8 g + 2 v and + 1.
+template <int DH>
+__device__ __forceinline__ void eight(const f32x4 (&o)[DH / 16], int k, float scale, f32x4 &lo, f32x4 &hi) {
+  const f32x4 x = o[2 * k] * scale, y = o[2 * k + 1] * scale;
+  lo = f32x4{x[0], y[0], x[1], y[1]};
+  hi = f32x4{x[2], y[2], x[3], y[3]};
+}
+// A row's record (write_piece_row's form) and its output, by its four lanes.
+template <typename T, int DH>
+__device__ __forceinline__ void write_record_row(uint8_t *rec, int rows, int row, int lg,
+                                                 const f32x4 (&o)[DH / 16], float m, float l) {
+  float q = 1.f, sc = 1.f;
+  if constexpr (sizeof(T) == 2) {
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    float amax = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DH / 16; ++dt)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) amax = fmaxf(amax, fabsf(o[dt][v]));
+    amax = group_max(amax) * inv;
+    const int e = (amax > 0.f && amax < __builtin_huge_valf()) ? __builtin_amdgcn_frexp_expf(amax) - 15 : 0;
+    sc = __builtin_amdgcn_ldexpf(inv, -e);
+    q = __builtin_amdgcn_ldexpf(l, e);
+  }
+#pragma unroll
+  for (int k = 0; k < DH / 32; ++k) {
+    f32x4 lo, hi;
+    eight<DH>(o, k, sc, lo, hi);
+    uint8_t *dst = rec + (static_cast<size_t>(row) * DH + 32 * k + 8 * lg) * rec_elem_bytes(sizeof(T));
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<u32x4 *>(dst) =
+          u32x4{pack_f16(lo[0], lo[1]), pack_f16(lo[2], lo[3]), pack_f16(hi[0], hi[1]), pack_f16(hi[2], hi[3])};
+    } else {
+      reinterpret_cast<f32x4 *>(dst)[0] = lo;
+      reinterpret_cast<f32x4 *>(dst)[1] = hi;
+    }
+  }
+  if (lg == 0)
+    *reinterpret_cast<f32x4 *>(rec + static_cast<size_t>(rows) * DH * rec_elem_bytes(sizeof(T)) + row * 16) =
+        f32x4{m, l, q, 0.f};
+}
+template <typename T, int DH>
+__device__ __forceinline__ void write_output_row(const AttnQ8Params &p, int b, int kvh, int row, int lg,
+                                                 const f32x4 (&o)[DH / 16], float m, float l) {
+  const int pos = row / p.group, h = kvh * p.group + row % p.group;
+  T *out = static_cast<T *>(p.out) + ((static_cast<size_t>(b) * p.w + pos) * p.hq + h) * DH;
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int k = 0; k < DH / 32; ++k) {
+    f32x4 lo, hi;
+    eight<DH>(o, k, inv, lo, hi);
+    store_out4(out + 32 * k + 8 * lg, lo);
+    store_out4(out + 32 * k + 8 * lg + 4, hi);
+  }
+  if (lg == 0 && p.lse)
+    p.lse[(static_cast<size_t>(b) * p.hq + h) * p.w + pos] = (m + log2f(l)) * 0.69314718055994530942f;
+}
+
 // Shared memory of a workgroup. RW > 1: the tiles that waves with different rows share, a
 // ring of NB steps of IW tiles, their exponents per wave, and room for a block tile's
 // probabilities; afterwards the merge area of one row tile. RW == 1: the merge area, before
@@ -449,11 +513,12 @@ __device__ __forceinline__ void block_tile(Acc<DH, NQ> &st, Block<T, DH> &t, con
 template <int DH, int NQ, int RW>
 struct Lds {
   static constexpr int IW = kWavesQ8 / RW;             // waves that share a chunk's tiles
-  static constexpr int NB = RW == 1 ? 0 : RW == 2 ? 3 : 4;
+  static constexpr int TPS = RW == 4 ? 2 : 1;          // tiles of a wave and step
+  static constexpr int NB = RW == 1 ? 0 : 3;           // steps of the ring
   static constexpr int TILE = 2 * kTile * DH;          // bytes of a tile
   static constexpr int RS = DH + 4;                    // row stride of the merge area (floats)
-  static constexpr int EXPS = NB * IW * TILE;
-  static constexpr int PROBS = EXPS + NB * kWavesQ8 * 8;
+  static constexpr int EXPS = NB * IW * TPS * TILE;
+  static constexpr int PROBS = EXPS + NB * TPS * kWavesQ8 * 8;
   static constexpr int PROB_STRIDE = RW == 1 ? 16 * RS * 4 : 16 * NQ * kTile * 4;
   static constexpr int MERGE = kWavesQ8 * 16 * RS * 4;
   static constexpr int BYTES = PROBS + kWavesQ8 * PROB_STRIDE > MERGE ? PROBS + kWavesQ8 * PROB_STRIDE : MERGE;
@@ -596,26 +661,30 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     // and for itself the tile's exponents; one barrier a step publishes step s and frees
     // the slot of step s - 1, which step s - 1 + NB takes. Reading tiles from the L2 once
     // per row wave instead held 128 rows x 16384 tokens at 77 us of loads.
-    constexpr int NB = L::NB, LPW = (2 * KS + RW - 1) / RW;
-    const int steps = (g_end - chunk * p.chunk_tiles + IW - 1) / IW;  // of every wave
-    uint32_t visible = 0;  // of the last four issued steps, 8 bits each
+    constexpr int NB = L::NB, TPS = L::TPS, LPW = (2 * KS + RW - 1) / RW;
+    const int steps = (g_end - chunk * p.chunk_tiles + IW * TPS - 1) / (IW * TPS);  // of every wave
+    uint64_t visible = 0;  // of the tiles of the last NB issued steps, 8 bits each
     auto issue = [&](int s) {
-      visible <<= 8;
-      if (s < n_block || s >= n) return;
-      size_t off, eoff;
-      visible |= locate(s, off, eoff);
-      const auto rk = buffer_of(p.k_layer + off, kTile * DH), rv = buffer_of(p.v_layer + off, kTile * DH);
-      uint8_t *slot = smem + ((s % NB) * IW + iw) * L::TILE;
 #pragma unroll
-      for (int c = 0; c < LPW; ++c) {
-        const int f = (rw * LPW + c) % (2 * KS);  // the last wave's may come twice
-        if (f < KS) dma16<kNonTemporal>(rk, lane_k, 256 * f, slot + f * kFragBytes);
-        else dma16<kNonTemporal>(rv, lane_v, 256 * (f - KS), slot + f * kFragBytes);
+      for (int t = 0; t < TPS; ++t) {
+        const int i = TPS * s + t, at = (s % NB) * TPS + t;
+        visible <<= 8;
+        if (i < n_block || i >= n) continue;
+        size_t off, eoff;
+        visible |= locate(i, off, eoff);
+        const auto rk = buffer_of(p.k_layer + off, kTile * DH), rv = buffer_of(p.v_layer + off, kTile * DH);
+        uint8_t *slot = smem + (at * IW + iw) * L::TILE;
+#pragma unroll
+        for (int c = 0; c < LPW; ++c) {
+          const int f = (rw * LPW + c) % (2 * KS);  // the last wave's may come twice
+          if (f < KS) dma16<kNonTemporal>(rk, lane_k, 256 * f, slot + f * kFragBytes);
+          else dma16<kNonTemporal>(rv, lane_v, 256 * (f - KS), slot + f * kFragBytes);
+        }
+        if (lane < 2)
+          __builtin_amdgcn_global_load_lds(
+              (__attribute__((address_space(1))) void *)(lane == 0 ? p.k_exp + eoff : p.v_exp + eoff),
+              (__attribute__((address_space(3))) void *)(smem + L::EXPS + (at * kWavesQ8 + wave) * 8), 4, 0, 0);
       }
-      if (lane < 2)
-        __builtin_amdgcn_global_load_lds(
-            (__attribute__((address_space(1))) void *)(lane == 0 ? p.k_exp + eoff : p.v_exp + eoff),
-            (__attribute__((address_space(3))) void *)(smem + L::EXPS + ((s % NB) * kWavesQ8 + wave) * 8), 4, 0, 0);
     };
     // steps of block tiles need no ring: they are done while its first loads are under way
     for (int s = 0; s < NB - 1; ++s) issue(s);
@@ -623,22 +692,26 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
       if (s > 0) load_block<T, DH>(blk, p, b, kvh, g0 + IW * s, ln, lg);
       block_tile<T, DH, NQ>(st, blk, p, b, kvh, g0 + IW * s, qf, row_pos, probs, ln, lg);
     }
+#pragma unroll 1
     for (int s = 0; s < steps; ++s) {
-      const bool mine = s >= n_block && s < n;
-      if (mine) wait_tiles<LPW + 1>(min(NB - 2, n - 1 - s));
+      // tiles that may still be under way: those of the later steps
+      wait_tiles<LPW + 1>(min(n, TPS * (s + NB - 1)) - TPS * (s + 1));
       __syncthreads();
       issue(s + NB - 1);
-      if (mine) {
-        const uint8_t *slot = smem + ((s % NB) * IW + iw) * L::TILE + 16 * lane;
-        Raw<DH> t;
 #pragma unroll
-        for (int k = 0; k < KS; ++k) t.k[k] = *reinterpret_cast<const u32x4 *>(slot + k * kFragBytes);
+      for (int t = 0; t < TPS; ++t) {
+        const int i = TPS * s + t, at = (s % NB) * TPS + t;
+        if (i < n_block || i >= n) continue;
+        const uint8_t *slot = smem + (at * IW + iw) * L::TILE + 16 * lane;
+        Raw<DH> x;
 #pragma unroll
-        for (int k = 0; k < KS; ++k) t.v[k] = *reinterpret_cast<const u32x4 *>(slot + (KS + k) * kFragBytes);
-        const u32x2 e = *reinterpret_cast<const u32x2 *>(smem + L::EXPS + ((s % NB) * kWavesQ8 + wave) * 8);
-        t.ke = e[0];
-        t.ve = e[1];
-        prefix_tile<T, DH, NQ>(st, t, qf, visible >> (8 * (NB - 1)) & 255, p.scale_log2, ln, lg);
+        for (int k = 0; k < KS; ++k) x.k[k] = *reinterpret_cast<const u32x4 *>(slot + k * kFragBytes);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) x.v[k] = *reinterpret_cast<const u32x4 *>(slot + (KS + k) * kFragBytes);
+        const u32x2 e = *reinterpret_cast<const u32x2 *>(smem + L::EXPS + (at * kWavesQ8 + wave) * 8);
+        x.ke = e[0];
+        x.ve = e[1];
+        prefix_tile<T, DH, NQ>(st, x, qf, static_cast<int>(visible >> (8 * (TPS * NB - 1 - t)) & 255), p.scale_log2, ln, lg);
       }
     }
     __syncthreads();  // the ring has been read
@@ -662,6 +735,16 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     }
   }
   uint8_t *rec = p.ws + (static_cast<size_t>(unit) * p.nsplit + chunk) * p.piece_stride;
+  if constexpr (IW == 1) {  // a row's result is one wave's
+#pragma unroll
+    for (int qt = 0; qt < NQ; ++qt) {
+      const int row = row0 + 16 * qt + ln;
+      if (row >= p.rows) continue;  // a row's four lanes together
+      if (nsb > 1) write_record_row<T, DH>(rec, p.rows, row, lg, st.o[qt], m[qt], st.l[qt]);
+      else write_output_row<T, DH>(p, b, kvh, row, lg, st.o[qt], m[qt], st.l[qt]);
+    }
+    return;
+  }
   // Merge of the waves' results: every row's maxima and sums first, then, one
   // 16-row tile at a time, the outputs scaled to the common maximum.
 #pragma unroll
