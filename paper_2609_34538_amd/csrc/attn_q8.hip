@@ -507,8 +507,8 @@ __device__ __forceinline__ void write_output_row(const AttnQ8Params &p, int b, i
 }
 
 // Shared memory of a workgroup. RW > 1: the tiles that waves with different rows share, a
-// ring of NB steps of IW tiles, their exponents per wave, and room for a block tile's
-// probabilities; afterwards the merge area of one row tile. RW == 1: the merge area, before
+// ring of NB steps of IW * TPS tiles, their exponents per wave, and room for a block tile's
+// probabilities; afterwards, with IW > 1, the merge area of one row tile. RW == 1: the merge area, before
 // that the probabilities.
 template <int DH, int NQ, int RW>
 struct Lds {
@@ -677,8 +677,8 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
 #pragma unroll
         for (int c = 0; c < LPW; ++c) {
           const int f = (rw * LPW + c) % (2 * KS);  // the last wave's may come twice
-          if (f < KS) dma16<kNonTemporal>(rk, lane_k, 256 * f, slot + f * kFragBytes);
-          else dma16<kNonTemporal>(rv, lane_v, 256 * (f - KS), slot + f * kFragBytes);
+          const bool key = f < KS;
+          dma16<kNonTemporal>(key ? rk : rv, key ? lane_k : lane_v, 256 * (key ? f : f - KS), slot + f * kFragBytes);
         }
         if (lane < 2)
           __builtin_amdgcn_global_load_lds(

@@ -111,6 +111,23 @@ def test_outliers(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kept", [1, 511, 512, 513])
+def test_kept_tokens_around_the_bound_of_a_list(dtype, kept):
+    """`kept` tokens far above the rest, by each filter and by two of them; with distinct
+    logits, and with equal ones that make a list overflow where top-k alone would not.
+    Logits of 200 and more leave the range in which bf16 rows are counted by value."""
+    z, u = _logits(7, 6, 2, 9000, dtype)
+    g = torch.Generator(device=DEV).manual_seed(8)
+    at = torch.randperm(9000, generator=g, device=DEV)[:kept]
+    z[:, :, at] = (212 + torch.rand((6, 2, kept), generator=g, device=DEV)).to(dtype)
+    z[3:, :, at] = 210.0
+    f = dict(T=[1.0, 0.8, 1.2] * 2, k=[kept, 0, min(kept, 300)] * 2, p=[1.0, 0.9, 0.7] * 2, low=[0.0, 0.0, 0.01] * 2)
+    check(z, u, **f)
+    check(z, u, low=[1e-4, 0.5, 1.0] * 2)
+    check(z, u, p=[0.99, 0.5, 1e-6] * 2, low=[0.2, 0.0, 0.9] * 2)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_infinities_and_nan(dtype):
     z, u = _logits(3, 6, 1, 3001, dtype)
     z[0, 0, ::2] = float("nan")
