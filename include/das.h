@@ -382,7 +382,8 @@ typedef struct das_cache_q8 {
  * Numerics: elements are exact in the products' types. bf16 calls multiply values
  * in fp16 with probabilities of 11 bits; a group's values below 2^-24 of the largest
  * scale's unit met so far round there. fp32 calls multiply in fp32. Accumulation and
- * softmax statistics are fp32. lse as for das_attn_policy.
+ * softmax statistics are fp32; sums are divided last, so that values whose sum over
+ * the positions passes the largest fp32 give infinities. lse as for das_attn_policy.
  *
  * das_attn_q8_workspace_bytes returns 0 for arguments that das_attn_q8 rejects; the
  * workspace is 256-byte aligned, needs no init, and calls that run concurrently need

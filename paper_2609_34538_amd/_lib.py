@@ -493,6 +493,15 @@ def _check_opt(t: Optional[torch.Tensor], dtype, shape, device, what: str):
     return None if t is None else _check(t, dtype, shape, device, what)
 
 
+def _empty_on(stream, shape, dtype, device) -> torch.Tensor:
+    """Memory for a call on `stream`, from that stream's pool: what is freed while the call
+    is under way may be given out again at once, but only to later work of the same stream."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 class _Call:
     """A library call with its arguments marshalled: calling it enqueues it on `stream`
     (None: the current stream of the tensors' device) with that device current. The
@@ -511,7 +520,9 @@ class _Call:
         self._args = (*args, handle)
 
     def __call__(self):
-        if self._index is not None and torch.cuda.current_device() != self._index:
+        if self._index is None:
+            raise ValueError(f"{self._name} takes tensors on a GPU")
+        if torch.cuda.current_device() != self._index:
             with torch.cuda.device(self._index):
                 st = self._fn(*self._args)
         else:
@@ -616,12 +627,12 @@ def workspace_bytes_q8(cache: QuantCache, batch: Batch, num_q_heads: int, block_
                                            num_q_heads, block_len)
 
 
-def alloc_workspace_q8(cache: QuantCache, batch: Batch, num_q_heads: int,
-                       block_len: int) -> torch.Tensor:
+def alloc_workspace_q8(cache: QuantCache, batch: Batch, num_q_heads: int, block_len: int,
+                       stream=None) -> torch.Tensor:
     n = workspace_bytes_q8(cache, batch, num_q_heads, block_len)
     if n == 0:
         raise DasError(-2, "workspace query rejected the shapes")
-    return torch.empty(n, dtype=torch.uint8, device=cache.device)
+    return _empty_on(stream, n, torch.uint8, cache.device)
 
 
 class PreparedAttentionQ8(_Call):
@@ -654,9 +665,9 @@ def attn_policy_q8(cache: QuantCache, batch: Batch, layer: int, kappa: int, nu: 
                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Eq. (2)-(3) over an 8-bit cache: prefix keys at depth kappa, values at depth nu."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty_on(stream, q.shape, q.dtype, q.device)
     if workspace is None:
-        workspace = alloc_workspace_q8(cache, batch, q.shape[2], q.shape[1])
+        workspace = alloc_workspace_q8(cache, batch, q.shape[2], q.shape[1], stream)
     PreparedAttentionQ8(cache, batch, layer, kappa, nu, q, k_blk, v_blk, out, workspace, lse,
                         stream)()
     return out
@@ -706,7 +717,7 @@ class PreparedSample(_Call):
                 B > 1 and w > 1 and logits.stride(0) != w * stride):
             raise ValueError("logits must have contiguous rows at one even distance")
         if tokens is None:
-            tokens = torch.empty((B, w), dtype=torch.int32, device=dev)
+            tokens = _empty_on(stream, (B, w), torch.int32, dev)
         self.tokens, self.probs = tokens, probs
         f32 = torch.float32
         args = (B, w, V, DTYPE_CODES[logits.dtype], logits.data_ptr(), stride,

@@ -182,6 +182,8 @@ das_status das_kv_append_q8(const das_cache_q8 *cache, const das_batch *batch, c
   // the grid: one wave per (plane, layer, KV head), four per workgroup, keys and
   // values in separate workgroups; at most 2^32 - 1 work-items along x
   const long long per_plane = static_cast<long long>(c->num_layers) * c->num_kv_heads;
+  constexpr long long kMost = 1 << 26;  // units that such a grid holds; the products fit 64 bits
+  if (per_plane > kMost || c->num_k_planes > kMost || c->num_v_planes > kMost) return DAS_ERR_SHAPE;
   const long long blocks =
       (c->num_k_planes * per_plane + 3) / 4 + (c->num_v_planes * per_plane + 3) / 4;
   if (blocks * 256 > 0xffffffffLL) return DAS_ERR_SHAPE;

@@ -164,9 +164,8 @@ def attention(host: HostCache, table, lens, b, layer, kplane, vplane, q, kb, vb,
     a, _ = orc.policy_attention(f(q), k, np.abs(v), f(kb), np.abs(f(vb)))
     dh, G = q.shape[-1], q.shape[2] // kb.shape[2]
     kk = np.abs(np.concatenate([k, f(kb)]))            # [S + w, Hkv, dh]
-    size = np.einsum("wgd,sgd->wg", np.abs(f(q))[:, ::G], kk[:0]) if not len(kk) else max(
-        float((np.abs(f(q)) @ kk[:, h].T)[:, h * G:(h + 1) * G].max()) for h in range(kb.shape[2]))
-    return o, lse, a, float(size) / np.sqrt(dh)
+    size = max(float((np.abs(f(q)) @ kk[:, h].T)[:, h * G:(h + 1) * G].max()) for h in range(kb.shape[2]))
+    return o, lse, a, size / np.sqrt(dh)
 
 
 def tolerance(dtype, ref, a, size, n, dh):

@@ -22,7 +22,7 @@ def _new(seed, cache, B, w, scale=1.0):
             for n in (cache.k_pool.shape[0], cache.v_pool.shape[0])]
 
 
-def _assert_same(cache, host, nan_sign=True):
+def _assert_same(cache, host):
     got = HostCache(cache)
     for s in "kv":
         assert np.array_equal(got.exp[s], host.exp[s]), f"{s} exponents"

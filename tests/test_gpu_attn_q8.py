@@ -261,3 +261,25 @@ def test_repeats_streams_and_graphs_agree():
             g.replay()
             torch.cuda.synchronize()
             assert torch.equal(o, w), rep
+
+
+def test_a_given_stream_owns_the_workspace_of_its_call():
+    """The workspace that a call allocates is free again when the call returns, while its
+    kernels wait on their stream: tensors that the current stream then fills must not take it."""
+    lens = [8000, 5000]
+    cache, batch, table = random_cache(8, BF16, 2, 2, 128, lens)
+    x = _block(3, BF16, 2, 8, 4, 2, 128)
+    want = das.attn_policy_q8(cache, batch, 0, 1, 1, *x)
+    n = das.workspace_bytes_q8(cache, batch, 4, 8)
+    assert n > 1 << 12
+    side, busy = torch.cuda.Stream(), torch.ones((4096, 4096), device=DEV)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                busy @ busy
+        out = das.attn_policy_q8(cache, batch, 0, 1, 1, *x, stream=side)
+        fill = [torch.full((n,), 255, dtype=torch.uint8, device=DEV) for _ in range(8)]
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        del fill

@@ -99,6 +99,13 @@ def test_append_refusals(args, status):
     assert LIB.das_kv_append_q8(ctypes.byref(_cache()), ctypes.byref(_batch()), *args, None) == status
 
 
+@pytest.mark.parametrize("kw", [dict(num_layers=1 << 30), dict(num_k_planes=1 << 30), dict(num_v_planes=1 << 25),
+                                dict(num_layers=2 ** 31 - 1, num_kv_heads=65535, num_k_planes=2 ** 31 - 1)])
+def test_append_refuses_grids_that_are_too_large(kw):
+    args = FAKE, FAKE, 8, FAKE, None, None
+    assert LIB.das_kv_append_q8(ctypes.byref(_cache(**kw)), ctypes.byref(_batch()), *args) == SHAPE
+
+
 def test_workspace_grows_with_the_call():
     c, b = _cache(), _batch(max_pages_per_seq=400)
     n = lambda hq, w: LIB.das_attn_q8_workspace_bytes(ctypes.byref(c), ctypes.byref(b), hq, w)  # noqa: E731
@@ -203,3 +210,15 @@ def test_binding_checks_of_the_pages():
                dict(free_pages=torch.zeros((3, 3), **i32)), dict(dev_error=torch.zeros(1))):
         with pytest.raises(ValueError):
             das.pages_update(**{**good, **kw})
+
+
+def test_the_binding_refuses_tensors_in_host_memory():
+    cache, batch, q, kb = _tensors()
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32)  # noqa: E731
+    new = torch.zeros((2, 2, 3, 4, 2, 64), dtype=torch.bfloat16)
+    for call in (lambda: das.attn_policy_q8(cache, batch, 0, 1, 2, q, kb, kb),
+                 lambda: das.kv_append_q8(cache, batch, new, new[:1], i32(3)),
+                 lambda: das.sample(torch.zeros((2, 3, 50)), torch.zeros((2, 3))),
+                 lambda: das.pages_update(i32(3), i32(3, 4), i32(3), i32(9), i32(1))):
+        with pytest.raises(ValueError, match="on a GPU"):
+            call()
