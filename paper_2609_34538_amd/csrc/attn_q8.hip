@@ -6,7 +6,14 @@
 // waves each. RW of the waves hold different query rows (16 * NQ each), the other
 // 4 / RW take a chunk's tiles in turn, each with its own running maximum, sum and
 // output; they merge through LDS, and where a unit has several chunks these leave
-// records that a second kernel merges.
+// records that a second kernel merges. Up to 16 * NQ rows a wave has tiles of its own,
+// from memory into registers, two on the way; waves that share a tile get it from LDS.
+//
+// Bound by HBM for few rows (24 x 8 KV heads x 1-4099 tokens, one query token, dh 128:
+// 26 us, 3.8 TB/s; 32 x 55 heads x 32 rows, dh 96, 2.1 GB: 358 us, 5.9 TB/s, what a copy
+// reaches), for many by the vector and matrix work of a tile, which two waves per SIMD do
+// not overlap wholly (4 x 8 KV heads x 128 rows, dh 128, 137 MB: 59 us, 580 TFLOP/s; 31
+// matrix instructions and 170 vector ones a tile and wave).
 //
 // Both products take the key / value tile as the A operand, as in mfma_tile.h:
 //   S^T (tokens x rows) = K . Q^T,   O^T (dh x rows) += V^T . P^T
@@ -104,29 +111,37 @@ struct QFrag {
 // become probabilities in place, the lane's share of the sum is added. The reference
 // (the same in a row's four lanes) moves to the row's maximum only when a logit passes it
 // by more than kSlack, which after the first tiles is rare: most tiles need no reduction
-// over lanes and no rescaling (128 rows x 16384 tokens 94 -> 89 us).
-template <int DH, int NQ>
-__device__ __forceinline__ void softmax_step(Acc<DH, NQ> &st, f32x4 (&s)[NQ][2],
-                                             const int (&cap)[NQ], int limit, bool full, float scale,
-                                             float shift, int lg) {
+// over lanes and no rescaling. E / 2 tiles at once; BLOCK: a row sees tokens up to its cap.
+template <int DH, int NQ, int E, bool BLOCK>
+__device__ __forceinline__ void softmax_step(Acc<DH, NQ> &st, f32x4 (&s)[NQ][E], const int (&cap)[NQ],
+                                             const int (&limit)[E / 2], float scale, float shift, int lg) {
+  bool full = !BLOCK;
+#pragma unroll
+  for (int j = 0; j < E / 2; ++j) full = full && limit[j] >= kTile;
+  float mx[NQ];
+  bool moves = false;
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) {
     if (!full) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int e = 0; e < E; ++e)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const int t = 8 * lg + 4 * e + v;
-          s[qt][e][v] = ((t < limit) & (t <= cap[qt])) ? s[qt][e][v] : kNegInf;
+          const int t = 8 * lg + 4 * (e % 2) + v;
+          s[qt][e][v] = ((t < limit[e / 2]) & (!BLOCK | (t <= cap[qt]))) ? s[qt][e][v] : kNegInf;
         }
     }
-    float mx = kNegInf;
+    mx[qt] = kNegInf;
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
+    for (int e = 0; e < E; ++e)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) mx = fmaxf(mx, s[qt][e][v]);
-    if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(mx, scale, st.neg[qt]) > shift + kSlack) != 0) {
-      const float m = group_max(mx) * scale;
+      for (int v = 0; v < 4; ++v) mx[qt] = fmaxf(mx[qt], s[qt][e][v]);
+    moves |= __builtin_fmaf(mx[qt], scale, st.neg[qt]) > shift + kSlack;
+  }
+  if (__builtin_amdgcn_ballot_w64(moves) != 0) {
+#pragma unroll
+    for (int qt = 0; qt < NQ; ++qt) {
+      const float m = group_max(mx[qt]) * scale;
       // rows with nothing visible, and those that stay within their slack, keep theirs
       const float neg = m + st.neg[qt] > shift + kSlack ? shift - m : st.neg[qt];
       const float alpha = __builtin_amdgcn_exp2f(neg - st.neg[qt]);  // 0 from kNoRef
@@ -136,15 +151,17 @@ __device__ __forceinline__ void softmax_step(Acc<DH, NQ> &st, f32x4 (&s)[NQ][2],
 #pragma unroll
       for (int dt = 0; dt < DH / 16; ++dt) st.o[qt][dt] *= alpha;
     }
+  }
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
+  for (int qt = 0; qt < NQ; ++qt)
+#pragma unroll
+    for (int e = 0; e < E; ++e)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][e][v], scale, st.neg[qt]));
         s[qt][e][v] = p;
         st.l[qt] += p;
       }
-  }
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
@@ -158,6 +175,42 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
+// Codes of a tile's values with those of invisible tokens cleared, and the exponent byte
+// of their group, 1 where none of it is visible: whatever the page holds there adds nothing.
+// On the codes and in a branch: masks on the converted values took 32 of the 235 vector
+// instructions of every tile.
+template <int N>
+__device__ __forceinline__ void clear_invisible(u32x4 (&v)[N], uint32_t &vexp, int limit, int lg) {
+  const int seen = min(max(limit - 8 * lg, 0), 8);
+  const uint32_t lo = seen >= 4 ? ~0u : (1u << 8 * seen) - 1;
+  const uint32_t hi = seen >= 8 ? ~0u : seen <= 4 ? 0u : (1u << 8 * (seen - 4)) - 1;
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] &= u32x4{lo, hi, lo, hi};
+  if (seen == 0) vexp = 1;
+}
+// The largest exponent of the groups with a visible token, as a wave-uniform value.
+__device__ __forceinline__ int most_exponent(uint32_t ve, int limit) {
+  uint32_t w = __builtin_amdgcn_readfirstlane(ve);
+  if (limit < kTile) w &= limit > 24 ? ~0u : limit > 16 ? 0xffffffu : limit > 8 ? 0xffffu : limit > 0 ? 0xffu : 0u;
+  return max(max(static_cast<int>(w & 255), static_cast<int>(w >> 8 & 255)),
+             max(static_cast<int>(w >> 16 & 255), static_cast<int>(w >> 24))) - 127;
+}
+// Output in units of 2^vref from now on.
+template <int DH, int NQ>
+__device__ __forceinline__ void raise_vref(Acc<DH, NQ> &st, int vref) {
+  if (vref <= st.vref) return;
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt)
+#pragma unroll
+    for (int dt = 0; dt < DH / 16; ++dt)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) st.o[qt][dt][v] = __builtin_amdgcn_ldexpf(st.o[qt][dt][v], st.vref - vref);
+  st.vref = vref;
+}
+// Scale of a group's values in units of 2^vref.
+__device__ __forceinline__ float scale_of(uint32_t vexp, int vref) {
+  return __uint_as_float(static_cast<uint32_t>(max(static_cast<int>(vexp) - vref, 0)) << 23);
+}
 // A tile of the prefix through both products. `limit`: visible tokens.
 template <typename T, int DH, int NQ>
 __device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, Raw<DH> &t,
@@ -198,41 +251,14 @@ __device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, Raw<DH> &t,
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) s[qt][0] += odd[qt][0], s[qt][1] += odd[qt][1];
   }
-  int none[NQ];
-#pragma unroll
-  for (int qt = 0; qt < NQ; ++qt) none[qt] = 0x7fffffff;
-  softmax_step<DH, NQ>(st, s, none, limit, full, scale, sizeof(T) == 2 ? kProbShift : 0.f, lg);
+  const int none[NQ] = {}, limits[1] = {limit};
+  softmax_step<DH, NQ, 2, false>(st, s, none, limits, scale, sizeof(T) == 2 ? kProbShift : 0.f, lg);
 
   uint32_t vexp = __builtin_amdgcn_ubfe(t.ve, 8 * lg, 8);
-  if (!full) {
-    // Invisible tokens enter with probability 0; their codes are cleared, and the exponent
-    // of a group without visible ones too, so that whatever the page holds adds nothing.
-    // On the codes and in a branch: masks on the converted values took 32 of the 235 vector
-    // instructions of every tile.
-    const int seen = min(max(limit - 8 * lg, 0), 8);
-    const uint32_t lo = seen >= 4 ? ~0u : (1u << 8 * seen) - 1;
-    const uint32_t hi = seen >= 8 ? ~0u : seen <= 4 ? 0u : (1u << 8 * (seen - 4)) - 1;
-#pragma unroll
-    for (int k = 0; k < DH / 32; ++k) t.v[k] &= u32x4{lo, hi, lo, hi};
-    if (seen == 0) vexp = 1;
-  }
+  if (!full) clear_invisible(t.v, vexp, limit, lg);
   if constexpr (sizeof(T) == 2) {
-    // the largest exponent of the groups with a visible token, as a wave-uniform value
-    uint32_t w = __builtin_amdgcn_readfirstlane(t.ve);
-    if (!full) w &= limit > 24 ? ~0u : limit > 16 ? 0xffffffu : limit > 8 ? 0xffffu : limit > 0 ? 0xffu : 0u;
-    const int most = max(max(static_cast<int>(w & 255), static_cast<int>(w >> 8 & 255)),
-                         max(static_cast<int>(w >> 16 & 255), static_cast<int>(w >> 24))) - 127;
-    if (most > st.vref) {
-#pragma unroll
-      for (int qt = 0; qt < NQ; ++qt)
-#pragma unroll
-        for (int dt = 0; dt < DH / 16; ++dt)
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-            st.o[qt][dt][v] = __builtin_amdgcn_ldexpf(st.o[qt][dt][v], st.vref - most);
-      st.vref = most;
-    }
-    const float vs = __uint_as_float(static_cast<uint32_t>(max(static_cast<int>(vexp) - st.vref, 0)) << 23);
+    raise_vref(st, most_exponent(t.ve, limit));
+    const float vs = scale_of(vexp, st.vref);
     u32x4 pf[NQ];
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt)
@@ -261,6 +287,55 @@ __device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, Raw<DH> &t,
             st.o[qt][2 * k + i] = mfma16x16x4(__float_as_uint(a[j]), __float_as_uint(s[qt][j / 4][j % 4]),
                                               st.o[qt][2 * k + i]);
         }
+      }
+  }
+}
+
+// A bf16 call's N tiles, `stride` bytes apart, from their converted fragments in LDS: 2 KB
+// per 32 dims of keys, then of values, of which a lane takes 16 bytes twice. Values are in
+// units of 2^st.vref. One softmax step for all of them: fewer branches, and products of one
+// tile while another's probabilities are made.
+constexpr int kConvBytes = 2048;
+template <int DH, int NQ, int N>
+__device__ __forceinline__ void shared_tiles(Acc<DH, NQ> &st, const uint8_t *tiles, int stride,
+                                             const QFrag<bf16_t, DH> (&qf)[NQ], const int (&limit)[N], float scale,
+                                             int lane) {
+  constexpr int KS = DH / 32;
+  auto part = [&](int t, int f, int i) {
+    return *reinterpret_cast<const u32x4 *>(tiles + t * stride + f * kConvBytes + i * kFragBytes + 16 * lane);
+  };
+  f32x4 s[NQ][2 * N];
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt)
+#pragma unroll
+    for (int e = 0; e < 2 * N; ++e) s[qt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const u32x4 a = part(t, k, e);
+#pragma unroll
+        for (int qt = 0; qt < NQ; ++qt) s[qt][2 * t + e] = mfma16x16x32(a, qf[qt].x[k][0], s[qt][2 * t + e]);
+      }
+  const int none[NQ] = {};
+  softmax_step<DH, NQ, 2 * N, false>(st, s, none, limit, scale, kProbShift, lane >> 4);
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    u32x4 pf[NQ];
+#pragma unroll
+    for (int qt = 0; qt < NQ; ++qt)
+      pf[qt] = u32x4{pack_f16(s[qt][2 * t][0], s[qt][2 * t][1]), pack_f16(s[qt][2 * t][2], s[qt][2 * t][3]),
+                     pack_f16(s[qt][2 * t + 1][0], s[qt][2 * t + 1][1]),
+                     pack_f16(s[qt][2 * t + 1][2], s[qt][2 * t + 1][3])};
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const u32x4 a = part(t, KS + k, i);
+#pragma unroll
+        for (int qt = 0; qt < NQ; ++qt) st.o[qt][2 * k + i] = mfma_f16(a, pf[qt], st.o[qt][2 * k + i]);
       }
   }
 }
@@ -368,7 +443,8 @@ __device__ __forceinline__ void block_tile(Acc<DH, NQ> &st, Block<T, DH> &t, con
   int cap[NQ];
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) cap[qt] = row_pos[qt] - kTile * u;
-  softmax_step<DH, NQ>(st, s, cap, p.w - kTile * u, false, p.scale_log2, sizeof(T) == 2 ? kProbShift : 0.f, lg);
+  const int limits[1] = {p.w - kTile * u};
+  softmax_step<DH, NQ, 2, true>(st, s, cap, limits, p.scale_log2, sizeof(T) == 2 ? kProbShift : 0.f, lg);
 
   // the largest magnitude's bits tell whether every value is finite
   bool odd = false;
@@ -506,29 +582,35 @@ __device__ __forceinline__ void write_output_row(const AttnQ8Params &p, int b, i
     p.lse[(static_cast<size_t>(b) * p.hq + h) * p.w + pos] = (m + log2f(l)) * 0.69314718055994530942f;
 }
 
-// Shared memory of a workgroup. RW > 1: the tiles that waves with different rows share, a
-// ring of NB steps of IW * TPS tiles, their exponents per wave, and room for a block tile's
-// probabilities; afterwards, with IW > 1, the merge area of one row tile. RW == 1: the merge area, before
-// that the probabilities.
-template <int DH, int NQ, int RW>
+// Shared memory of a workgroup.
+// RW == 1: the merge area of one row tile, before that a block tile's probabilities.
+// RW > 1, bf16: two steps of IW * TPS converted tiles; before the first step, in the second
+// one's place, the probabilities; afterwards, with IW > 1, the merge area.
+// RW > 1, fp32: a ring of NB steps of IW * TPS tiles of codes, their exponents per wave, and
+// the probabilities; afterwards the merge area.
+template <typename T, int DH, int NQ, int RW>
 struct Lds {
+  static constexpr bool CONV = RW > 1 && sizeof(T) == 2;
   static constexpr int IW = kWavesQ8 / RW;             // waves that share a chunk's tiles
   static constexpr int TPS = RW == 4 ? 2 : 1;          // tiles of a wave and step
-  static constexpr int NB = RW == 1 ? 0 : 3;           // steps of the ring
-  static constexpr int TILE = 2 * kTile * DH;          // bytes of a tile
+  static constexpr int NB = RW == 1 ? 0 : CONV ? 2 : 3;  // steps held
+  static constexpr int TILE = CONV ? 2 * (DH / 32) * kConvBytes : 2 * kTile * DH;  // bytes of a tile
+  static constexpr int STEP = IW * TPS * TILE;
   static constexpr int RS = DH + 4;                    // row stride of the merge area (floats)
-  static constexpr int EXPS = NB * IW * TPS * TILE;
-  static constexpr int PROBS = EXPS + NB * TPS * kWavesQ8 * 8;
+  static constexpr int EXPS = NB * STEP;
+  static constexpr int PROBS = CONV ? STEP : EXPS + NB * TPS * kWavesQ8 * 8;
   static constexpr int PROB_STRIDE = RW == 1 ? 16 * RS * 4 : 16 * NQ * kTile * 4;
-  static constexpr int MERGE = kWavesQ8 * 16 * RS * 4;
-  static constexpr int BYTES = PROBS + kWavesQ8 * PROB_STRIDE > MERGE ? PROBS + kWavesQ8 * PROB_STRIDE : MERGE;
+  static constexpr int MERGE = IW == 1 ? 0 : kWavesQ8 * 16 * RS * 4;
+  static constexpr int WITH_PROBS = PROBS + kWavesQ8 * PROB_STRIDE;
+  static constexpr int HELD = EXPS > WITH_PROBS ? EXPS : WITH_PROBS;
+  static constexpr int BYTES = HELD > MERGE ? HELD : MERGE;
   static_assert(PROB_STRIDE >= 16 * NQ * kTile * 4 && PROBS % 16 == 0, "a tile's probabilities fit");
 };
 
 template <typename T, int DH, int NQ, int RW>
 __global__ __launch_bounds__(64 * kWavesQ8) __attribute__((amdgpu_waves_per_eu(2)))
 void attn_q8_kernel(AttnQ8Params p, int n_rg) {
-  using L = Lds<DH, NQ, RW>;
+  using L = Lds<T, DH, NQ, RW>;
   constexpr int IW = L::IW;
   constexpr int RS = L::RS;
   constexpr int KS = DH / 32;
@@ -655,12 +737,99 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
       if (i + 1 < n) prefix_tile<T, DH, NQ>(st, tb, qf, lb, p.scale_log2, ln, lg);
       lb = load(i + 3, tb);
     }
+  } else if constexpr (L::CONV) {
+    // Waves that share a tile share its conversion: each brings every RW-th fragment's codes
+    // into registers, a step ahead, and writes them converted to LDS, from where all multiply.
+    // One barrier a step publishes step s and frees the slot of step s - 1, which step s + 1
+    // takes. All know the exponents, and with them the same vref. Codes in LDS, converted by
+    // every wave, took 250 vector instructions a tile instead of 170 (128 rows 64 -> 59 us,
+    // dh 64 49 -> 43); three waves per SIMD spill (133 us).
+    constexpr int TPS = L::TPS, LPW = (2 * KS + RW - 1) / RW;
+    const int np = n - n_block;  // this wave's prefix tiles
+    const int steps = (g_end - chunk * p.chunk_tiles + IW * TPS - 1) / (IW * TPS);  // of every wave
+    u32x4 raw[TPS][LPW];
+    uint32_t ke[TPS], ve[TPS];
+    int limit[TPS], ahead[TPS];
+    int vref = st.vref;
+    // always issued, past the last tile from empty buffers
+    auto load = [&](int step) {
+#pragma unroll
+      for (int t = 0; t < TPS; ++t) {
+        const int i = n_block + TPS * step + t;
+        size_t off, eoff;
+        const int visible = locate(i, off, eoff);
+        ahead[t] = i < n ? visible : 0;
+        const int bytes = i < n ? kTile * DH : 0;
+        const auto rk = buffer_of(p.k_layer + off, bytes), rv = buffer_of(p.v_layer + off, bytes);
+#pragma unroll
+        for (int c = 0; c < LPW; ++c) {
+          const int f = min(rw + RW * c, 2 * KS - 1);  // the last may be loaded by several
+          const bool key = f < KS;
+          raw[t][c] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+              key ? rk : rv, key ? lane_k : lane_v, 256 * (key ? f : f - KS), kNonTemporal));
+        }
+        ke[t] = __builtin_amdgcn_raw_buffer_load_b32(buffer_of(p.k_exp + eoff, bytes ? 4 : 0), 0, 0, kCached);
+        ve[t] = __builtin_amdgcn_raw_buffer_load_b32(buffer_of(p.v_exp + eoff, bytes ? 4 : 0), 0, 0, kCached);
+      }
+    };
+    auto convert = [&](int step) {
+      uint8_t *slot = smem + (step % 2) * L::STEP + iw * L::TILE + 16 * lane;
+#pragma unroll
+      for (int t = 0; t < TPS; ++t) vref = max(vref, most_exponent(ve[t], ahead[t]));
+#pragma unroll
+      for (int t = 0; t < TPS; ++t) {
+        limit[t] = ahead[t];
+        const float ks = __uint_as_float(__builtin_amdgcn_ubfe(ke[t], 8 * (ln >> 2), 8) << 23);
+#pragma unroll
+        for (int c = 0; c < LPW; ++c) {
+          const int f = rw + RW * c;
+          if (f >= 2 * KS) continue;
+          u32x4 x, y;
+          if (f < KS) {
+            x = codes_to_bf16(raw[t][c][0], raw[t][c][1], ks);
+            y = codes_to_bf16(raw[t][c][2], raw[t][c][3], ks);
+          } else {
+            uint32_t vexp = __builtin_amdgcn_ubfe(ve[t], 8 * lg, 8);
+            u32x4 v[1] = {raw[t][c]};
+            if (limit[t] < kTile) clear_invisible(v, vexp, limit[t], lg);
+            const float vs = scale_of(vexp, vref);
+            x = codes_to_f16(v[0][0], v[0][1], vs);
+            y = codes_to_f16(v[0][2], v[0][3], vs);
+          }
+          uint8_t *to = slot + t * IW * L::TILE + f * kConvBytes;
+          *reinterpret_cast<u32x4 *>(to) = x;
+          *reinterpret_cast<u32x4 *>(to + kFragBytes) = y;
+        }
+      }
+    };
+    for (int k = 0; k < n_block; ++k) {
+      if (k > 0) load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
+      block_tile<T, DH, NQ>(st, blk, p, b, kvh, g0 + IW * k, qf, row_pos, probs, ln, lg);
+    }
+    load(0);  // not ahead of the block: registers
+    convert(0);
+    load(1);
+#pragma unroll 1
+    for (int step = 0; step < steps; ++step) {
+      __syncthreads();
+      int now[TPS];
+      const int units_of = vref;
+#pragma unroll
+      for (int t = 0; t < TPS; ++t) now[t] = limit[t];
+      convert(step + 1);
+      load(step + 2);
+      raise_vref(st, units_of);
+      const uint8_t *slot = smem + (step % 2) * L::STEP + iw * L::TILE;
+      // a last step's missing tile: zeros of an empty buffer, none of them visible
+      if (TPS * step < np) shared_tiles<DH, NQ, TPS>(st, slot, IW * L::TILE, qf, now, p.scale_log2, lane);
+    }
+    __syncthreads();  // the tiles have been read
   } else {
-    // Step s: every wave's s-th tile, all from the ring. A wave fetches its share of the
-    // tile that it works on with the other row waves (whole fragments, straight into LDS),
-    // and for itself the tile's exponents; one barrier a step publishes step s and frees
-    // the slot of step s - 1, which step s - 1 + NB takes. Reading tiles from the L2 once
-    // per row wave instead held 128 rows x 16384 tokens at 77 us of loads.
+    // Step s: every wave's s-th tiles, all from the ring. A wave fetches its share of the
+    // tiles that it works on with the other row waves (whole fragments, straight into LDS),
+    // and for itself the tiles' exponents; one barrier a step publishes step s and frees
+    // the slot of step s - 1, which step s - 1 + NB takes. Codes, as fp32 elements are four
+    // times as many bytes and their matrix instructions cost far more than conversions.
     constexpr int NB = L::NB, TPS = L::TPS, LPW = (2 * KS + RW - 1) / RW;
     const int steps = (g_end - chunk * p.chunk_tiles + IW * TPS - 1) / (IW * TPS);  // of every wave
     uint64_t visible = 0;  // of the tiles of the last NB issued steps, 8 bits each

@@ -67,9 +67,9 @@ struct PlanQ8 {
 //   8: 20 to 30 chunks 17.5, 59 18.9), but for 16 tiles at least, 8 where there are few
 //   (8 x 4000 tokens, 126 tiles: 8 tiles 9.7 us, 4 10.5, 16 11.1).
 // - Waves with different rows share a chunk's tiles instead of taking them in turn: two
-//   workgroups per CU, which is what is resident (4 x 8 x 16384 x 128 rows: 33 tiles 71
-//   us, 20 91, 43 84), of 8 tiles at least, 4 with two such waves (96 rows, 81 tiles: 8
-//   26 us, 4 34; 64 rows, 127 tiles: 4 15.3, 8 16.6).
+//   workgroups per CU, which is what is resident (4 x 8 x 16384 x 128 rows: 33 tiles 58
+//   us, 24 69, 43 67), of 8 tiles at least, 4 with two such waves (96 rows, 81 tiles: 8
+//   23 us, 4 29; 64 rows, 127 tiles: 4 17, 8 19).
 das_status plan_attn(const das_cache_q8 *cache, const das_batch *b, int hq, int w, PlanQ8 *plan) {
   const das_cache *c = &cache->base;
   if (hq < 1 || hq % c->num_kv_heads != 0) return DAS_ERR_SHAPE;
