@@ -17,7 +17,7 @@
 // - bf16 rows (sample_values) are counted by value in LDS; counts, one exponential per
 //   value and a scan give every cut, a second pass adds up the looked-up weights of every
 //   block of 512 tokens or more, and one wave goes once more through the block that holds
-//   the drawn one (64 rows of 100003: 40 us).
+//   the drawn one (64 rows of 100003: 38 us).
 // - fp32 rows, and bf16 ones whose logits that does not suit: a pass for the maximum, then
 //   a cut in the order is found by counting (top-k) or weighing (top-p) the row in 2048
 //   bins of equal width below it. Where few tokens lie above the end of the cut's bin, the
@@ -62,21 +62,15 @@ __device__ __forceinline__ Raw8<T> load8(const T *row, int i, int n) {
     __builtin_memcpy(&r, row + i, sizeof(r));
     return r;
   }
+  // all at once: one after the other they held a row's last wave up, and with it every pass
 #pragma unroll
-  for (int k = 0; k < static_cast<int>(sizeof(r) / 4); ++k) r.w[k] = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
-#pragma unroll 1
-  for (int j = 0; j < 8 && i < n; ++j) {  // in at the top, one after the other
-    constexpr int N = sizeof(r) / 4;
+  for (int j = 0; j < 8; ++j) {
+    const T z = row[min(i + j, n - 1)];
     if constexpr (sizeof(T) == 2) {
-      const uint32_t v = i + j < n ? row[i + j] : 0xff80u;
-#pragma unroll
-      for (int k = 0; k < N - 1; ++k) r.w[k] = r.w[k] >> 16 | r.w[k + 1] << 16;
-      r.w[N - 1] = r.w[N - 1] >> 16 | v << 16;
+      const uint32_t v = i + j < n ? z : 0xff80u;
+      r.w[j / 2] = j % 2 ? r.w[j / 2] | v << 16 : v;
     } else {
-      const uint32_t v = i + j < n ? __float_as_uint(row[i + j]) : 0xff800000u;
-#pragma unroll
-      for (int k = 0; k < N - 1; ++k) r.w[k] = r.w[k + 1];
-      r.w[N - 1] = v;
+      r.w[j] = i + j < n ? __float_as_uint(z) : 0xff800000u;
     }
   }
   return r;
@@ -111,15 +105,6 @@ __device__ __forceinline__ uint64_t weight_of(double x) {
   q = __builtin_fma(q, f, 1.0);
   const double w = __builtin_amdgcn_ldexp(q, static_cast<int>(n) + 40);
   return __builtin_bit_cast(uint64_t, w + 0x1p52) & 0xfffffffffffffull;
-}
-
-// The next of the eight to place 0.
-template <typename T>
-__device__ __forceinline__ void pop(Raw8<T> &r) {
-  constexpr int N = sizeof(r.w) / 4;
-#pragma unroll
-  for (int k = 0; k < N - 1; ++k) r.w[k] = sizeof(T) == 2 ? r.w[k] >> 16 | r.w[k + 1] << 16 : r.w[k + 1];
-  if (sizeof(T) == 2) r.w[N - 1] >>= 16;
 }
 
 struct Row {
@@ -558,17 +543,14 @@ __device__ __forceinline__ void clear(Blocks &blk) {
   for (int i = threadIdx.x; i < kMaxBlocks; i += THREADS) blk.above[i] = 0, blk.ties[i] = 0;
   __syncthreads();
 }
-// A wave's step of block b: its weights and ties.
+// A wave's step of block b: its weights (below 2^50) and ties, in one sum over the wave.
 __device__ __forceinline__ void add_step(Blocks &blk, int b, uint64_t sum, uint32_t ties) {
-  const bool lead = threadIdx.x % 64 == 0;
-  if (__builtin_amdgcn_ballot_w64(sum != 0)) {
-    sum = wave_sum(sum);
-    if (lead) atomicAdd(&blk.above[b], static_cast<unsigned long long>(sum));
-  }
-  if (__builtin_amdgcn_ballot_w64(ties != 0)) {
-    ties = static_cast<uint32_t>(wave_sum(ties));
-    if (lead) atomicAdd(&blk.ties[b], ties);
-  }
+  sum += static_cast<uint64_t>(ties) << 52;
+  if (__builtin_amdgcn_ballot_w64(sum != 0) == 0) return;
+  sum = wave_sum(sum);
+  if (threadIdx.x % 64 != 0) return;
+  atomicAdd(&blk.above[b], static_cast<unsigned long long>(sum & 0xfffffffffffffull));
+  if (sum >> 52) atomicAdd(&blk.ties[b], static_cast<uint32_t>(sum >> 52));
 }
 
 // The drawn token from the sums of the blocks: `above(z)` is the weight of a token that is
@@ -606,14 +588,16 @@ __device__ __forceinline__ void pick(const SampleParams &p, const T *row, int ro
   for (int i0 = sh.at << shift; i0 < n; i0 += kStep) {
     const int i = i0 + 8 * lane;
     const Raw8<T> z8 = load8<T>(row, i, n);
-    uint64_t sum = 0;
+    uint64_t sum = 0, w[8];
     uint32_t ties = 0;
-    Raw8<T> z = z8;
-#pragma unroll 1
-    for (int j = 0; j < 8; ++j, pop(z)) {
-      const float x = logit<T>(z, 0);
-      if (limit && tie(x)) ++ties;
-      else if (i + j < n) sum += above(x);
+    bool at_cut[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float x = logit<T>(z8, j);
+      at_cut[j] = limit && tie(x);
+      w[j] = !at_cut[j] && i + j < n ? above(x) : 0;
+      ties += at_cut[j];
+      sum += w[j];
     }
     const uint32_t ties_before = rank + static_cast<uint32_t>(wave_scan(ties)) - ties;
     const uint32_t ties_kept = min(ties_before + ties, limit) - min(ties_before, limit);
@@ -622,19 +606,15 @@ __device__ __forceinline__ void pick(const SampleParams &p, const T *row, int ro
     const uint64_t end = run + wave_sum(sum);
     if (target < end) {
       uint32_t own = ties_before;
-      z = z8;
-#pragma unroll 1
-      for (int j = 0; j < 8; ++j, pop(z)) {
-        const float x = logit<T>(z, 0);
-        uint64_t w = 0;
-        if (limit && tie(x)) w = own++ < limit ? tie_weight : 0;
-        else if (i + j < n) w = above(x);
-        if (w_run <= target && target < w_run + w) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (at_cut[j]) w[j] = own++ < limit ? tie_weight : 0;
+        if (w_run <= target && target < w_run + w[j]) {
           p.tokens[row_id] = i + j;
           if (p.probs)
-            p.probs[row_id] = greedy ? 1.f : static_cast<float>(static_cast<double>(w) / static_cast<double>(total));
+            p.probs[row_id] = greedy ? 1.f : static_cast<float>(static_cast<double>(w[j]) / static_cast<double>(total));
         }
-        w_run += w;
+        w_run += w[j];
       }
       return;
     }
@@ -741,31 +721,33 @@ __device__ bool sample_values(const SampleParams &p, const bf16_t *row, int row_
     uint64_t centre_sum;
     block_scan<THREADS>(mine, sh, &centre_sum);
     uint64_t counts = 0, sums = 0, all, unused;
-#pragma unroll 1
-    for (int i = bin0; i < bin1; ++i) {
-      const uint32_t c = sh.value.count[i];
-      const uint64_t w = c && i != kCentre && i < kBottom ? r.weight(bin_value(i)) : 0;
-      sh.value.weight[i] = w;
-      counts += c;
-      sums += i == kCentre ? centre_sum : w * c;
+    uint64_t weights[PER], own[PER];  // of a token, and of all tokens of the thread's bins
+    uint32_t held[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int i = bin0 + j;
+      held[j] = i < bin1 ? sh.value.count[i] : 0;
+      weights[j] = held[j] && i != kCentre && i < kBottom ? r.weight(bin_value(i)) : 0;
+      own[j] = i < bin1 && i == kCentre ? centre_sum : weights[j] * held[j];
+      if (i < bin1) sh.value.weight[i] = weights[j];
+      counts += held[j];
+      sums += own[j];
     }
     const uint64_t sums_before = block_scan<THREADS>(sums, sh, &all);
     uint64_t limit = all;  // weight that top-k leaves
     if (k > 0 && k < n) {
       uint64_t before = block_scan<THREADS>(counts, sh, &unused), sum = sums_before;
       const uint64_t want = static_cast<uint32_t>(k);
-#pragma unroll 1
-      for (int i = bin0; i < bin1; ++i) {
-        const uint32_t c = sh.value.count[i];
-        const uint64_t w = sh.value.weight[i];
-        if (before < want && before + c >= want) {
-          sh.at = i;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        if (before < want && before + held[j] >= want) {
+          sh.at = bin0 + j;
           sh.answer_ties = static_cast<uint32_t>(want - before);
-          sh.answer64 = sum + w * (want - before);
-          sh.answer32 = c;
+          sh.answer64 = sum + weights[j] * (want - before);
+          sh.answer32 = held[j];
         }
-        before += c;
-        sum += i == kCentre ? centre_sum : w * c;
+        before += held[j];
+        sum += own[j];
       }
       __syncthreads();
       cut = sh.at;
@@ -784,27 +766,28 @@ __device__ bool sample_values(const SampleParams &p, const bf16_t *row, int row_
       uint64_t target = share < 1.0 ? 1 : static_cast<uint64_t>(share);
       if (target > limit) target = limit;
       uint64_t sum = sums_before;
-#pragma unroll 1
-      for (int i = bin0; i < bin1; ++i) {
-        const uint64_t w = sh.value.weight[i];
-        const uint64_t own = i == kCentre ? centre_sum : w * sh.value.count[i];
-        if (sum < target && sum + own >= target) {
-          sh.at = i;
-          sh.answer_ties = i == kCentre ? 0 : static_cast<uint32_t>((target - sum + w - 1) / w);
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        if (sum < target && sum + own[j] >= target) {
+          sh.at = bin0 + j;
+          sh.answer64 = target - sum;
         }
-        sum += own;
+        sum += own[j];
       }
       __syncthreads();
       if (sh.at == kCentre) return false;
       cut = sh.at;
-      ties = sh.answer_ties;
+      const uint64_t w = sh.value.weight[cut];
+      ties = static_cast<uint32_t>((sh.answer64 + w - 1) / w);
     }
     tie_weight = cut < kBottom && cut != kCentre ? sh.value.weight[cut] : 0;
     if (tie_weight < r.least) ties = 0;
   }
   __syncthreads();  // counts and weights have been read
-#pragma unroll 1
-  for (int i = bin0; i < bin1; ++i) {
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int i = bin0 + j;
+    if (i >= bin1) break;
     const uint64_t w = i < cut && !greedy ? sh.value.weight[i] : 0;
     sh.value.weight[i] = w >= r.least ? w : 0;
   }
