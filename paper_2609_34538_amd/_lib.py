@@ -664,6 +664,8 @@ def attn_policy_q8(cache: QuantCache, batch: Batch, layer: int, kappa: int, nu: 
                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Eq. (2)-(3) over an 8-bit cache: prefix keys at depth kappa, values at depth nu."""
+    if q.dim() != 4:
+        raise ValueError("q must be [B, w, Hq, dh]")
     if out is None:
         out = _empty_on(stream, q.shape, q.dtype, q.device)
     if workspace is None:

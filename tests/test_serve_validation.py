@@ -216,6 +216,8 @@ def test_the_binding_refuses_tensors_in_host_memory():
     cache, batch, q, kb = _tensors()
     i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32)  # noqa: E731
     new = torch.zeros((2, 2, 3, 4, 2, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="q must be"):
+        das.attn_policy_q8(cache, batch, 0, 1, 2, q[0, 0], kb, kb)
     for call in (lambda: das.attn_policy_q8(cache, batch, 0, 1, 2, q, kb, kb),
                  lambda: das.kv_append_q8(cache, batch, new, new[:1], i32(3)),
                  lambda: das.sample(torch.zeros((2, 3, 50)), torch.zeros((2, 3))),
