@@ -118,11 +118,11 @@ struct Row {
   float width;
   __device__ __forceinline__ int bin(float z) const {
     const float d = (best - z) * width;  // NaN where both are infinite: bin 0
-    return d < kBins - 1 ? static_cast<int>(d) : d >= kBins - 1 ? kBins - 1 : 0;
+    return static_cast<int>(fminf(fmaxf(d, 0.f), kBins - 1.f));
   }
   __device__ __forceinline__ uint64_t weight(float z) const {
-    return z == best ? static_cast<uint64_t>(kOne)
-                     : weight_of((static_cast<double>(z) - static_cast<double>(best)) * c);
+    // infinities as 2^1000, so that they are 0 apart, and all others infinitely far
+    return weight_of((fmin(static_cast<double>(z), 0x1p1000) - fmin(static_cast<double>(best), 0x1p1000)) * c);
   }
 };
 
@@ -382,16 +382,18 @@ __device__ bool find_cut(const SampleParams &p, const T *row, int row_id, Row &r
   }
   __syncthreads();
   const int wave = tid / 64;
+  // in the order of the keys, as no logit is NaN or -0; NaN where there is no cut yet
+  const float cut = of_key(r.key);
   if constexpr (WEIGH) {
     for_tokens<THREADS, T>(row, n, [&](int, float z) {
-      if (key_of(z) <= r.key) return;  // those equal are added below, as many as count
+      if (z <= cut) return;  // those equal are added below, as many as count
       const uint64_t w = r.weight(z);
       if (w) atomicAdd(reinterpret_cast<unsigned long long *>(&sh.cut.bin.weight[bin_of(z)]),
                        static_cast<unsigned long long>(w));
     });
   } else {
     for_tokens<THREADS, T>(row, n, [&](int, float z) {
-      if (key_of(z) >= r.key) atomicAdd(&sh.cut.bin.count[bin_of(z)], 1u);
+      if (!(z < cut)) atomicAdd(&sh.cut.bin.count[bin_of(z)], 1u);
     });
   }
   __syncthreads();
@@ -914,12 +916,13 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
   __syncthreads();
   clear<THREADS>(sh.last);
   const int shift = row_shift(n);
+  const float cut = of_key(r.key);  // NaN: none
   auto above = [&](float z) -> uint64_t {
-    if (key_of(z) <= r.key) return 0;
+    if (z <= cut) return 0;
     const uint64_t w = r.weight(z);
     return w >= r.least ? w : 0;
   };
-  auto tie = [&](float z) { return key_of(z) == r.key; };
+  auto tie = [&](float z) { return z == cut; };
   if constexpr (sizeof(T) == 4) {
     for_row<THREADS, T>(row, n, [&](int i, const Raw8<T> &z8) {
       uint64_t sum = 0;
