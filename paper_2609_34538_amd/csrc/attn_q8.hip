@@ -29,7 +29,10 @@
 // Values are held relative to the largest exponent that the wave
 // has met (vref, per wave), which like the running maximum rescales the output
 // when it grows, by a power of two. Draft-block values are bf16 with bf16's range:
-// their probabilities enter as a bf16 and its remainder, two products.
+// their probabilities enter as a bf16 and its remainder, two products. Sums are in units of
+// 2^vref / 2^9, down to 2^-73, which a block value past 2^40 could take past the largest
+// fp32: those, as what is not finite, are left out of the products and added one by one at
+// the end, when the sums are plain, to the rows that see them (kLate).
 // fp32 calls use v_mfma_f32_16x16x4_f32 for both products; reduction slots may be
 // numbered freely as long as both operands agree, so the same pieces serve: step i
 // takes a lane's i-th dim or token.
@@ -340,15 +343,24 @@ __device__ __forceinline__ void shared_tiles(Acc<DH, NQ> &st, const uint8_t *til
   }
 }
 
-// A word of block values (two bf16 or one fp32) with what is not finite replaced by 0.
+// The bits of the smallest block value that is added late: 2^40 in bf16 calls (probabilities
+// reach 2^15 in units of 2^-64, and a block has 64 positions: 2^125 at most), in fp32 calls
+// infinity.
 template <typename T>
-__device__ __forceinline__ uint32_t finite_word(uint32_t w) {
+constexpr uint32_t kLate = sizeof(T) == 2 ? (127u + 40) << 7 : 0x7f800000u;
+// A word of block values (two bf16 or one fp32) with those of them replaced by 0.
+template <typename T>
+__device__ __forceinline__ uint32_t without_late(uint32_t w) {
   if constexpr (sizeof(T) == 2) {
-    const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu;
-    return (w & 0x7f800000u) == 0x7f800000u ? lo : lo | (w & 0xffff0000u);
+    const uint32_t lo = (w & 0x7fffu) >= kLate<T> ? 0u : w & 0xffffu;
+    return (w >> 16 & 0x7fffu) >= kLate<T> ? lo : lo | (w & 0xffff0000u);
   } else {
-    return (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
+    return (w & 0x7fffffffu) >= kLate<T> ? 0u : w;
   }
+}
+template <typename T>
+__device__ __forceinline__ bool is_late(float x) {
+  return (__float_as_uint(x) & 0x7fffffffu) >= (sizeof(T) == 2 ? kLate<T> << 16 : kLate<T>);
 }
 
 // A draft-block tile as loaded, in the call's type, straight from the token-major rows:
@@ -390,42 +402,13 @@ __device__ __forceinline__ void load_block(Block<T, DH> &t, const AttnQ8Params &
   }
 }
 
-// What finite_word took out of a draft-block tile's values, for the rows that see it: in a
-// product 0 * NaN would reach the rows that do not. probs: the tile's probabilities,
-// [row tile][row][token].
+// Logits of tile u of the draft block.
 template <typename T, int DH, int NQ>
-__device__ __forceinline__ void add_not_finite(Acc<DH, NQ> &st, const float *probs, const T *vb,
-                                               size_t row_elems, int t0, int w, const int (&cap)[NQ],
-                                               int ln, int lg) {
-#pragma unroll
-  for (int k = 0; k < DH / 32; ++k) {
-#pragma unroll 1
-    for (int t = 0; t < kTile && t0 + t < w; ++t) {
-      const T *src = vb + (t0 + t) * row_elems + 32 * k + 8 * lg;
-#pragma unroll
-      for (int qt = 0; qt < NQ; ++qt) {
-        const float pt = probs[(16 * qt + ln) * kTile + t];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {  // tile 2 k + i % 2 holds dim 32 k + 8 g + i
-          const float x = to_f32<T>(src[i]);
-          if (!(fabsf(x) < __builtin_huge_valf()) && t <= cap[qt]) st.o[qt][2 * k + i % 2][i / 2] += pt * x;
-        }
-      }
-    }
-  }
-}
-
-// Tile u of the draft block through both products.
-template <typename T, int DH, int NQ>
-__device__ __forceinline__ void block_tile(Acc<DH, NQ> &st, Block<T, DH> &t, const AttnQ8Params &p, int b,
-                                           int kvh, int u, const QFrag<T, DH> (&qf)[NQ],
-                                           const int (&row_pos)[NQ], float *probs, int ln, int lg) {
-  constexpr int KS = DH / 32;
-  f32x4 s[NQ][2];
+__device__ __forceinline__ void block_logits(f32x4 (&s)[NQ][2], const Block<T, DH> &t, const QFrag<T, DH> (&qf)[NQ]) {
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) s[qt][0] = s[qt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int k = 0; k < KS; ++k)
+  for (int k = 0; k < DH / 32; ++k)
 #pragma unroll
     for (int h = 0; h < Block<T, DH>::W; ++h)
 #pragma unroll
@@ -440,14 +423,23 @@ __device__ __forceinline__ void block_tile(Acc<DH, NQ> &st, Block<T, DH> &t, con
             for (int qt = 0; qt < NQ; ++qt) s[qt][e] = mfma16x16x4(t.k[e][k][h][i], qf[qt].x[k][h][i], s[qt][e]);
         }
       }
+}
+
+// Tile u of the draft block through both products. True if values of it are left to
+// late_values.
+template <typename T, int DH, int NQ>
+__device__ __forceinline__ bool block_tile(Acc<DH, NQ> &st, Block<T, DH> &t, const AttnQ8Params &p, int u,
+                                           const QFrag<T, DH> (&qf)[NQ], const int (&row_pos)[NQ], int lg) {
+  constexpr int KS = DH / 32;
+  f32x4 s[NQ][2];
+  block_logits<T, DH, NQ>(s, t, qf);
   int cap[NQ];
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) cap[qt] = row_pos[qt] - kTile * u;
   const int limits[1] = {p.w - kTile * u};
   softmax_step<DH, NQ, 2, true>(st, s, cap, limits, p.scale_log2, sizeof(T) == 2 ? kProbShift : 0.f, lg);
 
-  // the largest magnitude's bits tell whether every value is finite
-  bool odd = false;
+  // the largest magnitude's bits tell whether any is late
   typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
   u16x2 most = {0, 0};
   uint32_t most32 = 0;
@@ -460,20 +452,15 @@ __device__ __forceinline__ void block_tile(Acc<DH, NQ> &st, Block<T, DH> &t, con
       else
         most32 = max(most32, max(t.v[k][j][0] & 0x7fffffffu, t.v[k][j][1] & 0x7fffffffu));
     }
-  odd = sizeof(T) == 2 ? most[0] >= 0x7f80 || most[1] >= 0x7f80 : most32 >= 0x7f800000u;
-  const bool any_odd = __builtin_amdgcn_ballot_w64(odd) != 0;
-  if (any_odd) {
+  if constexpr (sizeof(T) == 2) most32 = max(most[0], most[1]);
+  const bool any_late = __builtin_amdgcn_ballot_w64(most32 >= kLate<T>) != 0;
+  if (any_late) {
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int h = 0; h < Block<T, DH>::W; ++h) t.v[k][j][h] = finite_word<T>(t.v[k][j][h]);
-#pragma unroll
-    for (int qt = 0; qt < NQ; ++qt) {
-      f32x4 *dst = reinterpret_cast<f32x4 *>(probs + (16 * qt + ln) * kTile + 8 * lg);
-      dst[0] = s[qt][0], dst[1] = s[qt][1];
-    }
+        for (int h = 0; h < Block<T, DH>::W; ++h) t.v[k][j][h] = without_late<T>(t.v[k][j][h]);
   }
   if constexpr (sizeof(T) == 2) {
     u32x4 hi[NQ], lo[NQ];
@@ -514,13 +501,51 @@ __device__ __forceinline__ void block_tile(Acc<DH, NQ> &st, Block<T, DH> &t, con
           for (int qt = 0; qt < NQ; ++qt)
             st.o[qt][2 * k + h] = mfma16x16x4(t.v[k][j][h], __float_as_uint(s[qt][j / 4][j % 4]), st.o[qt][2 * k + h]);
   }
-  if (any_odd) {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    const size_t row_elems = static_cast<size_t>(p.hkv) * DH;
-    const T *vb = static_cast<const T *>(p.vb) + (static_cast<size_t>(b) * p.w * p.hkv + kvh) * DH;
-    add_not_finite<T, DH, NQ>(st, probs, vb, row_elems, kTile * u, p.w, cap, ln, lg);
+  return any_late;
+}
+
+// The late values of tile u of the draft block, for the rows that see them (in a product
+// 0 * NaN would reach the rows that do not). `o`: plain sums, relative to the references m;
+// probs: the wave's place in LDS for the tile's probabilities, [row tile][row][token].
+template <typename T, int DH, int NQ>
+__device__ __forceinline__ void late_values(f32x4 (&o)[NQ][DH / 16], const float (&m)[NQ], const AttnQ8Params &p,
+                                            int b, int kvh, int u, const QFrag<T, DH> (&qf)[NQ],
+                                            const int (&row_pos)[NQ], float *probs, int ln, int lg) {
+  Block<T, DH> t;
+  load_block<T, DH>(t, p, b, kvh, u, ln, lg);
+  f32x4 s[NQ][2];
+  block_logits<T, DH, NQ>(s, t, qf);
+  __builtin_amdgcn_wave_barrier();  // the tile before has been read
+#pragma unroll
+  for (int qt = 0; qt < NQ; ++qt) {
+    f32x4 *dst = reinterpret_cast<f32x4 *>(probs + (16 * qt + ln) * kTile + 8 * lg);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        s[qt][e][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][e][v], p.scale_log2, -m[qt]));
+    dst[0] = s[qt][0], dst[1] = s[qt][1];
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  const size_t row_elems = static_cast<size_t>(p.hkv) * DH;
+  const T *vb = static_cast<const T *>(p.vb) + (static_cast<size_t>(b) * p.w * p.hkv + kvh) * DH;
+#pragma unroll
+  for (int k = 0; k < DH / 32; ++k) {
+#pragma unroll 1
+    for (int i = 0; i < kTile && kTile * u + i < p.w; ++i) {
+      const T *src = vb + (kTile * u + i) * row_elems + 32 * k + 8 * lg;
+#pragma unroll
+      for (int qt = 0; qt < NQ; ++qt) {
+        const float pt = probs[(16 * qt + ln) * kTile + i];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {  // tile 2 k + j % 2 holds dim 32 k + 8 g + j
+          const float x = to_f32<T>(src[j]);
+          if (is_late<T>(x) && kTile * u + i <= row_pos[qt]) o[qt][2 * k + j % 2][j / 2] += pt * x;
+        }
+      }
+    }
   }
 }
 
@@ -583,9 +608,10 @@ __device__ __forceinline__ void write_output_row(const AttnQ8Params &p, int b, i
 }
 
 // Shared memory of a workgroup.
-// RW == 1: the merge area of one row tile, before that a block tile's probabilities.
-// RW > 1, bf16: two steps of IW * TPS converted tiles; before the first step, in the second
-// one's place, the probabilities; afterwards, with IW > 1, the merge area.
+// RW == 1: the merge area of one row tile, before that a block tile's probabilities for its
+// late values.
+// RW > 1, bf16: two steps of IW * TPS converted tiles; afterwards, in the second one's place,
+// the probabilities, and then, with IW > 1, the merge area.
 // RW > 1, fp32: a ring of NB steps of IW * TPS tiles of codes, their exponents per wave, and
 // the probabilities; afterwards the merge area.
 template <typename T, int DH, int NQ, int RW>
@@ -680,7 +706,6 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     for (int dt = 0; dt < DH / 16; ++dt) st.o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  float *probs = reinterpret_cast<float *>(smem + L::PROBS + wave * L::PROB_STRIDE);
   const uint32_t lane_k = (ln >> 2) * 8 * DH + lg * 64 + (ln & 3) * 16;
   const uint32_t lane_v = lg * 8 * DH + ln * 16;
   // Where the wave's i-th tile lies, and the number of its visible tokens. An out-of-range
@@ -700,6 +725,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     return ok ? min(kTile, S - kTile * tile) : 0;
   };
   const int n_block = g0 < nb ? min((nb - g0 + IW - 1) / IW, n) : 0;  // the wave's block tiles
+  bool late = false;                                                  // they have late values
 
   if constexpr (RW == 1) {
     // Past the last tile the loads go to empty buffers: they are always issued, so that
@@ -724,10 +750,10 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     int i = n_block;
     int la = load(i, ta);
     if (has_block) {
-      block_tile<T, DH, NQ>(st, blk, p, b, kvh, g0, qf, row_pos, probs, ln, lg);
+      late = block_tile<T, DH, NQ>(st, blk, p, g0, qf, row_pos, lg);
       for (int k = 1; k < n_block; ++k) {
         load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
-        block_tile<T, DH, NQ>(st, blk, p, b, kvh, g0 + IW * k, qf, row_pos, probs, ln, lg);
+        late |= block_tile<T, DH, NQ>(st, blk, p, g0 + IW * k, qf, row_pos, lg);
       }
     }
     int lb = load(i + 1, tb);
@@ -804,7 +830,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     };
     for (int k = 0; k < n_block; ++k) {
       if (k > 0) load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
-      block_tile<T, DH, NQ>(st, blk, p, b, kvh, g0 + IW * k, qf, row_pos, probs, ln, lg);
+      late |= block_tile<T, DH, NQ>(st, blk, p, g0 + IW * k, qf, row_pos, lg);
     }
     load(0);  // not ahead of the block: registers
     convert(0);
@@ -859,7 +885,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     for (int s = 0; s < NB - 1; ++s) issue(s);
     for (int s = 0; s < n_block; ++s) {
       if (s > 0) load_block<T, DH>(blk, p, b, kvh, g0 + IW * s, ln, lg);
-      block_tile<T, DH, NQ>(st, blk, p, b, kvh, g0 + IW * s, qf, row_pos, probs, ln, lg);
+      late |= block_tile<T, DH, NQ>(st, blk, p, g0 + IW * s, qf, row_pos, lg);
     }
 #pragma unroll 1
     for (int s = 0; s < steps; ++s) {
@@ -902,6 +928,11 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
         for (int v = 0; v < 4; ++v)
           st.o[qt][dt][v] = __builtin_amdgcn_ldexpf(st.o[qt][dt][v], st.vref - 9);
     }
+  }
+  if (late) {
+    float *probs = reinterpret_cast<float *>(smem + L::PROBS + wave * L::PROB_STRIDE);
+    for (int k = 0; k < n_block; ++k)
+      late_values<T, DH, NQ>(st.o, m, p, b, kvh, g0 + IW * k, qf, row_pos, probs, ln, lg);
   }
   uint8_t *rec = p.ws + (static_cast<size_t>(unit) * p.nsplit + chunk) * p.piece_stride;
   if constexpr (IW == 1) {  // a row's result is one wave's
