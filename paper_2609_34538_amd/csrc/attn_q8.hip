@@ -56,7 +56,14 @@ constexpr int kWavesQ8 = 4;
 // that the largest fit fp16 and those down to 2^-23 of the reference are normal there.
 constexpr float kSlack = 6.f;
 constexpr float kProbShift = 9.f;
-constexpr float kNoRef = 1e30f;  // in place of shift - reference: nothing seen yet
+constexpr float kNoRef = 3e38f;  // in place of shift - reference: nothing seen yet
+// A reference past this (in base-2 units) is far: the rounding of reference * scale would be
+// a factor of its own in every probability, past fp16's range from 2^27 on. A wave that has
+// met one goes through its tiles again, in a form that takes the references off the logits
+// (5 x 32 heads x 4 x 29 rows x 2005 tokens: 43.6 us without, 44.6 so, 46.7 with that form
+// in the steps themselves).
+constexpr float kFar = 0x1p20f;
+constexpr float kLowest = -3.402823466e38f;  // as a reference of that form: nothing seen yet
 
 __device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h16x8, a),
@@ -95,8 +102,9 @@ struct Raw {
   uint32_t ke, ve;
 };
 
-// One wave's running result: neg = shift - reference, a lane's share of the sum l and
-// the output o, in units of 2^vref for bf16 calls, both times 2^shift.
+// One wave's running result: neg = shift - reference (far form: the reference, before the
+// scale), a lane's share of the sum l and the output o, in units of 2^vref for bf16 calls,
+// both times 2^shift.
 template <int DH, int NQ>
 struct Acc {
   float neg[NQ], l[NQ];
@@ -115,8 +123,9 @@ struct QFrag {
 // (the same in a row's four lanes) moves to the row's maximum only when a logit passes it
 // by more than kSlack, which after the first tiles is rare: most tiles need no reduction
 // over lanes and no rescaling. E / 2 tiles at once; BLOCK: a row sees tokens up to its cap.
-template <int DH, int NQ, int E, bool BLOCK>
-__device__ __forceinline__ void softmax_step(Acc<DH, NQ> &st, f32x4 (&s)[NQ][E], const int (&cap)[NQ],
+// FAR: the far form; otherwise `far` receives the lanes of rows whose reference is far.
+template <int DH, int NQ, int E, bool BLOCK, bool FAR>
+__device__ __forceinline__ void softmax_step(Acc<DH, NQ> &st, uint64_t &far, f32x4 (&s)[NQ][E], const int (&cap)[NQ],
                                              const int (&limit)[E / 2], float scale, float shift, int lg) {
   bool full = !BLOCK;
 #pragma unroll
@@ -139,15 +148,28 @@ __device__ __forceinline__ void softmax_step(Acc<DH, NQ> &st, f32x4 (&s)[NQ][E],
     for (int e = 0; e < E; ++e)
 #pragma unroll
       for (int v = 0; v < 4; ++v) mx[qt] = fmaxf(mx[qt], s[qt][e][v]);
-    moves |= __builtin_fmaf(mx[qt], scale, st.neg[qt]) > shift + kSlack;
+    if constexpr (FAR) moves = true;
+    else moves |= __builtin_fmaf(mx[qt], scale, st.neg[qt]) > shift + kSlack;
   }
   if (__builtin_amdgcn_ballot_w64(moves) != 0) {
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
-      const float m = group_max(mx[qt]) * scale;
-      // rows with nothing visible, and those that stay within their slack, keep theirs
-      const float neg = m + st.neg[qt] > shift + kSlack ? shift - m : st.neg[qt];
-      const float alpha = __builtin_amdgcn_exp2f(neg - st.neg[qt]);  // 0 from kNoRef
+      float neg, alpha;
+      if constexpr (FAR) {
+        const float top = group_max(mx[qt]);
+        neg = (top - st.neg[qt]) * scale > kSlack ? top : st.neg[qt];
+        alpha = __builtin_amdgcn_exp2f((st.neg[qt] - neg) * scale);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) s[qt][e][v] -= neg;
+      } else {
+        const float m = group_max(mx[qt]) * scale;
+        // rows with nothing visible, and those that stay within their slack, keep theirs
+        neg = m + st.neg[qt] > shift + kSlack ? shift - m : st.neg[qt];
+        alpha = __builtin_amdgcn_exp2f(neg - st.neg[qt]);  // 0 from kNoRef
+        far |= __builtin_amdgcn_ballot_w64(fabsf(neg) > kFar && neg != kNoRef);
+      }
       st.neg[qt] = neg;
       st.l[qt] *= alpha;
       // a lane's accumulators of row tile qt all belong to one row
@@ -161,7 +183,7 @@ __device__ __forceinline__ void softmax_step(Acc<DH, NQ> &st, f32x4 (&s)[NQ][E],
     for (int e = 0; e < E; ++e)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][e][v], scale, st.neg[qt]));
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][e][v], scale, FAR ? shift : st.neg[qt]));
         s[qt][e][v] = p;
         st.l[qt] += p;
       }
@@ -215,8 +237,8 @@ __device__ __forceinline__ float scale_of(uint32_t vexp, int vref) {
   return __uint_as_float(static_cast<uint32_t>(max(static_cast<int>(vexp) - vref, 0)) << 23);
 }
 // A tile of the prefix through both products. `limit`: visible tokens.
-template <typename T, int DH, int NQ>
-__device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, Raw<DH> &t,
+template <typename T, int DH, int NQ, bool FAR = false>
+__device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, uint64_t &far, Raw<DH> &t,
                                             const QFrag<T, DH> (&qf)[NQ], int limit, float scale,
                                             int ln, int lg) {
   const bool full = limit >= kTile;
@@ -255,7 +277,7 @@ __device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, Raw<DH> &t,
     for (int qt = 0; qt < NQ; ++qt) s[qt][0] += odd[qt][0], s[qt][1] += odd[qt][1];
   }
   const int none[NQ] = {}, limits[1] = {limit};
-  softmax_step<DH, NQ, 2, false>(st, s, none, limits, scale, sizeof(T) == 2 ? kProbShift : 0.f, lg);
+  softmax_step<DH, NQ, 2, false, FAR>(st, far, s, none, limits, scale, sizeof(T) == 2 ? kProbShift : 0.f, lg);
 
   uint32_t vexp = __builtin_amdgcn_ubfe(t.ve, 8 * lg, 8);
   if (!full) clear_invisible(t.v, vexp, limit, lg);
@@ -300,7 +322,7 @@ __device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, Raw<DH> &t,
 // tile while another's probabilities are made.
 constexpr int kConvBytes = 2048;
 template <int DH, int NQ, int N>
-__device__ __forceinline__ void shared_tiles(Acc<DH, NQ> &st, const uint8_t *tiles, int stride,
+__device__ __forceinline__ void shared_tiles(Acc<DH, NQ> &st, uint64_t &far, const uint8_t *tiles, int stride,
                                              const QFrag<bf16_t, DH> (&qf)[NQ], const int (&limit)[N], float scale,
                                              int lane) {
   constexpr int KS = DH / 32;
@@ -323,7 +345,7 @@ __device__ __forceinline__ void shared_tiles(Acc<DH, NQ> &st, const uint8_t *til
         for (int qt = 0; qt < NQ; ++qt) s[qt][2 * t + e] = mfma16x16x32(a, qf[qt].x[k][0], s[qt][2 * t + e]);
       }
   const int none[NQ] = {};
-  softmax_step<DH, NQ, 2 * N, false>(st, s, none, limit, scale, kProbShift, lane >> 4);
+  softmax_step<DH, NQ, 2 * N, false, false>(st, far, s, none, limit, scale, kProbShift, lane >> 4);
 #pragma unroll
   for (int t = 0; t < N; ++t) {
     u32x4 pf[NQ];
@@ -427,8 +449,8 @@ __device__ __forceinline__ void block_logits(f32x4 (&s)[NQ][2], const Block<T, D
 
 // Tile u of the draft block through both products. True if values of it are left to
 // late_values.
-template <typename T, int DH, int NQ>
-__device__ __forceinline__ bool block_tile(Acc<DH, NQ> &st, Block<T, DH> &t, const AttnQ8Params &p, int u,
+template <typename T, int DH, int NQ, bool FAR = false>
+__device__ __forceinline__ bool block_tile(Acc<DH, NQ> &st, uint64_t &far, Block<T, DH> &t, const AttnQ8Params &p, int u,
                                            const QFrag<T, DH> (&qf)[NQ], const int (&row_pos)[NQ], int lg) {
   constexpr int KS = DH / 32;
   f32x4 s[NQ][2];
@@ -437,7 +459,7 @@ __device__ __forceinline__ bool block_tile(Acc<DH, NQ> &st, Block<T, DH> &t, con
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) cap[qt] = row_pos[qt] - kTile * u;
   const int limits[1] = {p.w - kTile * u};
-  softmax_step<DH, NQ, 2, true>(st, s, cap, limits, p.scale_log2, sizeof(T) == 2 ? kProbShift : 0.f, lg);
+  softmax_step<DH, NQ, 2, true, FAR>(st, far, s, cap, limits, p.scale_log2, sizeof(T) == 2 ? kProbShift : 0.f, lg);
 
   // the largest magnitude's bits tell whether any is late
   typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -505,10 +527,11 @@ __device__ __forceinline__ bool block_tile(Acc<DH, NQ> &st, Block<T, DH> &t, con
 }
 
 // The late values of tile u of the draft block, for the rows that see them (in a product
-// 0 * NaN would reach the rows that do not). `o`: plain sums, relative to the references m;
-// probs: the wave's place in LDS for the tile's probabilities, [row tile][row][token].
+// 0 * NaN would reach the rows that do not). Of st, sums are plain here and m their
+// references in base-2 units; probs: the wave's place in LDS for the tile's probabilities,
+// [row tile][row][token].
 template <typename T, int DH, int NQ>
-__device__ __forceinline__ void late_values(f32x4 (&o)[NQ][DH / 16], const float (&m)[NQ], const AttnQ8Params &p,
+__device__ __forceinline__ void late_values(Acc<DH, NQ> &st, bool far, const float (&m)[NQ], const AttnQ8Params &p,
                                             int b, int kvh, int u, const QFrag<T, DH> (&qf)[NQ],
                                             const int (&row_pos)[NQ], float *probs, int ln, int lg) {
   Block<T, DH> t;
@@ -522,8 +545,10 @@ __device__ __forceinline__ void late_values(f32x4 (&o)[NQ][DH / 16], const float
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
-        s[qt][e][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][e][v], p.scale_log2, -m[qt]));
+      for (int v = 0; v < 4; ++v) {
+        const float x = far ? s[qt][e][v] - st.neg[qt] : s[qt][e][v];
+        s[qt][e][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x, p.scale_log2, far ? 0.f : -m[qt]));
+      }
     dst[0] = s[qt][0], dst[1] = s[qt][1];
   }
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -542,7 +567,7 @@ __device__ __forceinline__ void late_values(f32x4 (&o)[NQ][DH / 16], const float
 #pragma unroll
         for (int j = 0; j < 8; ++j) {  // tile 2 k + j % 2 holds dim 32 k + 8 g + j
           const float x = to_f32<T>(src[j]);
-          if (is_late<T>(x) && kTile * u + i <= row_pos[qt]) o[qt][2 * k + j % 2][j / 2] += pt * x;
+          if (is_late<T>(x) && kTile * u + i <= row_pos[qt]) st.o[qt][2 * k + j % 2][j / 2] += pt * x;
         }
       }
     }
@@ -697,14 +722,18 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
   const int n = g_end > g0 ? (g_end - g0 + IW - 1) / IW : 0;  // this wave's tiles
 
   Acc<DH, NQ> st;
-  st.vref = kQ8MinExp;
+  uint64_t far = 0;  // lanes of rows that have met a far reference
+  auto clear = [&](float neg) {
+    st.vref = kQ8MinExp;
 #pragma unroll
-  for (int qt = 0; qt < NQ; ++qt) {
-    st.neg[qt] = kNoRef;
-    st.l[qt] = 0.f;
+    for (int qt = 0; qt < NQ; ++qt) {
+      st.neg[qt] = neg;
+      st.l[qt] = 0.f;
 #pragma unroll
-    for (int dt = 0; dt < DH / 16; ++dt) st.o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+      for (int dt = 0; dt < DH / 16; ++dt) st.o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  clear(kNoRef);
 
   const uint32_t lane_k = (ln >> 2) * 8 * DH + lg * 64 + (ln & 3) * 16;
   const uint32_t lane_v = lg * 8 * DH + ln * 16;
@@ -727,40 +756,42 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
   const int n_block = g0 < nb ? min((nb - g0 + IW - 1) / IW, n) : 0;  // the wave's block tiles
   bool late = false;                                                  // they have late values
 
+  // The wave's i-th tile into registers. Past the last tile the loads go to empty buffers:
+  // they are always issued, so that the compiler can count them, and waits for one tile leave
+  // the next under way.
+  auto load = [&](int i, Raw<DH> &t) {
+    size_t off, eoff;
+    const int visible = locate(i, off, eoff);
+    const int bytes = i < n ? kTile * DH : 0;
+    const auto rk = buffer_of(p.k_layer + off, bytes), rv = buffer_of(p.v_layer + off, bytes);
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+      t.k[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, lane_k, 256 * k, kNonTemporal));
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+      t.v[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, lane_v, 256 * k, kNonTemporal));
+    t.ke = __builtin_amdgcn_raw_buffer_load_b32(buffer_of(p.k_exp + eoff, bytes ? 4 : 0), 0, 0, kCached);
+    t.ve = __builtin_amdgcn_raw_buffer_load_b32(buffer_of(p.v_exp + eoff, bytes ? 4 : 0), 0, 0, kCached);
+    return visible;
+  };
+
   if constexpr (RW == 1) {
-    // Past the last tile the loads go to empty buffers: they are always issued, so that
-    // the compiler can count them, and waits for one tile leave the next under way.
-    auto load = [&](int i, Raw<DH> &t) {
-      size_t off, eoff;
-      const int visible = locate(i, off, eoff);
-      const int bytes = i < n ? kTile * DH : 0;
-      const auto rk = buffer_of(p.k_layer + off, bytes), rv = buffer_of(p.v_layer + off, bytes);
-#pragma unroll
-      for (int k = 0; k < KS; ++k)
-        t.k[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, lane_k, 256 * k, kNonTemporal));
-#pragma unroll
-      for (int k = 0; k < KS; ++k)
-        t.v[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, lane_v, 256 * k, kNonTemporal));
-      t.ke = __builtin_amdgcn_raw_buffer_load_b32(buffer_of(p.k_exp + eoff, bytes ? 4 : 0), 0, 0, kCached);
-      t.ve = __builtin_amdgcn_raw_buffer_load_b32(buffer_of(p.v_exp + eoff, bytes ? 4 : 0), 0, 0, kCached);
-      return visible;
-    };
     // two tiles in flight, the first of the prefix before the block's are worked on
     Raw<DH> ta, tb;
     int i = n_block;
     int la = load(i, ta);
     if (has_block) {
-      late = block_tile<T, DH, NQ>(st, blk, p, g0, qf, row_pos, lg);
+      late = block_tile<T, DH, NQ>(st, far, blk, p, g0, qf, row_pos, lg);
       for (int k = 1; k < n_block; ++k) {
         load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
-        late |= block_tile<T, DH, NQ>(st, blk, p, g0 + IW * k, qf, row_pos, lg);
+        late |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * k, qf, row_pos, lg);
       }
     }
     int lb = load(i + 1, tb);
     for (; i < n; i += 2) {
-      prefix_tile<T, DH, NQ>(st, ta, qf, la, p.scale_log2, ln, lg);
+      prefix_tile<T, DH, NQ>(st, far, ta, qf, la, p.scale_log2, ln, lg);
       la = load(i + 2, ta);
-      if (i + 1 < n) prefix_tile<T, DH, NQ>(st, tb, qf, lb, p.scale_log2, ln, lg);
+      if (i + 1 < n) prefix_tile<T, DH, NQ>(st, far, tb, qf, lb, p.scale_log2, ln, lg);
       lb = load(i + 3, tb);
     }
   } else if constexpr (L::CONV) {
@@ -830,7 +861,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     };
     for (int k = 0; k < n_block; ++k) {
       if (k > 0) load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
-      late |= block_tile<T, DH, NQ>(st, blk, p, g0 + IW * k, qf, row_pos, lg);
+      late |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * k, qf, row_pos, lg);
     }
     load(0);  // not ahead of the block: registers
     convert(0);
@@ -847,7 +878,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
       raise_vref(st, units_of);
       const uint8_t *slot = smem + (step % 2) * L::STEP + iw * L::TILE;
       // a last step's missing tile: zeros of an empty buffer, none of them visible
-      if (TPS * step < np) shared_tiles<DH, NQ, TPS>(st, slot, IW * L::TILE, qf, now, p.scale_log2, lane);
+      if (TPS * step < np) shared_tiles<DH, NQ, TPS>(st, far, slot, IW * L::TILE, qf, now, p.scale_log2, lane);
     }
     __syncthreads();  // the tiles have been read
   } else {
@@ -885,7 +916,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     for (int s = 0; s < NB - 1; ++s) issue(s);
     for (int s = 0; s < n_block; ++s) {
       if (s > 0) load_block<T, DH>(blk, p, b, kvh, g0 + IW * s, ln, lg);
-      late |= block_tile<T, DH, NQ>(st, blk, p, g0 + IW * s, qf, row_pos, lg);
+      late |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * s, qf, row_pos, lg);
     }
 #pragma unroll 1
     for (int s = 0; s < steps; ++s) {
@@ -906,18 +937,34 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
         const u32x2 e = *reinterpret_cast<const u32x2 *>(smem + L::EXPS + (at * kWavesQ8 + wave) * 8);
         x.ke = e[0];
         x.ve = e[1];
-        prefix_tile<T, DH, NQ>(st, x, qf, static_cast<int>(visible >> (8 * (TPS * NB - 1 - t)) & 255), p.scale_log2, ln, lg);
+        prefix_tile<T, DH, NQ>(st, far, x, qf, static_cast<int>(visible >> (8 * (TPS * NB - 1 - t)) & 255), p.scale_log2, ln, lg);
       }
     }
     __syncthreads();  // the ring has been read
   }
 
+  const bool again = far != 0;
+  if (again) {  // far references: the wave by itself, one tile after the other
+    clear(kLowest);
+    for (int k = 0; k < n_block; ++k) {
+      load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
+      late |= block_tile<T, DH, NQ, true>(st, far, blk, p, g0 + IW * k, qf, row_pos, lg);
+    }
+    window = load_window(0);
+#pragma unroll 1
+    for (int i = n_block; i < n; ++i) {
+      Raw<DH> t;
+      const int visible = load(i, t);
+      prefix_tile<T, DH, NQ, true>(st, far, t, qf, visible, p.scale_log2, ln, lg);
+    }
+  }
   // From here on l and o are the plain ones, unnormalised, without shifts.
   constexpr float kShift = sizeof(T) == 2 ? kProbShift : 0.f;
   float m[NQ];
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) {
-    m[qt] = st.neg[qt] == kNoRef ? kNegInf : kShift - st.neg[qt];
+    m[qt] = again ? (st.neg[qt] == kLowest ? kNegInf : st.neg[qt] * p.scale_log2)
+            : st.neg[qt] == kNoRef ? kNegInf : kShift - st.neg[qt];
     st.l[qt] = group_sum(st.l[qt]);
     if constexpr (sizeof(T) == 2) {
       st.l[qt] *= 0x1p-9f;
@@ -932,7 +979,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
   if (late) {
     float *probs = reinterpret_cast<float *>(smem + L::PROBS + wave * L::PROB_STRIDE);
     for (int k = 0; k < n_block; ++k)
-      late_values<T, DH, NQ>(st.o, m, p, b, kvh, g0 + IW * k, qf, row_pos, probs, ln, lg);
+      late_values<T, DH, NQ>(st, again, m, p, b, kvh, g0 + IW * k, qf, row_pos, probs, ln, lg);
   }
   uint8_t *rec = p.ws + (static_cast<size_t>(unit) * p.nsplit + chunk) * p.piece_stride;
   if constexpr (IW == 1) {  // a row's result is one wave's

@@ -1,5 +1,5 @@
 """Attention over the 8-bit cache at the ends of its types' ranges, against the 64-bit
-oracle: block values far above and below the cache's."""
+oracle: block values far above and below the cache's, and logits of any size."""
 
 from __future__ import annotations
 
@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2609_34538_amd import _lib as das
-from q8_ref import HostCache, attention, random_cache, tolerance
+from q8_ref import HostCache, attention, key_bytes, random_cache, tolerance
 from test_gpu_attn_q8 import _block
 
 pytestmark = pytest.mark.gpu
@@ -55,3 +55,62 @@ def test_large_block_values_reach_only_the_rows_that_see_them(shape):
     out = check(cache, batch, table, lens, q, kb, vb)
     assert torch.equal(out[:, :5], clean[:, :5])
     assert bool((out[:, 5:].float() > 2.0 ** 60).all())
+
+
+def _alone(cache, e, sign, B, w, hq, dh):
+    """Keys of the cache and the block, and queries, that give every position the logit
+    sign * 181 / 128 * 2^e before the scale, exactly: all in dimension 0. Returns (q, k_blk)."""
+    c = max(min(e // 2, 110), -60)
+    codes = cache.k_pool.view(torch.uint8)
+    codes.zero_()
+    codes[..., key_bytes(dh)[:, 0]] = 0x38  # 1
+    cache.k_exp.copy_(torch.where(cache.k_exp == 255, cache.k_exp, torch.full_like(cache.k_exp, 127 + c)))
+    q = torch.zeros((B, w, hq, dh), dtype=cache.dtype, device=DEV)
+    kb = torch.zeros((B, w, cache.num_kv_heads, dh), dtype=cache.dtype, device=DEV)
+    q[..., 0], kb[..., 0] = sign * 181 / 128 * 2.0 ** (e - c), 2.0 ** c
+    return q, kb
+
+
+@pytest.mark.parametrize("lens", [[0, 40], [4000, 700]], ids=["one-chunk", "chunks"])
+@pytest.mark.parametrize("shape", SHAPES, ids=ids)
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("e", [3, 20, 24, 27, 31, 60, 104, 120])
+def test_logits_of_any_size(e, sign, shape, lens):
+    """Equal logits are averaged, and twice the logit from block position 3 on takes all or
+    leaves all, whatever their size. The logits are exact, so they add nothing to the bound
+    but the fp32 steps of 2^e in the logarithm."""
+    dtype, dh, G, w = shape
+    cache, batch, table = random_cache(7, dtype, 2, 2, dh, lens)
+    _, _, vb = _block(11, dtype, 2, w, 2 * G, 2, dh)
+    q, kb = _alone(cache, e, sign, 2, w, 2 * G, dh)
+    host = HostCache(cache)
+    for twice in (False, True):
+        if twice:
+            kb[:, 3:] *= 2
+        lse = torch.full((2, 2 * G, w), float("nan"), device=DEV)
+        out = das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb, lse=lse)
+        for b in range(2):
+            ref, rl, a, _ = attention(host, table, lens, b, 0, 0, 0, q, kb, vb)
+            tol = tolerance(dtype, ref, a, 0.0, lens[b] + w, dh)
+            err = np.abs(out[b].double().cpu().numpy() - ref)
+            assert (err <= tol).all(), (b, twice, float((err / tol).max()))
+            lt = 2 * (lens[b] + 80) * 2.0 ** -24 + 2.0 ** -21 * np.abs(rl)
+            assert (np.abs(lse[b].double().cpu().numpy() - rl) <= lt).all(), (b, twice)
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=ids)
+def test_large_logits_and_block_values(shape):
+    """Rows that reach far logits step by step, with values that are added at the end."""
+    dtype, dh, G, w = shape
+    lens = [500, 0]
+    cache, batch, table = random_cache(7, dtype, 2, 2, dh, lens)
+    _, _, vb = _block(11, dtype, 2, w, 2 * G, 2, dh)
+    vb *= 2.0 ** 60
+    q, kb = _alone(cache, 10, 1, 2, w, 2 * G, dh)
+    kb[..., 0] *= 2.0 ** (torch.arange(w, device=DEV) * 3 % 32)[None, :, None]
+    host = HostCache(cache)
+    out = das.attn_policy_q8(cache, batch, 0, 1, 1, q, kb, vb)
+    for b in range(2):
+        ref, _, a, _ = attention(host, table, lens, b, 0, 0, 0, q, kb, vb)
+        tol = tolerance(dtype, ref, a, 0.0, lens[b] + w, dh)
+        assert (np.abs(out[b].double().cpu().numpy() - ref) <= tol).all(), b
