@@ -53,9 +53,12 @@ constexpr int kTilesPerPage = kPage / kTile;
 constexpr int kWavesQ8 = 4;
 // Probabilities are held relative to a reference that a row's logits may pass by
 // kSlack binary orders before it moves; bf16 calls hold them times 2^kProbShift, so
-// that the largest fit fp16 and those down to 2^-23 of the reference are normal there.
+// that the largest fit fp16 and those down to 2^-23 of the reference are normal there. Plain
+// sums, and all of fp32 calls', are relative to the reference plus kSlack: no probability is
+// over 1, so that a sum passes the largest fp32 only where the values' does.
 constexpr float kSlack = 6.f;
 constexpr float kProbShift = 9.f;
+constexpr float kBySlack = 0x1p-6f, kFromSlack = 0x1p6f;  // 2^-kSlack, 2^kSlack
 constexpr float kNoRef = 3e38f;  // in place of shift - reference: nothing seen yet
 // A reference past this (in base-2 units) is far: the rounding of reference * scale would be
 // a factor of its own in every probability, past fp16's range from 2^27 on. A wave that has
@@ -123,8 +126,8 @@ struct QFrag {
 // (the same in a row's four lanes) moves to the row's maximum only when a logit passes it
 // by more than kSlack, which after the first tiles is rare: most tiles need no reduction
 // over lanes and no rescaling. E / 2 tiles at once; BLOCK: a row sees tokens up to its cap.
-// FAR: the far form; otherwise `far` receives the lanes of rows whose reference is far.
-template <int DH, int NQ, int E, bool BLOCK, bool FAR>
+// F32: an fp32 call's. FAR: the far form; otherwise `far` receives the lanes of rows whose reference is far.
+template <int DH, int NQ, int E, bool BLOCK, bool FAR, bool F32>
 __device__ __forceinline__ void softmax_step(Acc<DH, NQ> &st, uint64_t &far, f32x4 (&s)[NQ][E], const int (&cap)[NQ],
                                              const int (&limit)[E / 2], float scale, float shift, int lg) {
   bool full = !BLOCK;
@@ -183,7 +186,8 @@ __device__ __forceinline__ void softmax_step(Acc<DH, NQ> &st, uint64_t &far, f32
     for (int e = 0; e < E; ++e)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][e][v], scale, FAR ? shift : st.neg[qt]));
+        float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][e][v], scale, FAR ? shift : st.neg[qt]));
+        if constexpr (F32) p *= kBySlack;
         s[qt][e][v] = p;
         st.l[qt] += p;
       }
@@ -277,7 +281,7 @@ __device__ __forceinline__ void prefix_tile(Acc<DH, NQ> &st, uint64_t &far, Raw<
     for (int qt = 0; qt < NQ; ++qt) s[qt][0] += odd[qt][0], s[qt][1] += odd[qt][1];
   }
   const int none[NQ] = {}, limits[1] = {limit};
-  softmax_step<DH, NQ, 2, false, FAR>(st, far, s, none, limits, scale, sizeof(T) == 2 ? kProbShift : 0.f, lg);
+  softmax_step<DH, NQ, 2, false, FAR, sizeof(T) == 4>(st, far, s, none, limits, scale, sizeof(T) == 2 ? kProbShift : 0.f, lg);
 
   uint32_t vexp = __builtin_amdgcn_ubfe(t.ve, 8 * lg, 8);
   if (!full) clear_invisible(t.v, vexp, limit, lg);
@@ -345,7 +349,7 @@ __device__ __forceinline__ void shared_tiles(Acc<DH, NQ> &st, uint64_t &far, con
         for (int qt = 0; qt < NQ; ++qt) s[qt][2 * t + e] = mfma16x16x32(a, qf[qt].x[k][0], s[qt][2 * t + e]);
       }
   const int none[NQ] = {};
-  softmax_step<DH, NQ, 2 * N, false, false>(st, far, s, none, limit, scale, kProbShift, lane >> 4);
+  softmax_step<DH, NQ, 2 * N, false, false, false>(st, far, s, none, limit, scale, kProbShift, lane >> 4);
 #pragma unroll
   for (int t = 0; t < N; ++t) {
     u32x4 pf[NQ];
@@ -459,7 +463,7 @@ __device__ __forceinline__ bool block_tile(Acc<DH, NQ> &st, uint64_t &far, Block
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) cap[qt] = row_pos[qt] - kTile * u;
   const int limits[1] = {p.w - kTile * u};
-  softmax_step<DH, NQ, 2, true, FAR>(st, far, s, cap, limits, p.scale_log2, sizeof(T) == 2 ? kProbShift : 0.f, lg);
+  softmax_step<DH, NQ, 2, true, FAR, sizeof(T) == 4>(st, far, s, cap, limits, p.scale_log2, sizeof(T) == 2 ? kProbShift : 0.f, lg);
 
   // the largest magnitude's bits tell whether any is late
   typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -547,7 +551,7 @@ __device__ __forceinline__ void late_values(Acc<DH, NQ> &st, bool far, const flo
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         const float x = far ? s[qt][e][v] - st.neg[qt] : s[qt][e][v];
-        s[qt][e][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x, p.scale_log2, far ? 0.f : -m[qt]));
+        s[qt][e][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(x, p.scale_log2, far ? 0.f : -m[qt])) * kBySlack;
       }
     dst[0] = s[qt][0], dst[1] = s[qt][1];
   }
@@ -629,7 +633,7 @@ __device__ __forceinline__ void write_output_row(const AttnQ8Params &p, int b, i
     store_out4(out + 32 * k + 8 * lg + 4, hi);
   }
   if (lg == 0 && p.lse)
-    p.lse[(static_cast<size_t>(b) * p.hq + h) * p.w + pos] = (m + log2f(l)) * 0.69314718055994530942f;
+    p.lse[(static_cast<size_t>(b) * p.hq + h) * p.w + pos] = (m + log2f(l * kFromSlack)) * 0.69314718055994530942f;
 }
 
 // Shared memory of a workgroup.
@@ -958,7 +962,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
       prefix_tile<T, DH, NQ, true>(st, far, t, qf, visible, p.scale_log2, ln, lg);
     }
   }
-  // From here on l and o are the plain ones, unnormalised, without shifts.
+  // From here on l and o are the plain ones, unnormalised, without shifts but kSlack.
   constexpr float kShift = sizeof(T) == 2 ? kProbShift : 0.f;
   float m[NQ];
 #pragma unroll
@@ -967,13 +971,13 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
             : st.neg[qt] == kNoRef ? kNegInf : kShift - st.neg[qt];
     st.l[qt] = group_sum(st.l[qt]);
     if constexpr (sizeof(T) == 2) {
-      st.l[qt] *= 0x1p-9f;
-      static_assert(kProbShift == 9.f, "the shift that is taken back");
+      st.l[qt] *= 0x1p-15f;
+      static_assert(kProbShift + kSlack == 15.f, "the shift that is taken back");
 #pragma unroll
       for (int dt = 0; dt < DH / 16; ++dt)
 #pragma unroll
         for (int v = 0; v < 4; ++v)
-          st.o[qt][dt][v] = __builtin_amdgcn_ldexpf(st.o[qt][dt][v], st.vref - 9);
+          st.o[qt][dt][v] = __builtin_amdgcn_ldexpf(st.o[qt][dt][v], st.vref - 15);
     }
   }
   if (late) {
@@ -1057,7 +1061,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
                  o * (1.f / den));
       if (p.lse && c == 0)
         p.lse[(static_cast<size_t>(b) * p.hq + h) * p.w + pos] =
-            (m2 + log2f(den)) * 0.69314718055994530942f;
+            (m2 + log2f(den * kFromSlack)) * 0.69314718055994530942f;
     }
   }
 }
@@ -1145,7 +1149,7 @@ __global__ __launch_bounds__(64 * kWavesQ8) void attn_q8_combine_kernel(AttnQ8Pa
   store_out4(static_cast<T *>(p.out) + ((static_cast<size_t>(b) * p.w + pos) * p.hq + h) * DH + c,
              o * (1.f / den));
   if (p.lse && c == 0)
-    p.lse[(static_cast<size_t>(b) * p.hq + h) * p.w + pos] = (mx + log2f(den)) * 0.69314718055994530942f;
+    p.lse[(static_cast<size_t>(b) * p.hq + h) * p.w + pos] = (mx + log2f(den * kFromSlack)) * 0.69314718055994530942f;
 }
 
 template <typename T, int DH, int NQ, int RW>

@@ -114,3 +114,29 @@ def test_large_logits_and_block_values(shape):
         ref, _, a, _ = attention(host, table, lens, b, 0, 0, 0, q, kb, vb)
         tol = tolerance(dtype, ref, a, 0.0, lens[b] + w, dh)
         assert (np.abs(out[b].double().cpu().numpy() - ref) <= tol).all(), b
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=ids)
+def test_values_up_to_the_largest(shape):
+    """Two prefix values of 1.5 * 2^126 whose logits pass those that a wave has met before by
+    a few binary orders: their sum is 3/4 of the largest fp32. Weights 2^3.5 or more against at
+    most 190 of 1: the two have a tenth of the sum, the output is over 2^123."""
+    dtype, dh, G, w = shape
+    lens = [128, 128]
+    cache, batch, table = random_cache(7, dtype, 2, 2, dh, lens)
+    q = torch.zeros((2, w, 2 * G, dh), dtype=dtype, device=DEV)
+    kb = torch.zeros((2, w, 2, dh), dtype=dtype, device=DEV)
+    q[..., 0] = 8
+    for pool in (cache.k_pool, cache.v_pool):
+        pool.view(torch.uint8).zero_()
+    cache.k_exp.fill_(127)
+    cache.v_exp.fill_(63)
+    tiles = (2 - (w + 31) // 32, 4 - (w + 31) // 32)
+    for b in range(2):
+        for t in (32 * i + 5 for i in tiles):
+            page, group, j = int(table[b, t // 64]), t % 64 // 8, t % 8
+            cache.k_pool.view(torch.uint8)[0, 0, :, page, group, int(key_bytes(dh)[j, 0])] = 0x46  # 3.5
+            cache.v_pool.view(torch.uint8)[0, 0, :, page, group, :, j] = 0x74  # 192
+            cache.v_exp[0, 0, page, :, group] = 119 + 127
+    out = check(cache, batch, table, lens, q, kb, torch.ones_like(kb), 2.0 ** 126)
+    assert bool((out.float() > 2.0 ** 123).all())
