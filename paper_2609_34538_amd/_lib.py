@@ -504,29 +504,27 @@ def _empty_on(stream, shape, dtype, device) -> torch.Tensor:
 
 class _Call:
     """A library call with its arguments marshalled: calling it enqueues it on `stream`
-    (None: the current stream of the tensors' device) with that device current. The
-    tensors are kept alive."""
+    (None: the stream of the tensors' device that is current when it is called, also one
+    that is being captured) with that device current. The tensors are kept alive."""
 
     def __init__(self, fn, name: str, args, keep, device: torch.device, stream):
-        self._fn, self._name, self._keep = fn, name, keep
+        self._fn, self._name, self._args, self._keep = fn, name, args, keep
         self._index = device.index if device.type == "cuda" else None
-        handle = 0
-        if self._index is not None:
-            if stream is None:
-                stream = torch.cuda.current_stream(device)
-            elif stream.device != device:
-                raise ValueError(f"the stream must be one of {device}")
-            handle = stream.cuda_stream
-        self._args = (*args, handle)
+        if self._index is not None and stream is not None and stream.device != device:
+            raise ValueError(f"the stream must be one of {device}")
+        self._stream = stream
 
     def __call__(self):
         if self._index is None:
             raise ValueError(f"{self._name} takes tensors on a GPU")
+        # the raw handle, without making a Stream of it
+        handle = (torch._C._cuda_getCurrentRawStream(self._index) if self._stream is None
+                  else self._stream.cuda_stream)
         if torch.cuda.current_device() != self._index:
             with torch.cuda.device(self._index):
-                st = self._fn(*self._args)
+                st = self._fn(*self._args, handle)
         else:
-            st = self._fn(*self._args)
+            st = self._fn(*self._args, handle)
         if st != DAS_OK:
             raise DasError(st, self._name)
 
