@@ -614,6 +614,12 @@ class QuantCache:
         return self._c
 
 
+def _tensors_of(cache: QuantCache, batch: Batch):
+    """What a call's marshalled structs point to, whatever the objects hold later."""
+    return (cache.k_pool, cache.v_pool, cache.k_exp, cache.v_exp, batch.prefix_len,
+            batch.block_table, batch.dev_error)
+
+
 def _check_batch_on(batch: Batch, device):
     if batch.prefix_len.device != device or batch.block_table.device != device:
         raise ValueError(f"prefix_len and block_table must be on {device}")
@@ -654,7 +660,8 @@ class PreparedAttentionQ8(_Call):
                 _check_opt(lse, torch.float32, (B, hq, w), dev, "lse"),
                 workspace.data_ptr(), workspace.numel())
         super().__init__(LIB.das_attn_q8, "das_attn_q8", args,
-                         (cache, batch, q, k_blk, v_blk, out, workspace, lse), dev, stream)
+                         (*_tensors_of(cache, batch), q, k_blk, v_blk, out, workspace, lse), dev,
+                         stream)
 
 
 def attn_policy_q8(cache: QuantCache, batch: Batch, layer: int, kappa: int, nu: int,
@@ -689,7 +696,7 @@ class PreparedAppendQ8(_Call):
                 _check(num_new, torch.int32, (batch.batch,), dev, "num_new"),
                 _check_opt(len_out, torch.int32, (batch.batch,), dev, "len_out"))
         super().__init__(LIB.das_kv_append_q8, "das_kv_append_q8", args,
-                         (cache, batch, k_new, v_new, num_new, len_out), dev, stream)
+                         (*_tensors_of(cache, batch), k_new, v_new, num_new, len_out), dev, stream)
 
 
 def kv_append_q8(cache: QuantCache, batch: Batch, k_new: torch.Tensor, v_new: torch.Tensor,
