@@ -398,7 +398,8 @@ das_status das_attn_q8(const das_cache_q8 *cache, const das_batch *batch, int32_
 
 /*
  * das_kv_append into an 8-bit cache. Arguments as for das_kv_append, with k_new and
- * v_new in base.dtype.
+ * v_new in base.dtype; len_out must share no element with batch->prefix_len or num_new
+ * (DAS_ERR_SHAPE).
  *
  * A group without earlier tokens of the sequence gets the smallest exponent e in
  * -64..119 with |x| <= 448 * 2^e for its new finite elements. A group with earlier

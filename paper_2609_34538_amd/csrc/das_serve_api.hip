@@ -14,6 +14,12 @@ namespace {
 
 bool aligned(const void *ptr, size_t a) { return reinterpret_cast<uintptr_t>(ptr) % a == 0; }
 
+// Whether two arrays of `bytes` bytes share any.
+bool overlap(const void *a, const void *b, size_t bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y ? y - x < bytes : x - y < bytes;
+}
+
 das_status check_cache(const das_cache_q8 *cache) {
   if (!cache) return DAS_ERR_NULL;
   const das_cache *c = &cache->base;
@@ -187,7 +193,9 @@ das_status das_kv_append_q8(const das_cache_q8 *cache, const das_batch *batch, c
   const long long blocks =
       (c->num_k_planes * per_plane + 3) / 4 + (c->num_v_planes * per_plane + 3) / 4;
   if (blocks * 256 > 0xffffffffLL) return DAS_ERR_SHAPE;
-  if (len_out && static_cast<const void *>(len_out) == static_cast<const void *>(batch->prefix_len))
+  // every workgroup of a sequence reads its length and count, one of them writes len_out
+  const size_t per_seq = sizeof(int32_t) * static_cast<size_t>(batch->batch);
+  if (len_out && (overlap(len_out, batch->prefix_len, per_seq) || overlap(len_out, num_new, per_seq)))
     return DAS_ERR_SHAPE;
   AppendQ8Params p;
   p.k_new = k_new;
