@@ -598,7 +598,7 @@ __device__ __forceinline__ void write_record_row(uint8_t *rec, int rows, int row
 #pragma unroll
       for (int v = 0; v < 4; ++v) amax = fmaxf(amax, fabsf(o[dt][v]));
     amax = group_max(amax) * inv;
-    const int e = (amax > 0.f && amax < __builtin_huge_valf()) ? __builtin_amdgcn_frexp_expf(amax) - 15 : 0;
+    const int e = record_exponent(amax);
     sc = __builtin_amdgcn_ldexpf(inv, -e);
     q = __builtin_amdgcn_ldexpf(l, e);
   }

@@ -131,6 +131,12 @@ template <typename T> struct RecVec;
 template <> struct RecVec<bf16_t> { typedef h16x4 type; };
 template <> struct RecVec<float> { typedef f32x4 type; };
 
+// The exponent e of a bf16 row's record for results of up to amax: these times 2^-e lie in
+// [2^14, 2^15), but under 2^-105, where 2^-e * (1 / l) with l of 2^-6 or more has to fit fp32.
+__device__ __forceinline__ int record_exponent(float amax) {
+  return (amax > 0.f && amax < __builtin_huge_valf()) ? max(__builtin_amdgcn_frexp_expf(amax) - 15, -120) : 0;
+}
+
 // One query row of a piece record (piece_record_bytes); the merge takes the
 // row's unnormalised output as the stored values times q.
 // bf16 caches: the row's normalised output O / l in fp16, scaled by 2^-e so
@@ -157,7 +163,7 @@ __device__ __forceinline__ void write_piece_row(uint8_t *rec, int rows, int row,
 #pragma unroll
       for (int v = 0; v < 4; ++v) amax = fmaxf(amax, fabsf(o[dt][v]));
     amax = group_max(amax) * inv;
-    const int e = (amax > 0.f && amax < __builtin_huge_valf()) ? __builtin_amdgcn_frexp_expf(amax) - 15 : 0;
+    const int e = record_exponent(amax);
     const float sc = __builtin_amdgcn_ldexpf(inv, -e);
     _Float16 *orow = reinterpret_cast<_Float16 *>(rec) + row * DH;
 #pragma unroll
@@ -189,7 +195,7 @@ __device__ __forceinline__ void write_piece_item(uint8_t *rec, int rows, int row
   } else {
     const float inv = l > 0.f ? 1.f / l : 0.f;
     bound *= inv;
-    const int e = (bound > 0.f && bound < __builtin_huge_valf()) ? __builtin_amdgcn_frexp_expf(bound) - 15 : 0;
+    const int e = record_exponent(bound);
     const float sc = __builtin_amdgcn_ldexpf(inv, -e);
     *reinterpret_cast<h16x4 *>(rec + at * 2) =
         h16x4{static_cast<_Float16>(o[0] * sc), static_cast<_Float16>(o[1] * sc),
