@@ -30,9 +30,11 @@
 // has met (vref, per wave), which like the running maximum rescales the output
 // when it grows, by a power of two. Draft-block values are bf16 with bf16's range:
 // their probabilities enter as a bf16 and its remainder, two products. Sums are in units of
-// 2^vref / 2^9, down to 2^-73, which a block value past 2^40 could take past the largest
-// fp32: those, as what is not finite, are left out of the products and added one by one at
-// the end, when the sums are plain, to the rows that see them (kLate).
+// 2^vref / 2^9, of 2^-73 or more after a block, which a value past 2^40 could take past the
+// largest fp32: those, as what is not finite, are left out of the products and added one by
+// one at the end, when the sums are plain, to the rows that see them (kLate). Waves without
+// a block, and blocks whose values all lie under 2^-40, start in units of 2^-111, so that
+// caches of the smallest scales keep their values.
 // fp32 calls use v_mfma_f32_16x16x4_f32 for both products; reduction slots may be
 // numbered freely as long as both operands agree, so the same pieces serve: step i
 // takes a lane's i-th dim or token.
@@ -58,6 +60,9 @@ constexpr int kWavesQ8 = 4;
 // over 1, so that a sum passes the largest fp32 only where the values' does.
 constexpr float kSlack = 6.f;
 constexpr float kProbShift = 9.f;
+// Exponent of a wave's units at first: probabilities of 2^15 in them fit fp32, and the
+// smallest codes of the smallest scale, 2^-9 * 2^-126, are 2^-24 of it, fp16's smallest.
+constexpr int kLowUnit = -111;
 constexpr float kBySlack = 0x1p-6f, kFromSlack = 0x1p6f;  // 2^-kSlack, 2^kSlack
 constexpr float kNoRef = 3e38f;  // in place of shift - reference: nothing seen yet
 // A reference past this (in base-2 units) is far: the rounding of reference * scale would be
@@ -451,11 +456,12 @@ __device__ __forceinline__ void block_logits(f32x4 (&s)[NQ][2], const Block<T, D
       }
 }
 
-// Tile u of the draft block through both products. True if values of it are left to
-// late_values.
+// Tile u of the draft block through both products, `first`: the wave's first tile. True if
+// values of it are left to late_values.
 template <typename T, int DH, int NQ, bool FAR = false>
 __device__ __forceinline__ bool block_tile(Acc<DH, NQ> &st, uint64_t &far, Block<T, DH> &t, const AttnQ8Params &p, int u,
-                                           const QFrag<T, DH> (&qf)[NQ], const int (&row_pos)[NQ], int lg) {
+                                           bool first, const QFrag<T, DH> (&qf)[NQ], const int (&row_pos)[NQ],
+                                           int lg) {
   constexpr int KS = DH / 32;
   f32x4 s[NQ][2];
   block_logits<T, DH, NQ>(s, t, qf);
@@ -489,6 +495,11 @@ __device__ __forceinline__ bool block_tile(Acc<DH, NQ> &st, uint64_t &far, Block
         for (int h = 0; h < Block<T, DH>::W; ++h) t.v[k][j][h] = without_late<T>(t.v[k][j][h]);
   }
   if constexpr (sizeof(T) == 2) {
+    constexpr uint32_t kSmall = (127u - 40) << 7;  // bits of 2^-40
+    if (__builtin_amdgcn_ballot_w64(most32 >= kSmall) != 0) {
+      if (first) st.vref = kQ8MinExp;
+      else raise_vref(st, kQ8MinExp);
+    }
     u32x4 hi[NQ], lo[NQ];
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt)
@@ -728,7 +739,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
   Acc<DH, NQ> st;
   uint64_t far = 0;  // lanes of rows that have met a far reference
   auto clear = [&](float neg) {
-    st.vref = kQ8MinExp;
+    st.vref = kLowUnit;
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
       st.neg[qt] = neg;
@@ -785,10 +796,10 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     int i = n_block;
     int la = load(i, ta);
     if (has_block) {
-      late = block_tile<T, DH, NQ>(st, far, blk, p, g0, qf, row_pos, lg);
+      late = block_tile<T, DH, NQ>(st, far, blk, p, g0, true, qf, row_pos, lg);
       for (int k = 1; k < n_block; ++k) {
         load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
-        late |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * k, qf, row_pos, lg);
+        late |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * k, false, qf, row_pos, lg);
       }
     }
     int lb = load(i + 1, tb);
@@ -811,7 +822,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     u32x4 raw[TPS][LPW];
     uint32_t ke[TPS], ve[TPS];
     int limit[TPS], ahead[TPS];
-    int vref = st.vref;
+    int vref;
     // always issued, past the last tile from empty buffers
     auto load = [&](int step) {
 #pragma unroll
@@ -865,8 +876,9 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     };
     for (int k = 0; k < n_block; ++k) {
       if (k > 0) load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
-      late |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * k, qf, row_pos, lg);
+      late |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * k, k == 0, qf, row_pos, lg);
     }
+    vref = st.vref;
     load(0);  // not ahead of the block: registers
     convert(0);
     load(1);
@@ -920,7 +932,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     for (int s = 0; s < NB - 1; ++s) issue(s);
     for (int s = 0; s < n_block; ++s) {
       if (s > 0) load_block<T, DH>(blk, p, b, kvh, g0 + IW * s, ln, lg);
-      late |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * s, qf, row_pos, lg);
+      late |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * s, s == 0, qf, row_pos, lg);
     }
 #pragma unroll 1
     for (int s = 0; s < steps; ++s) {
@@ -952,7 +964,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     clear(kLowest);
     for (int k = 0; k < n_block; ++k) {
       load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
-      late |= block_tile<T, DH, NQ, true>(st, far, blk, p, g0 + IW * k, qf, row_pos, lg);
+      late |= block_tile<T, DH, NQ, true>(st, far, blk, p, g0 + IW * k, k == 0, qf, row_pos, lg);
     }
     window = load_window(0);
 #pragma unroll 1

@@ -27,7 +27,11 @@ def check(cache, batch, table, lens, q, kb, vb, unit=1.0):
     host = HostCache(cache)
     for b in range(len(lens)):
         ref, _, a, size = attention(host, table, lens, b, 0, 0, 0, q, kb, vb)
-        tol = tolerance(cache.dtype, ref / unit, a / unit, size, lens[b] + q.shape[1], q.shape[3])
+        n = lens[b] + q.shape[1]
+        tol = tolerance(cache.dtype, ref / unit, a / unit, size, n, q.shape[3])
+        # under the smallest normal: half a step of bf16; half steps of fp32 in each sum, whose
+        # weights add up to 2^-6 or more
+        tol += (2.0 ** -134 if cache.dtype == BF16 else (n + 2) * 2.0 ** -144) / unit
         err = np.abs(out[b].double().cpu().numpy() - ref) / unit
         assert (err <= tol).all(), (b, lens[b], float((err / tol).max()))
     return out
@@ -140,3 +144,21 @@ def test_values_up_to_the_largest(shape):
             cache.v_exp[0, 0, page, :, group] = 119 + 127
     out = check(cache, batch, table, lens, q, kb, torch.ones_like(kb), 2.0 ** 126)
     assert bool((out.float() > 2.0 ** 123).all())
+
+
+@pytest.mark.parametrize("block", ["zero", "tiny", "alike"])
+@pytest.mark.parametrize("lens", [[40, 1], [4000, 700]], ids=["one-chunk", "chunks"])
+@pytest.mark.parametrize("shape", SHAPES, ids=ids)
+@pytest.mark.parametrize("byte", [1, 8, 20, 38, 62, 247])
+def test_scales_of_any_size(byte, shape, lens, block):
+    """A cache whose values all have one exponent byte, down to the smallest, and one past
+    what the commit gives; block values of 0, of 2^-100, and of the cache's size."""
+    dtype, dh, G, w = shape
+    cache, batch, table = random_cache(7, dtype, 2, 2, dh, lens)
+    cache.v_exp.copy_(torch.where(cache.v_exp == 255, cache.v_exp, torch.full_like(cache.v_exp, byte)))
+    if byte > 246:  # codes under 1: thousands of values whose sum fits fp32
+        codes = cache.v_pool.view(torch.uint8)
+        codes.copy_(torch.where(codes & 0x7f == 0x7f, codes, codes & 0x9f))
+    q, kb, vb = _block(11, dtype, 2, w, 2 * G, 2, dh)
+    vb *= {"zero": 0.0, "tiny": 2.0 ** -100, "alike": 2.0 ** (byte - 127)}[block]
+    check(cache, batch, table, lens, q, kb, vb, max(2.0 ** (byte - 127), float(vb.abs().max())))
