@@ -33,8 +33,9 @@
 // 2^vref / 2^9, of 2^-73 or more after a block, which a value past 2^40 could take past the
 // largest fp32: those, as what is not finite, are left out of the products and added one by
 // one at the end, when the sums are plain, to the rows that see them (kLate). Waves without
-// a block, and blocks whose values all lie under 2^-40, start in units of 2^-111, so that
-// caches of the smallest scales keep their values.
+// a block start in units of 2^-111, and one whose block lies under 2^-40 and which has met no
+// scale over 2^-64 goes through its tiles again so: caches of the smallest scales keep their
+// values.
 // fp32 calls use v_mfma_f32_16x16x4_f32 for both products; reduction slots may be
 // numbered freely as long as both operands agree, so the same pieces serve: step i
 // takes a lane's i-th dim or token.
@@ -456,12 +457,12 @@ __device__ __forceinline__ void block_logits(f32x4 (&s)[NQ][2], const Block<T, D
       }
 }
 
-// Tile u of the draft block through both products, `first`: the wave's first tile. True if
-// values of it are left to late_values.
+// Tile u of the draft block through both products. What its values are: kHasLate, some are
+// left to late_values; kHasLarge, some are 2^-40 or more (bf16 calls).
+constexpr uint32_t kHasLate = 1, kHasLarge = 2;
 template <typename T, int DH, int NQ, bool FAR = false>
-__device__ __forceinline__ bool block_tile(Acc<DH, NQ> &st, uint64_t &far, Block<T, DH> &t, const AttnQ8Params &p, int u,
-                                           bool first, const QFrag<T, DH> (&qf)[NQ], const int (&row_pos)[NQ],
-                                           int lg) {
+__device__ __forceinline__ uint32_t block_tile(Acc<DH, NQ> &st, uint64_t &far, Block<T, DH> &t, const AttnQ8Params &p, int u,
+                                           const QFrag<T, DH> (&qf)[NQ], const int (&row_pos)[NQ], int lg) {
   constexpr int KS = DH / 32;
   f32x4 s[NQ][2];
   block_logits<T, DH, NQ>(s, t, qf);
@@ -495,11 +496,6 @@ __device__ __forceinline__ bool block_tile(Acc<DH, NQ> &st, uint64_t &far, Block
         for (int h = 0; h < Block<T, DH>::W; ++h) t.v[k][j][h] = without_late<T>(t.v[k][j][h]);
   }
   if constexpr (sizeof(T) == 2) {
-    constexpr uint32_t kSmall = (127u - 40) << 7;  // bits of 2^-40
-    if (__builtin_amdgcn_ballot_w64(most32 >= kSmall) != 0) {
-      if (first) st.vref = kQ8MinExp;
-      else raise_vref(st, kQ8MinExp);
-    }
     u32x4 hi[NQ], lo[NQ];
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt)
@@ -538,7 +534,8 @@ __device__ __forceinline__ bool block_tile(Acc<DH, NQ> &st, uint64_t &far, Block
           for (int qt = 0; qt < NQ; ++qt)
             st.o[qt][2 * k + h] = mfma16x16x4(t.v[k][j][h], __float_as_uint(s[qt][j / 4][j % 4]), st.o[qt][2 * k + h]);
   }
-  return any_late;
+  constexpr uint32_t kLarge = (127u - 40) << 7;  // bits of 2^-40
+  return (any_late ? kHasLate : 0) | (__builtin_amdgcn_ballot_w64(most32 >= kLarge) != 0 ? kHasLarge : 0);
 }
 
 // The late values of tile u of the draft block, for the rows that see them (in a product
@@ -738,8 +735,8 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
 
   Acc<DH, NQ> st;
   uint64_t far = 0;  // lanes of rows that have met a far reference
-  auto clear = [&](float neg) {
-    st.vref = kLowUnit;
+  auto clear = [&](float neg, int vref) {
+    st.vref = vref;
 #pragma unroll
     for (int qt = 0; qt < NQ; ++qt) {
       st.neg[qt] = neg;
@@ -748,7 +745,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
       for (int dt = 0; dt < DH / 16; ++dt) st.o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
-  clear(kNoRef);
+  clear(kNoRef, has_block ? kQ8MinExp : kLowUnit);
 
   const uint32_t lane_k = (ln >> 2) * 8 * DH + lg * 64 + (ln & 3) * 16;
   const uint32_t lane_v = lg * 8 * DH + ln * 16;
@@ -769,7 +766,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     return ok ? min(kTile, S - kTile * tile) : 0;
   };
   const int n_block = g0 < nb ? min((nb - g0 + IW - 1) / IW, n) : 0;  // the wave's block tiles
-  bool late = false;                                                  // they have late values
+  uint32_t block = 0;                                                 // what they hold
 
   // The wave's i-th tile into registers. Past the last tile the loads go to empty buffers:
   // they are always issued, so that the compiler can count them, and waits for one tile leave
@@ -796,10 +793,10 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     int i = n_block;
     int la = load(i, ta);
     if (has_block) {
-      late = block_tile<T, DH, NQ>(st, far, blk, p, g0, true, qf, row_pos, lg);
+      block = block_tile<T, DH, NQ>(st, far, blk, p, g0, qf, row_pos, lg);
       for (int k = 1; k < n_block; ++k) {
         load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
-        late |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * k, false, qf, row_pos, lg);
+        block |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * k, qf, row_pos, lg);
       }
     }
     int lb = load(i + 1, tb);
@@ -822,7 +819,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     u32x4 raw[TPS][LPW];
     uint32_t ke[TPS], ve[TPS];
     int limit[TPS], ahead[TPS];
-    int vref;
+    int vref = st.vref;
     // always issued, past the last tile from empty buffers
     auto load = [&](int step) {
 #pragma unroll
@@ -876,9 +873,8 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     };
     for (int k = 0; k < n_block; ++k) {
       if (k > 0) load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
-      late |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * k, k == 0, qf, row_pos, lg);
+      block |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * k, qf, row_pos, lg);
     }
-    vref = st.vref;
     load(0);  // not ahead of the block: registers
     convert(0);
     load(1);
@@ -932,7 +928,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     for (int s = 0; s < NB - 1; ++s) issue(s);
     for (int s = 0; s < n_block; ++s) {
       if (s > 0) load_block<T, DH>(blk, p, b, kvh, g0 + IW * s, ln, lg);
-      late |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * s, s == 0, qf, row_pos, lg);
+      block |= block_tile<T, DH, NQ>(st, far, blk, p, g0 + IW * s, qf, row_pos, lg);
     }
 #pragma unroll 1
     for (int s = 0; s < steps; ++s) {
@@ -959,12 +955,14 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     __syncthreads();  // the ring has been read
   }
 
-  const bool again = far != 0;
-  if (again) {  // far references: the wave by itself, one tile after the other
-    clear(kLowest);
+  // far references, or values of small scales alone: the wave by itself, one tile after the other
+  const bool low = sizeof(T) == 2 && !(block & kHasLarge);
+  const bool again = far != 0 || (low && st.vref == kQ8MinExp && n_block > 0 && n > n_block);
+  if (again) {
+    clear(kLowest, low ? kLowUnit : kQ8MinExp);
     for (int k = 0; k < n_block; ++k) {
       load_block<T, DH>(blk, p, b, kvh, g0 + IW * k, ln, lg);
-      late |= block_tile<T, DH, NQ, true>(st, far, blk, p, g0 + IW * k, k == 0, qf, row_pos, lg);
+      block |= block_tile<T, DH, NQ, true>(st, far, blk, p, g0 + IW * k, qf, row_pos, lg);
     }
     window = load_window(0);
 #pragma unroll 1
@@ -992,7 +990,7 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
           st.o[qt][dt][v] = __builtin_amdgcn_ldexpf(st.o[qt][dt][v], st.vref - 15);
     }
   }
-  if (late) {
+  if (block & kHasLate) {
     float *probs = reinterpret_cast<float *>(smem + L::PROBS + wave * L::PROB_STRIDE);
     for (int k = 0; k < n_block; ++k)
       late_values<T, DH, NQ>(st, again, m, p, b, kvh, g0 + IW * k, qf, row_pos, probs, ln, lg);
