@@ -363,9 +363,9 @@ das_status das_greedy_accept(int32_t batch, int32_t block_len, const int32_t *pr
  *
  * base.dtype is the type of queries, block K/V, outputs and committed K/V; the
  * other fields of `base` are as in das_cache. Pools are 16-byte aligned, exponent
- * arrays 4-byte aligned. Half the bytes of a bf16 cache (a 1/128 of them more or
- * less for the exponents), so half the time of a call that is bound by them.
- * Places that hold no token of a sequence (behind its length) may hold anything.
+ * arrays 4-byte aligned. Half the bytes of a bf16 cache, and one exponent to 8 *
+ * head_dim codes, so half the time of a call that is bound by them. Places that hold no
+ * token of a sequence (behind its length) may hold anything.
  */
 typedef struct das_cache_q8 {
   das_cache base;
@@ -381,9 +381,13 @@ typedef struct das_cache_q8 {
  *
  * Numerics: elements are exact in the products' types. bf16 calls multiply values
  * in fp16 with probabilities of 11 bits; a group's values below 2^-24 of the largest
- * scale's unit met so far round there. fp32 calls multiply in fp32. Accumulation and
- * softmax statistics are fp32; sums are divided last, so that values whose sum over
- * the positions passes the largest fp32 give infinities. lse as for das_attn_policy.
+ * scale's unit met so far round there (beside a block with values of 2^-40 and more,
+ * below 2^-88 at least). Block values keep bf16's range. fp32 calls multiply in fp32.
+ * Accumulation and softmax statistics are fp32, for logits of any finite size; sums are
+ * divided last, so that values whose sum over the positions passes the largest fp32
+ * give infinities. Sequences that are cut into parts are joined from the parts' results,
+ * in bf16 calls from fp16 relative to each row's largest: what is under 2^-39 of it in
+ * its part is lost. lse as for das_attn_policy.
  *
  * das_attn_q8_workspace_bytes returns 0 for arguments that das_attn_q8 rejects; the
  * workspace is 256-byte aligned, needs no init, and calls that run concurrently need
@@ -450,8 +454,9 @@ das_status das_kv_append_q8(const das_cache_q8 *cache, const das_batch *batch, c
  *   dev_error    optional device word
  *
  * batch in 1..65535, block_len in 1..DAS_MAX_BLOCK, vocab in 1..DAS_MAX_VOCAB. Logits
- * are aligned to their type, the other arrays to 4 bytes. Results do not depend on
- * the order of the work: equal calls give equal bits.
+ * are aligned to their type, the other arrays to 4 bytes; tokens and probs must not
+ * overlap the inputs or each other. Results do not depend on the order of the work:
+ * equal calls give equal bits.
  */
 das_status das_sample(int32_t batch, int32_t block_len, int32_t vocab, int32_t dtype,
                       const void *logits, int64_t row_stride, const float *temperature,

@@ -9,11 +9,13 @@
 // records that a second kernel merges. Up to 16 * NQ rows a wave has tiles of its own,
 // from memory into registers, two on the way; waves that share a tile get it from LDS.
 //
-// Bound by HBM for few rows (24 x 8 KV heads x 1-4099 tokens, one query token, dh 128:
-// 26 us, 3.8 TB/s; 32 x 55 heads x 32 rows, dh 96, 2.1 GB: 358 us, 5.9 TB/s, what a copy
-// reaches), for many by the vector and matrix work of a tile, which two waves per SIMD do
-// not overlap wholly (4 x 8 KV heads x 128 rows, dh 128, 137 MB: 59 us, 580 TFLOP/s; 31
-// matrix instructions and 170 vector ones a tile and wave).
+// Bound by HBM for few rows (32 x 55 heads x 32 rows, dh 96, 2.1 GB: 350 us, 6.1 TB/s) or
+// by the longest unit's workgroup (24 x 8 KV heads x 1-4099 tokens, one query token, dh 128:
+// 25 us, 4.0 TB/s), for many by the vector and matrix work of a tile, which two waves per
+// SIMD do not overlap wholly (4 x 8 KV heads x 128 rows, dh 128, 137 MB: 60 us, 575
+// TFLOP/s; 32 matrix instructions and 140 others on vectors a tile and wave). fp32 calls are
+// bound by the fp32 matrix rate for many rows (4 x 8 KV heads x 128 rows x 4096 tokens, dh
+// 128: 99 us, 87 TFLOP/s; 16 x 55 heads x 16 rows x 512-4096, dh 96: 119 us, 105 TFLOP/s).
 //
 // Both products take the key / value tile as the A operand, as in mfma_tile.h:
 //   S^T (tokens x rows) = K . Q^T,   O^T (dh x rows) += V^T . P^T
@@ -811,8 +813,8 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
     // into registers, a step ahead, and writes them converted to LDS, from where all multiply.
     // One barrier a step publishes step s and frees the slot of step s - 1, which step s + 1
     // takes. All know the exponents, and with them the same vref. Codes in LDS, converted by
-    // every wave, took 250 vector instructions a tile instead of 170 (128 rows 64 -> 59 us,
-    // dh 64 49 -> 43); three waves per SIMD spill (133 us).
+    // every wave, took 250 vector instructions a tile instead of 170, its 32 matrix ones
+    // included (128 rows 64 -> 59 us, dh 64 49 -> 43); three waves per SIMD spill (133 us).
     constexpr int TPS = L::TPS, LPW = (2 * KS + RW - 1) / RW;
     const int np = n - n_block;  // this wave's prefix tiles
     const int steps = (g_end - chunk * p.chunk_tiles + IW * TPS - 1) / (IW * TPS);  // of every wave

@@ -17,7 +17,7 @@
 // the 8 tokens of two dims, 16 bytes of the page. Bound by the waves' dependent round trips
 // and their instructions (bf16 goes into the conversions packed, the largest magnitude is
 // taken on the bits): 32 + 32 planes x 4 layers x 55 heads x 8 tokens 17 us, 6 planes x 4 x
-// 55 x 32 sequences x 0-32 tokens 66 us (2.9 TB/s). Measured and not kept: the loads of one
+// 55 x 32 sequences x 0-32 tokens 60-63 us (3.2 TB/s); from fp32 19 and 83 us (3.9 TB/s). Measured and not kept: the loads of one
 // or two groups ahead (22 and 29 us on the first, 81 and 108 on the second: more registers
 // and instructions for groups that most waves do not have), a wave per group (22, 110).
 

@@ -12,7 +12,7 @@
 //
 // One workgroup per row (the call has no workspace to join parts of one through); the
 // first pass reads memory, later ones the caches. What bounds it is a pass's vector and
-// LDS work on one compute unit, not HBM: 1024 rows of 65536 bf16 logits take 74 us, 1.8
+// LDS work on one compute unit, not HBM: 1024 rows of 65536 bf16 logits take 70 us, 1.9
 // TB/s. No row is sorted.
 // - bf16 rows (sample_values) are counted by value in LDS; counts, one exponential per
 //   value and a scan give every cut, a second pass adds up the looked-up weights of every
@@ -666,7 +666,9 @@ __device__ __forceinline__ float bin_value(int bin) {
 // exponential per value, every sum; the last pass looks its weights up. Returns false
 // (having done nothing) for rows out of that range: a largest logit of 2^7 or more, or
 // within 2^-9 of 0, weights that matter below -2^7, many tokens within 2^-9 of 0, or a
-// cut there.
+// cut there. Those take the other way a token a lane at a time: 64 rows of 65536 logits
+// without a filter 23 us here, 61 at temperature 30, 65 with 5536 tokens at 0, 102 with all
+// logits around 130; with top-p 0.9 26, 133 and 356; 1024 rows 70, 296 and 397 us.
 template <int THREADS>
 __device__ bool sample_values(const SampleParams &p, const bf16_t *row, int row_id, float temperature, int k,
                               float top_p, float min_p, float u, bool greedy, Shared &sh) {
@@ -952,7 +954,9 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
 }  // namespace
 
 // Up to a row for every compute unit: 1024 threads, a CU's waves; more rows: 512, two
-// rows to a CU, one of which works while the other waits at a barrier.
+// rows to a CU, one of which works while the other waits at a barrier. Rows of 65536 without
+// a filter, 1024 against 512 threads: bf16 64 rows 24.2, 27.5 us, 256 25.2, 28.1, 257 44.0,
+// 35.9, 1024 90, 71; fp32 256 45.7, 48.4, 257 76.6, 67.7, 1024 159, 137.
 hipError_t launch_sample(const SampleParams &p, int dtype, hipStream_t s) {
   const int rows = p.batch * p.w;
   const dim3 grid(static_cast<unsigned>(rows));
