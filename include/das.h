@@ -436,8 +436,9 @@ das_status das_kv_append_q8(const das_cache_q8 *cache, const das_batch *batch, c
  *   min-p  keeps, of those, the tokens with w_j >= min_p[b] (0 or less: all; over 1
  *          counts as 1).
  * The token is the first in index order at which the running sum of kept weights
- * passes uniform[b][i] times their sum. Sums are exact sums of weights rounded to
- * 2^-40; a token below 2^-41 of the largest is never drawn. A temperature of 0 takes
+ * passes uniform[b][i] times their sum. Weights are rounded to 2^-40, for every filter
+ * and the draw, and their sums are exact; a token below 2^-41 of the largest is never
+ * drawn. A temperature of 0 takes
  * the largest logit, lowest index first; so do rows with a NaN, negative or infinite
  * temperature, a NaN filter or a random number outside [0, 1), which set
  * DAS_DEVERR_SAMPLE, and a row without any logit above -inf gives token 0.
