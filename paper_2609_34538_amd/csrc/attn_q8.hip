@@ -463,8 +463,9 @@ __device__ __forceinline__ void block_logits(f32x4 (&s)[NQ][2], const Block<T, D
 // left to late_values; kHasLarge, some are 2^-40 or more (bf16 calls).
 constexpr uint32_t kHasLate = 1, kHasLarge = 2;
 template <typename T, int DH, int NQ, bool FAR = false>
-__device__ __forceinline__ uint32_t block_tile(Acc<DH, NQ> &st, uint64_t &far, Block<T, DH> &t, const AttnQ8Params &p, int u,
-                                           const QFrag<T, DH> (&qf)[NQ], const int (&row_pos)[NQ], int lg) {
+__device__ __forceinline__ uint32_t block_tile(Acc<DH, NQ> &st, uint64_t &far, Block<T, DH> &t,
+                                               const AttnQ8Params &p, int u, const QFrag<T, DH> (&qf)[NQ],
+                                               const int (&row_pos)[NQ], int lg) {
   constexpr int KS = DH / 32;
   f32x4 s[NQ][2];
   block_logits<T, DH, NQ>(s, t, qf);
@@ -472,7 +473,8 @@ __device__ __forceinline__ uint32_t block_tile(Acc<DH, NQ> &st, uint64_t &far, B
 #pragma unroll
   for (int qt = 0; qt < NQ; ++qt) cap[qt] = row_pos[qt] - kTile * u;
   const int limits[1] = {p.w - kTile * u};
-  softmax_step<DH, NQ, 2, true, FAR, sizeof(T) == 4>(st, far, s, cap, limits, p.scale_log2, sizeof(T) == 2 ? kProbShift : 0.f, lg);
+  softmax_step<DH, NQ, 2, true, FAR, sizeof(T) == 4>(st, far, s, cap, limits, p.scale_log2,
+                                                     sizeof(T) == 2 ? kProbShift : 0.f, lg);
 
   // the largest magnitude's bits tell whether any is late
   typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
