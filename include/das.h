@@ -94,6 +94,7 @@ typedef enum das_dtype { DAS_F32 = 0, DAS_BF16 = 1 } das_dtype;
                                     range; the row was taken greedily               */
 #define DAS_DEVERR_POOL 32u      /* too few free pages for a sequence, or a free
                                     list that cannot be right                       */
+#define DAS_DEVERR_PROPOSAL 64u  /* a drafted token outside the vocabulary; rejected */
 
 /*
  * Depth-indexed, paged KV cache (caller-owned device memory).
@@ -502,6 +503,203 @@ das_status das_pages_update(int32_t batch, int32_t max_pages_per_seq, int32_t nu
                             int32_t *free_pages, int32_t *num_free, const int32_t *first,
                             int32_t block_len, int32_t *slots, uint32_t *dev_error,
                             hipStream_t stream);
+
+/* -------------------------------------------------------------------------
+ * A cache held in 4 bits
+ * -------------------------------------------------------------------------
+ * The same planes, layers, heads, pages and block tables with every element one e2m1 code
+ * (a sign bit and 0, 0.5, 1, 1.5, 2, 3, 4 or 6) and one power-of-two scale per token, KV head
+ * and 32 neighbouring dims ("block"), as OCP's MX formats have them. Element = code *
+ * 2^(byte - 127); byte 255 makes the block's 32 elements NaN. 4.25 bits an element: a cache
+ * holds 3.8 times the tokens of a bf16 one, and its attention reads a quarter of the bytes.
+ *
+ * A page of one head is 32 * head_dim bytes of two codes each, the even dim in the low four
+ * bits, and 2 * head_dim exponent bytes. With S = head_dim / 32, 64 "lanes" 16 g + n (g < 4,
+ * n < 16) and 16 bytes of each in every piece:
+ *
+ *   base.k_pool  [num_k_planes][L][Hkv][num_pages][S][64][16]: token 32 T + 8 (n / 4) + 4 e +
+ *                n % 4 (T, e < 2), dims 32 s + 8 g + 2 j and + 1 (j < 4): byte
+ *                4 ((2 T + e) S + s) + j of lane 16 g + n, 16 bytes to a piece
+ *   base.v_pool  [num_v_planes][L][Hkv][num_pages][S][64][16]: token 32 T + 8 g + i (i < 8),
+ *                dims 32 s + 2 n and + 1: byte 8 T + i of lane 16 g + n of piece s
+ *   k_exp        [num_k_planes][L][Hkv][num_pages][16][4 S]: the token and block above are
+ *                byte (2 T + e) S + s of n
+ *   v_exp        [num_v_planes][L][Hkv][num_pages][4][S][16]: byte 8 T + i of (g, s)
+ *
+ * base.dtype is the type of queries, block K/V, outputs, committed K/V and what is read back;
+ * the other fields of `base` are as in das_cache. All four arrays are 16-byte aligned. Bytes
+ * 0..252 keep every element within the range of both types. Places that hold no token of a
+ * sequence (behind its length) may hold anything.
+ */
+typedef struct das_cache_q4 {
+  das_cache base;
+  uint8_t *k_exp;
+  uint8_t *v_exp;
+} das_cache_q4;
+
+/*
+ * das_attn_policy over a 4-bit cache: prefix keys at depth kappa and values at depth nu are
+ * the elements above, block keys and values are the caller's in base.dtype. Arguments, masks,
+ * bounds and error words as for das_attn_policy, and the same limits (w in
+ * 1..DAS_MAX_BLOCK, Hq / Hkv <= 8), for any batch size.
+ *
+ * Numerics: cached elements are exact in the products' types. bf16 calls round probabilities
+ * to bf16 for cached values, and to twice its bits for block values; fp32 calls take every
+ * factor with its 24 bits. Accumulation and softmax statistics are fp32, for logits of any
+ * finite size; sums are divided last, so that values whose sum over the positions passes the
+ * largest fp32 give infinities. Block values that are infinite or NaN reach only the rows that
+ * see them. Sequences that are cut into parts are joined from the parts' results, in bf16
+ * calls from fp16 relative to each row's largest: what is under 2^-39 of it in its part is
+ * lost. lse as for das_attn_policy.
+ *
+ * das_attn_q4_workspace_bytes returns 0 for arguments that das_attn_q4 rejects; the
+ * workspace is 256-byte aligned, needs no init, and calls that run concurrently need
+ * separate ones.
+ */
+size_t das_attn_q4_workspace_bytes(const das_cache_q4 *cache, const das_batch *batch,
+                                   int32_t num_q_heads, int32_t block_len);
+das_status das_attn_q4(const das_cache_q4 *cache, const das_batch *batch, int32_t layer,
+                       int32_t kappa, int32_t nu, int32_t num_q_heads, int32_t block_len,
+                       const void *q, const void *k_blk, const void *v_blk, void *out, float *lse,
+                       void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * das_kv_append into a 4-bit cache. Arguments as for das_kv_append, with k_new and v_new in
+ * base.dtype; len_out must share no element with batch->prefix_len or num_new
+ * (DAS_ERR_SHAPE).
+ *
+ * A block gets the smallest exponent e in -120..125 with |x| <= 7 * 2^e for its 32 elements,
+ * so that none is further from its code than half the distance of the largest two (4 and 6).
+ * Codes are x * 2^-e rounded to the nearest, ties to an even code, past 6 to 6. A block with
+ * a NaN or an infinity gets byte 255. Tokens share nothing: the result does not depend on
+ * which tokens are committed together, and places of other tokens are left as they were.
+ */
+das_status das_kv_append_q4(const das_cache_q4 *cache, const das_batch *batch, const void *k_new,
+                            const void *v_new, int32_t w_max, const int32_t *num_new,
+                            int32_t *len_out, hipStream_t stream);
+
+/* Largest row count per sequence of das_kv_read_q4. */
+#define DAS_MAX_READ (1 << 20)
+
+/*
+ * Cached elements back in base.dtype, in the layout of a commit's inputs: positions first[b]
+ * .. first[b] + num[b] - 1 of sequence b, of every stored plane and core layer. For moving a
+ * sequence to a cache of another kind (with das_kv_append), or a block's K/V out of it.
+ *
+ *   k_out  [num_k_planes][L][B][w_max][Hkv][head_dim]  written, rows past num[b] left alone
+ *   v_out  [num_v_planes][L][B][w_max][Hkv][head_dim]  the same
+ *   first  device [B], num device [B] in 0..w_max: the positions must lie in the prefix
+ *          (first[b] + num[b] <= prefix_len[b]); else nothing of the sequence is written
+ *          (DAS_DEVERR_PREFIX). Positions on a page out of range are not written
+ *          (DAS_DEVERR_PAGE).
+ *
+ * w_max in 1..DAS_MAX_READ, batch * w_max * Hkv * head_dim < 2^46. k_out and v_out are
+ * 16-byte aligned and must not overlap the cache or each other.
+ */
+das_status das_kv_read_q4(const das_cache_q4 *cache, const das_batch *batch, const int32_t *first,
+                          const int32_t *num, int32_t w_max, void *k_out, void *v_out,
+                          hipStream_t stream);
+
+/*
+ * Norms of queries and keys for each head and their rotation by position, in one pass: what
+ * comes between a projection and das_attn_policy.
+ *
+ *   y = x * weight / sqrt(mean(x^2) + eps)                     over a head's head_dim elements
+ *   (y_i, y_j) -> (y_i cos t - y_j sin t, y_j cos t + y_i sin t),  t = position * inv_freq[pair]
+ *
+ * The first rotary_dim dims are rotated, in pairs (i, i + rotary_dim / 2), or (2 i, 2 i + 1)
+ * where `interleaved` is not 0; the others are only normalised. Values, if given, are copied:
+ * the block K/V of an attention or a commit are rows without gaps, a projection's need not be.
+ *
+ *   q  [B][w][Hq][head_dim], k, v [B][w][Hkv][head_dim] with the distances of sequences and
+ *      of tokens in elements (heads lie side by side), so that the three may be parts of one
+ *      projection's output. v may be NULL, and then v_out is.
+ *   q_out, k_out, v_out   without gaps. An output may be its own input where that has no gaps;
+ *      else outputs overlap no input and no other output (DAS_ERR_SHAPE).
+ *   q_weight, k_weight    device [head_dim] in `dtype`, or NULL: no norm of these
+ *   inv_freq   device [rotary_dim / 2] fp32
+ *   positions  device [B] int32: the position of a sequence's first token (prefix_len); or,
+ *      with each_position not 0, [B][w]
+ *
+ * head_dim 64, 96 or 128; rotary_dim a multiple of 16 in 0..head_dim (0: norm only, inv_freq
+ * may be NULL); Hq, Hkv in 1..65535; w in 1..DAS_MAX_READ, batch * w < 2^24; eps >= 0 and
+ * finite. Distances are multiples of 16 bytes, rows are 16-byte aligned. Angles are taken in
+ * 64 bits, the mean in 64, the rest in fp32, and results are rounded once. A head of zeros
+ * with eps 0 gives NaN.
+ */
+typedef struct das_rope {
+  int32_t dtype;          /* das_dtype of q, k, v, weights and outputs */
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t head_dim;
+  int32_t rotary_dim;
+  int32_t interleaved;
+  int32_t each_position;
+  float eps;
+  const float *inv_freq;
+  const void *q_weight;
+  const void *k_weight;
+} das_rope;
+das_status das_qk_rope(const das_rope *rope, int32_t batch, int32_t block_len, const void *q,
+                       int64_t q_batch_stride, int64_t q_token_stride, const void *k,
+                       int64_t k_batch_stride, int64_t k_token_stride, const void *v,
+                       int64_t v_batch_stride, int64_t v_token_stride, const int32_t *positions,
+                       void *q_out, void *k_out, void *v_out, hipStream_t stream);
+
+/*
+ * Verification of a block whose proposals were drawn from the draft's distributions, on the
+ * device: das_greedy_accept for sampling. Every emitted token is a draw from the target's
+ * distribution, whatever the draft's is; the nearer the two are, the more is accepted.
+ *
+ * Row (b, i) has the target's distribution p_i = softmax(target / temperature[b]) and the
+ * draft's q_i = softmax(draft / draft_temperature[b]), where the proposals must have been
+ * drawn (das_sample without filters; a caller's filter puts -inf in the logits of both). NaN
+ * logits count as -inf; a temperature of 0 makes the distribution one-hot at the largest
+ * logit, lowest index first, and a row without any logit above -inf is one-hot at token 0.
+ * Without draft logits q_i is one-hot at the proposal (a greedy draft).
+ *
+ * The first m_b = tested[b] proposals are checked in order; y_i is accepted while
+ * uniform[b][i] * q_i(y_i) < p_i(y_i). With a_b accepted, the next token is drawn with draw[b]
+ * - from max(p - q, 0) of position a_b where that was rejected (a difference below 2^-40 of
+ *   p counts as 0; where none is left, from p),
+ * - from p of position a_b where a_b = m_b < w,
+ * and with a_b = w none is. The token drawn is the first in index order at which the running
+ * sum passes draw[b] times the whole. Weights are 64-bit exponentials relative to the row's
+ * largest.
+ *
+ *   proposals    device [B][w] int32. One that is checked and lies outside the vocabulary is
+ *                rejected, with the whole of p as the residual but for q
+ *                (DAS_DEVERR_PROPOSAL)
+ *   target_logits, draft_logits   device rows of `vocab` elements of `dtype`, in the order
+ *                [B][w], their distances in elements (>= vocab); draft_logits may be NULL
+ *   temperature, draft_temperature   device [B] fp32, or NULL: 1. One that is NaN, negative
+ *                or infinite counts as 0 (DAS_DEVERR_SAMPLE)
+ *   tested       device [B] int32 or NULL (w), clamped to 0..w (DAS_DEVERR_TESTED)
+ *   uniform      device [B][w] fp32, draw device [B] fp32, in [0, 1). A uniform outside
+ *                rejects its proposal, a draw outside counts as 0 (DAS_DEVERR_SAMPLE)
+ *   accepted, num_keep, num_emitted, emitted   written as by das_greedy_accept: a_b,
+ *                min(a_b + 1, w) (das_kv_append's num_new), the same, and the tokens;
+ *                emitted and num_emitted may be NULL
+ *   probs        device [B][w] fp32 or NULL, written: p of the emitted tokens
+ *   workspace    >= das_sampled_accept_workspace_bytes(...), 256-byte aligned, needs no init;
+ *                calls that run concurrently need separate ones
+ *   dev_error    optional device word
+ *
+ * Rows past what is checked (and the row after it) are not read. batch in 1..65535, block_len
+ * in 1..DAS_MAX_BLOCK, vocab in 1..DAS_MAX_VOCAB. Logits are aligned to their type, the other
+ * arrays to 4 bytes; outputs must not overlap the inputs or each other. Entries of emitted and
+ * probs past num_emitted[b] are left alone. Equal calls give equal bits.
+ */
+size_t das_sampled_accept_workspace_bytes(int32_t batch, int32_t block_len, int32_t vocab);
+das_status das_sampled_accept(int32_t batch, int32_t block_len, int32_t vocab, int32_t dtype,
+                              const int32_t *proposals, const void *target_logits,
+                              int64_t target_stride, const void *draft_logits,
+                              int64_t draft_stride, const float *temperature,
+                              const float *draft_temperature, const int32_t *tested,
+                              const float *uniform, const float *draw, int32_t *accepted,
+                              int32_t *num_keep, int32_t *emitted, int32_t *num_emitted,
+                              float *probs, void *workspace, size_t workspace_bytes,
+                              uint32_t *dev_error, hipStream_t stream);
 
 /* Static description of a status code; never NULL. */
 const char *das_status_string(das_status status);

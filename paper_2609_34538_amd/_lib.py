@@ -11,7 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_char_p, c_int32, c_int64, c_size_t, c_uint32, c_void_p
+from ctypes import POINTER, c_char_p, c_float, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 from dataclasses import dataclass, field
 from typing import Dict, Optional
 
@@ -33,14 +33,17 @@ STATUS_NAMES = {0: "DAS_OK", -1: "DAS_ERR_NULL", -2: "DAS_ERR_SHAPE", -3: "DAS_E
 DTYPE_CODES = {torch.float32: 0, torch.bfloat16: 1}
 PATHS = {"auto": 0, "valu": 1, "mfma": 2, "balanced": 3}
 DEVERR_PAGE, DEVERR_PREFIX, DEVERR_COMMIT, DEVERR_TESTED = 1, 2, 4, 8
-DEVERR_SAMPLE, DEVERR_POOL = 16, 32
+DEVERR_SAMPLE, DEVERR_POOL, DEVERR_PROPOSAL = 16, 32, 64
 MAX_VOCAB = 1 << 20
 GROUP_TOKENS = 8  # tokens that share an exponent of the 8-bit cache
+BLOCK_DIMS = 32   # dims of a token that share an exponent of the 4-bit cache
 
 EXPORTED = ["das_attn_workspace_bytes", "das_attn_workspace_bytes_ex", "das_attn_draft_maturev",
             "das_attn_verify", "das_attn_policy", "das_attn_policy_noalloc", "das_kv_append",
             "das_greedy_accept", "das_attn_q8_workspace_bytes", "das_attn_q8", "das_kv_append_q8",
-            "das_sample", "das_pages_update",
+            "das_sample", "das_pages_update", "das_attn_q4_workspace_bytes", "das_attn_q4",
+            "das_kv_append_q4", "das_kv_read_q4", "das_qk_rope",
+            "das_sampled_accept_workspace_bytes", "das_sampled_accept",
             "das_status_string", "das_version"]
 
 
@@ -69,6 +72,17 @@ class DasOptionsC(ctypes.Structure):
 
 class DasCacheQ8C(ctypes.Structure):
     _fields_ = [("base", DasCacheC), ("k_exp", c_void_p), ("v_exp", c_void_p)]
+
+
+class DasCacheQ4C(ctypes.Structure):
+    _fields_ = [("base", DasCacheC), ("k_exp", c_void_p), ("v_exp", c_void_p)]
+
+
+class DasRopeC(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("num_q_heads", c_int32), ("num_kv_heads", c_int32),
+                ("head_dim", c_int32), ("rotary_dim", c_int32), ("interleaved", c_int32),
+                ("each_position", c_int32), ("eps", c_float), ("inv_freq", c_void_p),
+                ("q_weight", c_void_p), ("k_weight", c_void_p)]
 
 
 def _load() -> ctypes.CDLL:
@@ -115,6 +129,25 @@ def _load() -> ctypes.CDLL:
     lib.das_pages_update.argtypes = ([c_int32] * 3 + [c_void_p] * 6 + [c_int32] + [c_void_p] * 2
                                      + [c_void_p])
     lib.das_pages_update.restype = c_int32
+    p4 = POINTER(DasCacheQ4C)
+    lib.das_attn_q4_workspace_bytes.argtypes = [p4, pb, c_int32, c_int32]
+    lib.das_attn_q4_workspace_bytes.restype = c_size_t
+    lib.das_attn_q4.argtypes = [p4, *lib.das_attn_q8.argtypes[1:]]
+    lib.das_attn_q4.restype = c_int32
+    lib.das_kv_append_q4.argtypes = [p4, *lib.das_kv_append_q8.argtypes[1:]]
+    lib.das_kv_append_q4.restype = c_int32
+    lib.das_kv_read_q4.argtypes = [p4, pb, c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
+                                   c_void_p]
+    lib.das_kv_read_q4.restype = c_int32
+    lib.das_qk_rope.argtypes = ([POINTER(DasRopeC), c_int32, c_int32]
+                                + [c_void_p, c_int64, c_int64] * 3 + [c_void_p] * 4 + [c_void_p])
+    lib.das_qk_rope.restype = c_int32
+    lib.das_sampled_accept_workspace_bytes.argtypes = [c_int32] * 3
+    lib.das_sampled_accept_workspace_bytes.restype = c_size_t
+    lib.das_sampled_accept.argtypes = ([c_int32] * 4 + [c_void_p] + [c_void_p, c_int64] * 2
+                                       + [c_void_p] * 10 + [c_void_p, c_size_t, c_void_p]
+                                       + [c_void_p])
+    lib.das_sampled_accept.restype = c_int32
     lib.das_status_string.argtypes = [c_int32]
     lib.das_status_string.restype = c_char_p
     lib.das_version.argtypes = []
@@ -705,6 +738,17 @@ def kv_append_q8(cache: QuantCache, batch: Batch, k_new: torch.Tensor, v_new: to
     PreparedAppendQ8(cache, batch, k_new, v_new, num_new, len_out, stream)()
 
 
+def _row_stride(logits: torch.Tensor, what: str) -> int:
+    """Distance of the rows of logits [B, w, V], which may lie apart, but evenly in that
+    order."""
+    B, w, V = logits.shape
+    stride = logits.stride(1) if w > 1 else logits.stride(0) if B > 1 else V
+    if V > 1 and logits.stride(2) != 1 or stride < V or (
+            B > 1 and w > 1 and logits.stride(0) != w * stride):
+        raise ValueError(f"{what} must have contiguous rows at one even distance")
+    return stride
+
+
 class PreparedSample(_Call):
     """das_sample with its arguments marshalled up front; `tokens` and `probs` hold the
     results."""
@@ -718,11 +762,7 @@ class PreparedSample(_Call):
             raise ValueError("logits must be a float32 or bfloat16 tensor [B, w, V]")
         B, w, V = logits.shape
         dev = logits.device
-        stride = logits.stride(1) if w > 1 else logits.stride(0) if B > 1 else V
-        # rows may lie apart, but evenly in the order [B, w]
-        if V > 1 and logits.stride(2) != 1 or stride < V or (
-                B > 1 and w > 1 and logits.stride(0) != w * stride):
-            raise ValueError("logits must have contiguous rows at one even distance")
+        stride = _row_stride(logits, "logits")
         if tokens is None:
             tokens = _empty_on(stream, (B, w), torch.int32, dev)
         self.tokens, self.probs = tokens, probs
@@ -789,3 +829,339 @@ def pages_update(lengths: torch.Tensor, block_table: torch.Tensor, pages_held: t
     `first` and `slots` also write the slots of positions first[b] .. in the new table."""
     PreparedPages(lengths, block_table, pages_held, free_pages, num_free, first, slots, dev_error,
                   stream)()
+
+
+# ---------------------------------------------------------------------------
+# The 4-bit cache, norm and rotation of queries and keys, sampled verification
+# ---------------------------------------------------------------------------
+@dataclass
+class Quant4Cache:
+    """Caller-owned depth-indexed paged cache in 4 bits (layouts as in das.h), S = dh / 32.
+
+    k_pool / v_pool: uint8 [nK|nV, L, Hkv, P, S, 64, 16], two codes a byte; k_exp: uint8
+    [nK, L, Hkv, P, 16, 4 * S]; v_exp: uint8 [nV, L, Hkv, P, 4, S, 16]. `dtype` is the type
+    of queries, block K/V, outputs, committed K/V and what is read back."""
+    k_pool: torch.Tensor
+    v_pool: torch.Tensor
+    k_exp: torch.Tensor
+    v_exp: torch.Tensor
+    num_depths: int
+    k_plane: Dict[int, int]
+    v_plane: Dict[int, int]
+    dtype: torch.dtype = torch.bfloat16
+    _c: DasCacheQ4C = field(default=None, repr=False)
+
+    def __post_init__(self):
+        self.refresh()
+
+    @classmethod
+    def empty(cls, num_layers: int, num_kv_heads: int, num_pages: int, head_dim: int,
+              num_depths: int, k_plane: Dict[int, int], v_plane: Dict[int, int],
+              dtype: torch.dtype = torch.bfloat16, device="cuda") -> "Quant4Cache":
+        """An empty cache with planes for the depths that k_plane and v_plane name."""
+        nk, nv, s = max(k_plane.values()) + 1, max(v_plane.values()) + 1, head_dim // BLOCK_DIMS
+        at, u8 = (num_layers, num_kv_heads, num_pages), torch.uint8
+        return cls(torch.zeros((nk, *at, s, 64, 16), dtype=u8, device=device),
+                   torch.zeros((nv, *at, s, 64, 16), dtype=u8, device=device),
+                   torch.full((nk, *at, 16, 4 * s), 127, dtype=u8, device=device),
+                   torch.full((nv, *at, 4, s, 16), 127, dtype=u8, device=device),
+                   num_depths, k_plane, v_plane, dtype)
+
+    @property
+    def num_layers(self):
+        return self.k_pool.shape[1]
+
+    @property
+    def num_kv_heads(self):
+        return self.k_pool.shape[2]
+
+    @property
+    def num_pages(self):
+        return self.k_pool.shape[3]
+
+    @property
+    def head_dim(self):
+        return self.k_pool.shape[4] * BLOCK_DIMS
+
+    @property
+    def device(self):
+        return self.k_pool.device
+
+    def refresh(self):
+        k, v = self.k_pool, self.v_pool
+        if k.dim() != 7 or v.dim() != 7:
+            raise ValueError("k_pool and v_pool must be 7-d")
+        (nk, L, hkv, P, s), nv = k.shape[:5], v.shape[0]
+        u8, dev = torch.uint8, k.device
+        _check(k, u8, (nk, L, hkv, P, s, 64, 16), dev, "k_pool")
+        _check(v, u8, (nv, L, hkv, P, s, 64, 16), dev, "v_pool")
+        _check(self.k_exp, u8, (nk, L, hkv, P, 16, 4 * s), dev, "k_exp")
+        _check(self.v_exp, u8, (nv, L, hkv, P, 4, s, 16), dev, "v_exp")
+        if self.dtype not in DTYPE_CODES:
+            raise ValueError("dtype must be torch.float32 or torch.bfloat16")
+        c = DasCacheQ4C()
+        b = c.base
+        b.dtype, b.num_depths = DTYPE_CODES[self.dtype], self.num_depths
+        b.num_layers, b.num_kv_heads, b.num_pages, b.head_dim = L, hkv, P, s * BLOCK_DIMS
+        b.num_k_planes, b.num_v_planes = nk, nv
+        for r in range(MAX_DEPTH + 1):
+            b.k_plane[r] = self.k_plane.get(r, -1)
+            b.v_plane[r] = self.v_plane.get(r, -1)
+        b.k_pool, b.v_pool = k.data_ptr(), v.data_ptr()
+        c.k_exp, c.v_exp = self.k_exp.data_ptr(), self.v_exp.data_ptr()
+        self._c, self._ref = c, ctypes.byref(c)
+        self._dev, self._hkv, self._dh = dev, hkv, s * BLOCK_DIMS
+        return self
+
+    @property
+    def c(self) -> DasCacheQ4C:
+        return self._c
+
+
+def workspace_bytes_q4(cache: Quant4Cache, batch: Batch, num_q_heads: int, block_len: int) -> int:
+    return LIB.das_attn_q4_workspace_bytes(ctypes.byref(cache.c), ctypes.byref(batch.c),
+                                           num_q_heads, block_len)
+
+
+def alloc_workspace_q4(cache: Quant4Cache, batch: Batch, num_q_heads: int, block_len: int,
+                       stream=None) -> torch.Tensor:
+    n = workspace_bytes_q4(cache, batch, num_q_heads, block_len)
+    if n == 0:
+        raise DasError(-2, "workspace query rejected the shapes")
+    return _empty_on(stream, n, torch.uint8, cache.device)
+
+
+def _check_workspace(workspace: torch.Tensor, dev):
+    if (workspace.dtype is not torch.uint8 or workspace.device != dev
+            or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
+    return workspace.data_ptr(), workspace.numel()
+
+
+class PreparedAttentionQ4(_Call):
+    """das_attn_q4 with its arguments marshalled up front, for loops that issue the same
+    call many times."""
+
+    def __init__(self, cache: Quant4Cache, batch: Batch, layer: int, kappa: int, nu: int,
+                 q: torch.Tensor, k_blk: torch.Tensor, v_blk: torch.Tensor, out: torch.Tensor,
+                 workspace: torch.Tensor, lse: Optional[torch.Tensor] = None, stream=None):
+        if q.dim() != 4:
+            raise ValueError("q must be [B, w, Hq, dh]")
+        dev, dtype, B, (_, w, hq, _) = cache._dev, cache.dtype, batch.batch, q.shape
+        blk, q_shape = (B, w, cache._hkv, cache._dh), (B, w, hq, cache._dh)
+        _check_batch_on(batch, dev)
+        args = (cache._ref, ctypes.byref(batch.c), layer, kappa, nu, hq, w,
+                _check(q, dtype, q_shape, dev, "q"), _check(k_blk, dtype, blk, dev, "k_blk"),
+                _check(v_blk, dtype, blk, dev, "v_blk"), _check(out, dtype, q_shape, dev, "out"),
+                _check_opt(lse, torch.float32, (B, hq, w), dev, "lse"),
+                *_check_workspace(workspace, dev))
+        super().__init__(LIB.das_attn_q4, "das_attn_q4", args,
+                         (*_tensors_of(cache, batch), q, k_blk, v_blk, out, workspace, lse), dev,
+                         stream)
+
+
+def attn_policy_q4(cache: Quant4Cache, batch: Batch, layer: int, kappa: int, nu: int,
+                   q: torch.Tensor, k_blk: torch.Tensor, v_blk: torch.Tensor,
+                   out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Eq. (2)-(3) over a 4-bit cache: prefix keys at depth kappa, values at depth nu."""
+    if q.dim() != 4:
+        raise ValueError("q must be [B, w, Hq, dh]")
+    if out is None:
+        out = _empty_on(stream, q.shape, q.dtype, q.device)
+    if workspace is None:
+        workspace = alloc_workspace_q4(cache, batch, q.shape[2], q.shape[1], stream)
+    PreparedAttentionQ4(cache, batch, layer, kappa, nu, q, k_blk, v_blk, out, workspace, lse,
+                        stream)()
+    return out
+
+
+def _check_rows_q4(cache: Quant4Cache, batch: Batch, k, v, k_name: str, v_name: str):
+    """Shapes of committed or read K/V; returns their addresses and w_max."""
+    if k.dim() != 6:
+        raise ValueError(f"{k_name} must be [nK, L, B, w_max, Hkv, dh]")
+    dev, w_max = cache.device, k.shape[3]
+    tail = (cache.num_layers, batch.batch, w_max, cache.num_kv_heads, cache.head_dim)
+    _check_batch_on(batch, dev)
+    return (_check(k, cache.dtype, (cache.k_pool.shape[0], *tail), dev, k_name),
+            _check(v, cache.dtype, (cache.v_pool.shape[0], *tail), dev, v_name), w_max)
+
+
+class PreparedAppendQ4(_Call):
+    """das_kv_append_q4 with its arguments marshalled up front."""
+
+    def __init__(self, cache: Quant4Cache, batch: Batch, k_new: torch.Tensor, v_new: torch.Tensor,
+                 num_new: torch.Tensor, len_out: Optional[torch.Tensor] = None, stream=None):
+        k, v, w_max = _check_rows_q4(cache, batch, k_new, v_new, "k_new", "v_new")
+        dev = cache.device
+        args = (ctypes.byref(cache.c), ctypes.byref(batch.c), k, v, w_max,
+                _check(num_new, torch.int32, (batch.batch,), dev, "num_new"),
+                _check_opt(len_out, torch.int32, (batch.batch,), dev, "len_out"))
+        super().__init__(LIB.das_kv_append_q4, "das_kv_append_q4", args,
+                         (*_tensors_of(cache, batch), k_new, v_new, num_new, len_out), dev, stream)
+
+
+def kv_append_q4(cache: Quant4Cache, batch: Batch, k_new: torch.Tensor, v_new: torch.Tensor,
+                 num_new: torch.Tensor, len_out: Optional[torch.Tensor] = None, stream=None):
+    """Commit the first num_new[b] block entries of every plane and layer, in 4 bits."""
+    PreparedAppendQ4(cache, batch, k_new, v_new, num_new, len_out, stream)()
+
+
+class PreparedReadQ4(_Call):
+    """das_kv_read_q4 with its arguments marshalled up front."""
+
+    def __init__(self, cache: Quant4Cache, batch: Batch, first: torch.Tensor, num: torch.Tensor,
+                 k_out: torch.Tensor, v_out: torch.Tensor, stream=None):
+        k, v, w_max = _check_rows_q4(cache, batch, k_out, v_out, "k_out", "v_out")
+        dev = cache.device
+        args = (ctypes.byref(cache.c), ctypes.byref(batch.c),
+                _check(first, torch.int32, (batch.batch,), dev, "first"),
+                _check(num, torch.int32, (batch.batch,), dev, "num"), w_max, k, v)
+        super().__init__(LIB.das_kv_read_q4, "das_kv_read_q4", args,
+                         (*_tensors_of(cache, batch), first, num, k_out, v_out), dev, stream)
+
+
+def kv_read_q4(cache: Quant4Cache, batch: Batch, first: torch.Tensor, num: torch.Tensor,
+               k_out: torch.Tensor, v_out: torch.Tensor, stream=None):
+    """Positions first[b] .. first[b] + num[b] - 1 of every plane and layer, in the cache's
+    dtype, into k_out [nK, L, B, w_max, Hkv, dh] and v_out [nV, ...]; rows past num[b] are
+    left alone."""
+    PreparedReadQ4(cache, batch, first, num, k_out, v_out, stream)()
+
+
+class PreparedRope(_Call):
+    """das_qk_rope with its arguments marshalled up front. q [B, w, Hq, dh], k and v [B, w,
+    Hkv, dh] may be parts of one projection's output; their heads lie side by side."""
+
+    def __init__(self, q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor,
+                 inv_freq: Optional[torch.Tensor], q_out: torch.Tensor, k_out: torch.Tensor,
+                 q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                 eps: float = 1e-6, interleaved: bool = False, v: Optional[torch.Tensor] = None,
+                 v_out: Optional[torch.Tensor] = None, stream=None):
+        if q.dim() != 4 or k.dim() != 4 or q.dtype not in DTYPE_CODES:
+            raise ValueError("q and k must be float32 or bfloat16 tensors [B, w, H, dh]")
+        if (v is None) != (v_out is None):
+            raise ValueError("v and v_out go together")
+        B, w, hq, dh = q.shape
+        hkv, dev, dtype = k.shape[2], q.device, q.dtype
+
+        def rows(t, heads, what):
+            if (t.shape != (B, w, heads, dh) or t.dtype is not dtype or t.device != dev
+                    or t.stride(3) != 1 or (heads > 1 and t.stride(2) != dh)):
+                raise ValueError(f"{what} must be {dtype} [{B}, {w}, {heads}, {dh}] on {dev} with "
+                                 "its heads side by side")
+            return t.data_ptr(), t.stride(0), t.stride(1)
+
+        c = DasRopeC()
+        c.dtype, c.num_q_heads, c.num_kv_heads, c.head_dim = DTYPE_CODES[dtype], hq, hkv, dh
+        if inv_freq is not None:
+            c.rotary_dim = 2 * inv_freq.numel()
+            c.inv_freq = _check(inv_freq, torch.float32, (inv_freq.numel(),), dev, "inv_freq")
+        each = positions.dim() == 2
+        at = _check(positions, torch.int32, (B, w) if each else (B,), dev, "positions")
+        c.interleaved, c.each_position, c.eps = int(interleaved), int(each), eps
+        c.q_weight = _check_opt(q_weight, dtype, (dh,), dev, "q_weight")
+        c.k_weight = _check_opt(k_weight, dtype, (dh,), dev, "k_weight")
+        kv = (B, w, hkv, dh)
+        args = (ctypes.byref(c), B, w, *rows(q, hq, "q"), *rows(k, hkv, "k"),
+                *((None, 0, 0) if v is None else rows(v, hkv, "v")), at,
+                _check(q_out, dtype, (B, w, hq, dh), dev, "q_out"),
+                _check(k_out, dtype, kv, dev, "k_out"), _check_opt(v_out, dtype, kv, dev, "v_out"))
+        super().__init__(LIB.das_qk_rope, "das_qk_rope", args,
+                         (c, q, k, v, positions, inv_freq, q_out, k_out, v_out, q_weight, k_weight),
+                         dev, stream)
+
+
+def qk_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor,
+            inv_freq: Optional[torch.Tensor], q_out: Optional[torch.Tensor] = None,
+            k_out: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+            k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+            v: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None, stream=None):
+    """Norm (where a weight is given) and rotation (the first 2 * len(inv_freq) dims) of
+    queries and keys for each head, at positions[b] + i or positions[b, i], and copies of the
+    values. Returns (q_out, k_out), or (q_out, k_out, v_out) with v."""
+    if q_out is None:
+        q_out = _empty_on(stream, q.shape, q.dtype, q.device)
+    if k_out is None:
+        k_out = _empty_on(stream, k.shape, k.dtype, k.device)
+    if v is not None and v_out is None:
+        v_out = _empty_on(stream, v.shape, v.dtype, v.device)
+    PreparedRope(q, k, positions, inv_freq, q_out, k_out, q_weight, k_weight, eps, interleaved, v,
+                 v_out, stream)()
+    return (q_out, k_out) if v is None else (q_out, k_out, v_out)
+
+
+def alloc_workspace_accept(proposals: torch.Tensor, vocab: int, stream=None) -> torch.Tensor:
+    n = LIB.das_sampled_accept_workspace_bytes(*proposals.shape, vocab)
+    if n == 0:
+        raise DasError(-2, "workspace query rejected the shapes")
+    return _empty_on(stream, n, torch.uint8, proposals.device)
+
+
+class PreparedSampledAccept(_Call):
+    """das_sampled_accept with its arguments marshalled up front; `accepted`, `num_keep`,
+    `emitted`, `num_emitted` and `probs` hold the results."""
+
+    def __init__(self, proposals: torch.Tensor, target_logits: torch.Tensor,
+                 uniform: torch.Tensor, draw: torch.Tensor,
+                 draft_logits: Optional[torch.Tensor] = None,
+                 temperature: Optional[torch.Tensor] = None,
+                 draft_temperature: Optional[torch.Tensor] = None,
+                 tested: Optional[torch.Tensor] = None, accepted: Optional[torch.Tensor] = None,
+                 num_keep: Optional[torch.Tensor] = None, emitted: Optional[torch.Tensor] = None,
+                 num_emitted: Optional[torch.Tensor] = None, probs: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None,
+                 dev_error: Optional[torch.Tensor] = None, stream=None):
+        z, d = target_logits, draft_logits
+        if z.dim() != 3 or z.dtype not in DTYPE_CODES:
+            raise ValueError("target_logits must be a float32 or bfloat16 tensor [B, w, V]")
+        B, w, V = z.shape
+        dev, i32, f32 = z.device, torch.int32, torch.float32
+        if d is not None and (d.shape != z.shape or d.dtype is not z.dtype or d.device != dev):
+            raise ValueError("draft_logits must be shaped and typed like target_logits")
+        if proposals.shape != (B, w):
+            raise ValueError("proposals must be [B, w]")
+        if accepted is None:
+            accepted = _empty_on(stream, (B,), i32, dev)
+        if num_keep is None:
+            num_keep = _empty_on(stream, (B,), i32, dev)
+        if workspace is None:
+            workspace = alloc_workspace_accept(proposals, V, stream)
+        self.accepted, self.num_keep, self.probs = accepted, num_keep, probs
+        self.emitted, self.num_emitted = emitted, num_emitted
+        args = (B, w, V, DTYPE_CODES[z.dtype], _check(proposals, i32, (B, w), dev, "proposals"),
+                z.data_ptr(), _row_stride(z, "target_logits"), _ptr(d),
+                0 if d is None else _row_stride(d, "draft_logits"),
+                _check_opt(temperature, f32, (B,), dev, "temperature"),
+                _check_opt(draft_temperature, f32, (B,), dev, "draft_temperature"),
+                _check_opt(tested, i32, (B,), dev, "tested"),
+                _check(uniform, f32, (B, w), dev, "uniform"), _check(draw, f32, (B,), dev, "draw"),
+                _check(accepted, i32, (B,), dev, "accepted"),
+                _check(num_keep, i32, (B,), dev, "num_keep"),
+                _check_opt(emitted, i32, (B, w), dev, "emitted"),
+                _check_opt(num_emitted, i32, (B,), dev, "num_emitted"),
+                _check_opt(probs, f32, (B, w), dev, "probs"), *_check_workspace(workspace, dev),
+                _check_opt(dev_error, i32, (1,), dev, "dev_error"))
+        super().__init__(LIB.das_sampled_accept, "das_sampled_accept", args,
+                         (proposals, z, d, temperature, draft_temperature, tested, uniform, draw,
+                          accepted, num_keep, emitted, num_emitted, probs, workspace, dev_error),
+                         dev, stream)
+
+
+def sampled_accept(proposals: torch.Tensor, target_logits: torch.Tensor, uniform: torch.Tensor,
+                   draw: torch.Tensor, draft_logits: Optional[torch.Tensor] = None,
+                   temperature: Optional[torch.Tensor] = None,
+                   draft_temperature: Optional[torch.Tensor] = None,
+                   tested: Optional[torch.Tensor] = None, accepted: Optional[torch.Tensor] = None,
+                   num_keep: Optional[torch.Tensor] = None, emitted: Optional[torch.Tensor] = None,
+                   num_emitted: Optional[torch.Tensor] = None,
+                   probs: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                   dev_error: Optional[torch.Tensor] = None, stream=None):
+    """Verification of drawn proposals [B, w] against the target's distributions, with random
+    numbers uniform [B, w] and draw [B]: every emitted token is a draw from the target's.
+    Returns (accepted, num_keep); num_keep is das_kv_append's num_new."""
+    call = PreparedSampledAccept(proposals, target_logits, uniform, draw, draft_logits, temperature,
+                                 draft_temperature, tested, accepted, num_keep, emitted,
+                                 num_emitted, probs, workspace, dev_error, stream)
+    call()
+    return call.accepted, call.num_keep

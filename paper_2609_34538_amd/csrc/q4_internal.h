@@ -1,0 +1,87 @@
+// Internal declarations of the 4-bit cache's kernels, the queries' and keys' norm and
+// rotation, and the sampled verification, shared by their host side (das_draft_api.hip).
+// Not part of the public C ABI.
+#pragma once
+
+#include "q8_internal.h"
+
+namespace das {
+
+// Elements of a token that share one exponent, and the exponents that the commit gives (the
+// stored byte is 127 more): the smallest code of the smallest is 2^-121, a normal bf16, and
+// 6 * 2^125 is the largest multiple of 6 that fits one.
+constexpr int kQ4Block = 32;
+constexpr int kQ4MinExp = -120, kQ4MaxExp = 125;
+constexpr int kQ4NanByte = 255;
+// Bytes of a page of one head: two codes each, and the exponents.
+__host__ __device__ constexpr int q4_page_bytes(int dh) { return kPage * dh / 2; }
+__host__ __device__ constexpr int q4_page_exps(int dh) { return kPage * dh / kQ4Block; }
+
+// One attention call over the 4-bit cache: AttnQ8Params with k_layer, v_layer
+// [Hkv][P][dh / 32][64][16], k_exp, v_exp [Hkv][P][2 * dh], and chunk_tiles in tiles of 64
+// tokens (the draft block's, then a page each).
+hipError_t launch_attn_q4(const AttnQ8Params &p, int dtype, int dh, hipStream_t s);
+
+// Launch shape of the attention kernel: 16-row tiles of a wave (two of a bf16 call up to 32
+// rows do not fit its registers beside two pages under way at head dim 128, nor do two of an
+// fp32 call, whose queries are three operands each) and waves with different rows.
+__host__ __device__ constexpr int q4_row_tiles(int rows, int dh, int es) {
+  return rows <= 16 || es == 4 || (dh == 128 && rows <= 32) ? 1 : 2;
+}
+__host__ __device__ constexpr int q4_row_waves(int rows, int dh, int es) {
+  return rows <= 16 * q4_row_tiles(rows, dh, es) ? 1 : rows <= 32 * q4_row_tiles(rows, dh, es) ? 2 : 4;
+}
+__host__ __device__ constexpr int q4_group_rows(int rows, int dh, int es) {
+  return 16 * q4_row_tiles(rows, dh, es) * q4_row_waves(rows, dh, es);
+}
+
+// The commit into the 4-bit cache, and the way back (k_new, v_new written).
+struct TokensQ4Params {
+  void *k_new;             // [nK][L][B][w_max][Hkv][dh]
+  void *v_new;             // [nV][L][B][w_max][Hkv][dh]
+  uint8_t *k_pool;         // [nK][L][Hkv][P][dh / 32][64][16]
+  uint8_t *v_pool;         // [nV][L][Hkv][P][dh / 32][64][16]
+  uint8_t *k_exp, *v_exp;  // [planes][L][Hkv][P][2 * dh]
+  const int32_t *first;    // [B] first position: the prefix lengths of a commit
+  const int32_t *limit;    // [B] or null: positions that there are (reading)
+  const int32_t *block_table;
+  const int32_t *num;      // [B]
+  int32_t *len_out;        // [B] or null (commit)
+  uint32_t *dev_error;
+  int32_t batch, n_k_planes, n_v_planes, layers, hkv, num_pages, max_pages, w_max;
+};
+hipError_t launch_kv_append_q4(const TokensQ4Params &p, int dtype, int dh, hipStream_t s);
+hipError_t launch_kv_read_q4(const TokensQ4Params &p, int dtype, int dh, hipStream_t s);
+
+struct RopeParams {
+  const void *q, *k, *v;             // rows of heads; v may be null
+  void *q_out, *k_out, *v_out;
+  const void *q_weight, *k_weight;   // [dh] or null: no norm
+  const float *inv_freq;             // [rotary / 2]
+  const int32_t *positions;          // [B] first positions, or [B][w] (each)
+  int64_t q_batch, q_token, k_batch, k_token, v_batch, v_token;  // strides in elements
+  float eps;
+  int32_t batch, w, hq, hkv, dh, rotary, interleaved, each;
+};
+hipError_t launch_qk_rope(const RopeParams &p, int dtype, hipStream_t s);
+
+// Tokens of a row that one workgroup of the verification takes, and what it keeps of a part
+// and of a sequence in the workspace.
+constexpr int kAcceptPart = 8192;
+constexpr int kAcceptStatBytes = 16, kAcceptChainBytes = 48;
+struct SampledAcceptParams {
+  const int32_t *proposals;         // [B][w]
+  const void *target, *draft;       // rows of `vocab` logits; draft may be null
+  const float *temperature, *draft_temperature;  // [B] or null (1)
+  const int32_t *tested;            // [B] or null (w)
+  const float *uniform, *draw;      // [B][w], [B]
+  int32_t *accepted, *num_keep, *emitted, *num_emitted;  // the last may be null
+  float *probs;                     // [B][w] or null
+  uint32_t *dev_error;
+  uint8_t *ws;
+  int64_t target_stride, draft_stride;
+  int32_t batch, w, vocab, parts;  // parts of kAcceptPart tokens
+};
+hipError_t launch_sampled_accept(const SampledAcceptParams &p, int dtype, hipStream_t s);
+
+}  // namespace das
