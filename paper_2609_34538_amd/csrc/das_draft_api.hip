@@ -142,8 +142,9 @@ bool span_of(const void *at, int batch, int w, int heads, int dh, int64_t sb, in
 
 // Parts of a row of the sampled verification, and the workspace: statistics of target's and
 // draft's parts, the residual's sums, and what is known of a sequence.
-size_t accept_workspace(int64_t batch, int64_t w, int64_t parts) {
-  const int64_t bytes = 2 * batch * w * parts * kAcceptStatBytes + batch * parts * 8 + batch * kAcceptChainBytes;
+size_t accept_workspace(int64_t batch, int64_t w, int64_t vocab) {
+  const int64_t parts = (vocab + kAcceptPart - 1) / kAcceptPart, draws = (vocab + kAcceptDraw - 1) / kAcceptDraw;
+  const int64_t bytes = 2 * batch * w * parts * kAcceptStatBytes + batch * draws * 8 + batch * kAcceptChainBytes;
   return static_cast<size_t>(bytes + 255) / 256 * 256;
 }
 
@@ -354,7 +355,7 @@ size_t das_sampled_accept_workspace_bytes(int32_t batch, int32_t block_len, int3
   if (batch < 1 || batch > 65535 || block_len < 1 || block_len > DAS_MAX_BLOCK || vocab < 1 ||
       vocab > DAS_MAX_VOCAB)
     return 0;
-  return accept_workspace(batch, block_len, (vocab + kAcceptPart - 1) / kAcceptPart);
+  return accept_workspace(batch, block_len, vocab);
 }
 
 das_status das_sampled_accept(int32_t batch, int32_t block_len, int32_t vocab, int32_t dtype,
@@ -383,8 +384,12 @@ das_status das_sampled_accept(int32_t batch, int32_t block_len, int32_t vocab, i
   const int parts = (vocab + kAcceptPart - 1) / kAcceptPart;
   const int64_t rows = static_cast<int64_t>(batch) * block_len;
   // one workgroup of 256 threads per part of a target's and a draft's row; at most 2^32 - 1 work-items
-  if (rows * (draft_logits ? 2 : 1) * parts * 256 > 0xffffffffLL) return DAS_ERR_SHAPE;
-  if (!workspace || workspace_bytes < accept_workspace(batch, block_len, parts) || !aligned(workspace, 256))
+  // (and per part of a sequence's draw)
+  const int draws = (vocab + kAcceptDraw - 1) / kAcceptDraw;
+  if (rows * (draft_logits ? 2 : 1) * parts * 256 > 0xffffffffLL ||
+      static_cast<int64_t>(batch) * draws * 256 > 0xffffffffLL)
+    return DAS_ERR_SHAPE;
+  if (!workspace || workspace_bytes < accept_workspace(batch, block_len, vocab) || !aligned(workspace, 256))
     return DAS_ERR_WORKSPACE;
   SampledAcceptParams p;
   p.proposals = proposals;
@@ -408,6 +413,7 @@ das_status das_sampled_accept(int32_t batch, int32_t block_len, int32_t vocab, i
   p.w = block_len;
   p.vocab = vocab;
   p.parts = parts;
+  p.draw_parts = draws;
   return launch_sampled_accept(p, dtype, stream) == hipSuccess ? DAS_OK : DAS_ERR_HIP;
 }
 

@@ -65,9 +65,10 @@ struct RopeParams {
 };
 hipError_t launch_qk_rope(const RopeParams &p, int dtype, hipStream_t s);
 
-// Tokens of a row that one workgroup of the verification takes, and what it keeps of a part
-// and of a sequence in the workspace.
-constexpr int kAcceptPart = 8192;
+// Tokens of a row that one workgroup of the verification takes, for the rows' sums and for the
+// draw, and what it keeps of a part and of a sequence in the workspace.
+constexpr int kAcceptPart = 8192, kAcceptDraw = 2048;
+constexpr int kAcceptMostDraws = DAS_MAX_VOCAB / kAcceptDraw;
 constexpr int kAcceptStatBytes = 16, kAcceptChainBytes = 48;
 struct SampledAcceptParams {
   const int32_t *proposals;         // [B][w]
@@ -80,7 +81,7 @@ struct SampledAcceptParams {
   uint32_t *dev_error;
   uint8_t *ws;
   int64_t target_stride, draft_stride;
-  int32_t batch, w, vocab, parts;  // parts of kAcceptPart tokens
+  int32_t batch, w, vocab, parts, draw_parts;
 };
 hipError_t launch_sampled_accept(const SampledAcceptParams &p, int dtype, hipStream_t s);
 

@@ -11,10 +11,10 @@
 // below 2^-40 of p they count as 0, so that rounding leaves no token that p does not exceed q
 // at.
 //
-// Three kernels: the largest logit and the sum of weights of every part of every row (bound
-// by HBM and its 64-bit arithmetic); per sequence the run of accepted proposals, and of every
-// part of the row where it ends the sum of the residual; the token in the part where the
-// running sum passes the random number's share.
+// Three kernels: the largest logit and the sum of weights of every part of every row; per
+// sequence the run of accepted proposals, and of every part of the row where it ends the sum
+// of the residual; the token in the part where the running sum passes the random number's
+// share.
 
 #include "mfma_tile.h"
 #include "q4_internal.h"
@@ -31,7 +31,7 @@ constexpr double kNone = 0x1p-40;  // a residual below this share of p is none
 // What is known of a row, or of a part of one.
 struct Stat {
   float max;
-  int at;      // lowest index of the largest logit (greedy rows only)
+  int at;      // lowest index of the largest logit (one-hot rows only)
   double sum;  // of weights relative to max
 };
 // What the second kernel leaves for the third.
@@ -41,24 +41,37 @@ struct Chain {
 };
 constexpr int kNothing = 0, kPlain = 1, kLeft = 2;
 
-// 2^x for x <= 0 in 64 bits: 2^x = 2^n 2^(j / 32) 2^f with |f| <= 1 / 64 and the series of
-// e^(f ln 2) to f^5 (rest below 2^-48); table: 2^(j / 32), 32 entries that lie in different banks.
-__device__ __forceinline__ double exp2_of(double x, const double *table) {
-  const double t = fmax(x, -1000.0);
-  const double big = __builtin_fma(t, 32.0, 0x1.8p52);
+// A sequence's temperature: the factor of z - max in units of 1 / 32 octave; 0 for one-hot rows.
+__device__ __forceinline__ double temper(const float *temperature, int b, bool *bad) {
+  const float T = temperature ? temperature[b] : 1.f;
+  const bool ok = T >= 0.f && T < __builtin_huge_valf();
+  if (!ok) *bad = true;
+  return !ok || T == 0.f ? 0.0 : 32.0 * 1.4426950408889634 / static_cast<double>(T);
+}
+
+// 2^(d c32 / 32) for d <= 0, d c32 >= -32000, in 64 bits: 2^(k / 32 + f / 32), |f| <= 1/2, with
+// 2^(j / 32) from a table of 32 entries, which lie in different banks, and the series of e^(f ln
+// 2 / 32) to f^5 (rest below 2^-48). 1 exactly at d = 0.
+__device__ __forceinline__ double exp2_near(double d, double c32, const double *table) {
+  const double big = __builtin_fma(d, c32, 0x1.8p52);
   const int k = static_cast<int>(__builtin_bit_cast(uint64_t, big));
-  const double f = __builtin_fma(big - 0x1.8p52, -0.03125, t);
-  double q = 0.0013333558146428443;
-  q = __builtin_fma(q, f, 0.0096181291076284772);
-  q = __builtin_fma(q, f, 0.055504108664821580);
-  q = __builtin_fma(q, f, 0.24022650695910071);
-  q = __builtin_fma(q, f, 0.69314718055994531);
+  const double f = __builtin_fma(d, c32, -(big - 0x1.8p52));
+  // (ln 2 / 32)^n / n!
+  double q = 3.9737099845494154e-11;
+  q = __builtin_fma(q, f, 9.172562701824643e-09);
+  q = __builtin_fma(q, f, 1.6938509724371819e-06);
+  q = __builtin_fma(q, f, 2.3459619820224677e-04);
+  q = __builtin_fma(q, f, 2.166084939249829e-02);
   const double a = table[k & 31];
   return __builtin_amdgcn_ldexp(__builtin_fma(a * f, q, a), k >> 5);
 }
+// The same for any d <= 0; what is under 2^-1000 becomes that.
+__device__ __forceinline__ double exp2_of(double d, double c32, const double *table) {
+  return exp2_near(d * c32 < -32000.0 ? -32000.0 / c32 : d, c32, table);
+}
 __device__ __forceinline__ void fill_table(double *table) {
   if (threadIdx.x < 32) {
-    // 2^(j / 32), j < 32, from the series of e^x on [0, ln 2) by halving
+    // 2^(j / 32) from the series of e^x - 1 for a 16th of the exponent, doubled four times
     const double x = threadIdx.x * (0.69314718055994531 / 32.0 / 16.0);
     double q = 1.0 / 40320.0;
     q = __builtin_fma(q, x, 1.0 / 5040.0);
@@ -68,57 +81,29 @@ __device__ __forceinline__ void fill_table(double *table) {
     q = __builtin_fma(q, x, 1.0 / 6.0);
     q = __builtin_fma(q, x, 0.5);
     q = __builtin_fma(q, x, 1.0);
-    double e = q * x;  // e^x - 1, doubled four times
+    double e = q * x;
     for (int i = 0; i < 4; ++i) e = __builtin_fma(e, e, 2.0 * e);
     table[threadIdx.x] = 1.0 + e;
   }
   __syncthreads();
 }
 
-// A distribution's parameters: greedy rows are one-hot.
-struct Temper {
-  double c;  // log2(e) / T
-  bool greedy;
-};
-__device__ __forceinline__ Temper temper(const float *temperature, int b, bool *bad) {
-  const float T = temperature ? temperature[b] : 1.f;
-  const bool ok = T >= 0.f && T < __builtin_huge_valf();
-  if (!ok) *bad = true;
-  Temper t;
-  t.greedy = !ok || T == 0.f;
-  t.c = t.greedy ? 0.0 : 1.4426950408889634 / static_cast<double>(T);
-  return t;
-}
 // The weight of logit z at index j of a row.
-__device__ __forceinline__ double weight(float z, int j, const Stat &r, const Temper &t, const double *table) {
-  if (t.greedy || r.max == kNegInf) return j == r.at ? 1.0 : 0.0;
-  if (z == r.max) return 1.0;
-  if (z == kNegInf || r.max == __builtin_huge_valf()) return 0.0;
-  return exp2_of((static_cast<double>(z) - static_cast<double>(r.max)) * t.c, table);
+__device__ __forceinline__ double weight(float z, int j, const Stat &r, double c32, const double *table) {
+  if (c32 == 0.0 || r.max == kNegInf) return j == r.at ? 1.0 : 0.0;
+  if (r.max == __builtin_huge_valf()) return z == r.max ? 1.0 : 0.0;
+  const double w = exp2_of(static_cast<double>(z) - static_cast<double>(r.max), c32, table);
+  return z > kNegInf ? w : 0.0;
 }
 // What a draw weighs token `at` by, from the target's and the draft's logits.
 __device__ __forceinline__ double residual(const SampledAcceptParams &p, float zp, float zq, int at, const Chain &ch,
-                                           const Temper &tp, const Temper &tq, const double *table) {
+                                           double cp, double cq, const double *table) {
   if (at >= p.vocab) return 0.0;
-  const double w = weight(zp, at, ch.p, tp, table);
+  const double w = weight(zp, at, ch.p, cp, table);
   if (ch.drawn != kLeft) return w;
-  const double wq = p.draft ? weight(zq, at, ch.q, tq, table) : at == ch.y ? 1.0 : 0.0;
+  const double wq = p.draft ? weight(zq, at, ch.q, cq, table) : at == ch.y ? 1.0 : 0.0;
   const double a = w * ch.q.sum, d = a - wq * ch.p.sum;
   return d > kNone * a ? d : 0.0;
-}
-// Two parts of a row as one.
-__device__ __forceinline__ Stat join(const Stat &a, const Stat &b, const Temper &t, const double *table) {
-  const bool first = a.max > b.max || (a.max == b.max && a.at <= b.at);
-  const Stat &hi = first ? a : b, &lo = first ? b : a;
-  Stat r = hi;
-  if (!t.greedy && lo.max > kNegInf) {
-    const double w = lo.max == hi.max ? 1.0
-                     : hi.max == __builtin_huge_valf()
-                         ? 0.0
-                         : exp2_of((static_cast<double>(lo.max) - static_cast<double>(hi.max)) * t.c, table);
-    r.sum = hi.sum + lo.sum * w;
-  }
-  return r;
 }
 
 // 8 logits of a row of n (at least 1) from index i on, which may lie past its end; what does is
@@ -146,25 +131,49 @@ __device__ __forceinline__ Eight<T> load8(const T *row, int i, int n) {
   }
   return r;
 }
+// Logit j of the eight as it is, and with -inf for NaN.
 template <typename T>
-__device__ __forceinline__ float logit(const Eight<T> &r, int j) {
-  float z;
-  if constexpr (sizeof(T) == 2) z = __uint_as_float(j % 2 ? r.w[j / 2] & 0xffff0000u : r.w[j / 2] << 16);
-  else z = __uint_as_float(r.w[j]);
-  return z == z ? z : kNegInf;
+__device__ __forceinline__ float raw_logit(const Eight<T> &r, int j) {
+  if constexpr (sizeof(T) == 2) return __uint_as_float(j % 2 ? r.w[j / 2] & 0xffff0000u : r.w[j / 2] << 16);
+  else return __uint_as_float(r.w[j]);
 }
+__device__ __forceinline__ float no_nan(float z) { return z == z ? z : kNegInf; }
+template <typename T>
+__device__ __forceinline__ float logit(const Eight<T> &r, int j) { return no_nan(raw_logit<T>(r, j)); }
 
 __device__ __forceinline__ double join64(uint32_t lo, uint32_t hi) {
   return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
 }
-__device__ __forceinline__ double shuffled(double x, int mask) {
+template <int CTRL>
+__device__ __forceinline__ double plus_dpp(double x) {
   const uint64_t u = __builtin_bit_cast(uint64_t, x);
-  return join64(__shfl_xor(static_cast<int>(u), mask), __shfl_xor(static_cast<int>(u >> 32), mask));
+  return x + join64(__builtin_amdgcn_update_dpp(0, static_cast<uint32_t>(u), CTRL, 0xf, 0xf, false),
+                    __builtin_amdgcn_update_dpp(0, static_cast<uint32_t>(u >> 32), CTRL, 0xf, 0xf, false));
 }
+// Sum over the wave, in every lane: lanes 1 and 2 apart, mirrored in 8 and 16, then the swaps
+// of 16 and 32 lanes.
 __device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) x += shuffled(x, m);
-  return x;
+  x = plus_dpp<0xB1>(x);
+  x = plus_dpp<0x4E>(x);
+  x = plus_dpp<0x141>(x);
+  x = plus_dpp<0x140>(x);
+  uint64_t u = __builtin_bit_cast(uint64_t, x);
+  uint32_t lo = static_cast<uint32_t>(u), hi = static_cast<uint32_t>(u >> 32);
+  auto a = __builtin_amdgcn_permlane16_swap(lo, lo, false, false);
+  auto b = __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+  x = join64(a[0], b[0]) + join64(a[1], b[1]);
+  u = __builtin_bit_cast(uint64_t, x);
+  lo = static_cast<uint32_t>(u), hi = static_cast<uint32_t>(u >> 32);
+  a = __builtin_amdgcn_permlane32_swap(lo, lo, false, false);
+  b = __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+  return join64(a[0], b[0]) + join64(a[1], b[1]);
+}
+template <int CTRL>
+__device__ __forceinline__ float max_dpp(float x) {
+  return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, false)));
+}
+__device__ __forceinline__ float wave_max(float x) {
+  return group_max(max_dpp<0x140>(max_dpp<0x141>(max_dpp<0x4E>(max_dpp<0xB1>(x)))));
 }
 
 // Tokens of a sequence that are verified, clamped as das_greedy_accept does.
@@ -175,35 +184,22 @@ __device__ __forceinline__ int tested_of(const SampledAcceptParams &p, int b, bo
   return m;
 }
 
-constexpr int kVec = 4;                       // pieces of 8 logits of a thread
-constexpr int kPart = kThreads * 8 * kVec;    // tokens of a part
-static_assert(kPart == kAcceptPart && sizeof(Stat) == kAcceptStatBytes && sizeof(Chain) == kAcceptChainBytes,
-              "the workspace's layout");
-
-// Part `part` of a row: its tokens kThreads * 8 * v + 8 * thread .. + 7.
-template <typename T, typename Fn>
-__device__ __forceinline__ void for_part(const Eight<T> (&x)[kVec], int begin, Fn &&fn) {
-#pragma unroll
-  for (int v = 0; v < kVec; ++v)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) fn(begin + (v * kThreads + static_cast<int>(threadIdx.x)) * 8 + j, logit<T>(x[v], j));
-}
-template <typename T>
-__device__ __forceinline__ void load_part(Eight<T> (&x)[kVec], const T *row, int begin, int n) {
-#pragma unroll
-  for (int v = 0; v < kVec; ++v)
-    x[v] = load8<T>(row, begin + (v * kThreads + static_cast<int>(threadIdx.x)) * 8, n);
-}
-
+// The workspace: statistics of all parts of target and draft rows, sums of the draw's parts,
+// and a Chain for every sequence.
 __device__ __forceinline__ Stat *stats_of(const SampledAcceptParams &p, int side, int64_t row) {
   return reinterpret_cast<Stat *>(p.ws) + (static_cast<int64_t>(side) * p.batch * p.w + row) * p.parts;
 }
 __device__ __forceinline__ double *lefts_of(const SampledAcceptParams &p, int b) {
-  return reinterpret_cast<double *>(stats_of(p, 2, 0)) + static_cast<int64_t>(b) * p.parts;
+  return reinterpret_cast<double *>(stats_of(p, 2, 0)) + static_cast<int64_t>(b) * p.draw_parts;
 }
 __device__ __forceinline__ Chain *chain_of(const SampledAcceptParams &p, int b) {
   return reinterpret_cast<Chain *>(lefts_of(p, p.batch)) + b;
 }
+
+constexpr int kVec = kAcceptPart / (kThreads * 8);  // pieces of 8 logits of a thread
+constexpr int kDraw = kThreads * 8;                 // tokens of a part of the draw, one piece each
+static_assert(kDraw == kAcceptDraw && sizeof(Stat) == kAcceptStatBytes && sizeof(Chain) == kAcceptChainBytes,
+              "the workspace's layout");
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void accept_stats_kernel(SampledAcceptParams p) {
@@ -218,32 +214,64 @@ __global__ __launch_bounds__(kThreads) void accept_stats_kernel(SampledAcceptPar
   bool bad = false;
   const int m = tested_of(p, b, &bad);
   if (i > m || (side && i == m)) return;  // nobody asks for it
-  const Temper t = temper(side ? p.draft_temperature : p.temperature, b, &bad);
+  const double c32 = temper(side ? p.draft_temperature : p.temperature, b, &bad);
   const T *src = static_cast<const T *>(side ? p.draft : p.target) + row * (side ? p.draft_stride : p.target_stride);
   Eight<T> x[kVec];
-  const int begin = part * kPart;
-  load_part<T>(x, src, begin, p.vocab);
+  const int begin = part * kAcceptPart + static_cast<int>(threadIdx.x) * 8;
+#pragma unroll
+  for (int v = 0; v < kVec; ++v) x[v] = load8<T>(src, begin + v * kThreads * 8, p.vocab);
   fill_table(table);
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   float mx = kNegInf;
-  for_part<T>(x, begin, [&](int, float z) { mx = fmaxf(mx, z); });
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) mx = fmaxf(mx, __shfl_xor(mx, d));
+  for (int v = 0; v < kVec; ++v)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mx = fmaxf(mx, raw_logit<T>(x[v], j));  // NaN gives way
+  mx = wave_max(mx);
   if (lane == 0) part_max[wave] = mx;
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < kWavesA; ++k) mx = fmaxf(mx, part_max[k]);
   double sum = 0.0;
   int at = 0x7fffffff;
-  if (t.greedy || mx == kNegInf) {
-    for_part<T>(x, begin, [&](int j, float z) { at = z == mx ? min(at, j) : at; });
+  if (c32 == 0.0 || mx == kNegInf) {
+#pragma unroll
+    for (int v = 0; v < kVec; ++v)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) at = logit<T>(x[v], j) == mx ? min(at, begin + v * kThreads * 8 + j) : at;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) at = min(at, __shfl_xor(at, d));
   } else if (mx == __builtin_huge_valf()) {
-    for_part<T>(x, begin, [&](int, float z) { sum += z == mx ? 1.0 : 0.0; });
-  } else {
+#pragma unroll
+    for (int v = 0; v < kVec; ++v)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += logit<T>(x[v], j) == mx ? 1.0 : 0.0;
+  } else if (const float low = static_cast<float>(static_cast<double>(mx) - 28000.0 / c32);
+             low > -3e38f && (static_cast<double>(mx) - static_cast<double>(low)) * c32 < 32000.0 &&
+             (static_cast<double>(mx) - static_cast<double>(low)) * c32 > 24000.0) {
+    // Logits under `low` weigh nothing (2^-875, give or take fp32's rounding of it); as that they,
+    // NaN and -inf need no more tests.
     const double top = mx;
-    for_part<T>(x, begin, [&](int, float z) { sum += exp2_of((static_cast<double>(z) - top) * t.c, table); });
+#pragma unroll
+    for (int v = 0; v < kVec; ++v)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        sum += exp2_near(static_cast<double>(fmaxf(raw_logit<T>(x[v], j), low)) - top, c32, table);
+  } else {  // so hot that every finite logit counts, or so cold that fp32 has no such `low`
+    const double top = mx;
+#pragma unroll 1
+    for (int v = 0; v < kVec; ++v) {
+      Eight<T> y = x[0];
+#pragma unroll
+      for (int i = 1; i < kVec; ++i)
+        if (i == v) y = x[i];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float z = logit<T>(y, j);
+        const double w = exp2_of(static_cast<double>(z) - top, c32, table);
+        sum += z > kNegInf ? w : 0.0;
+      }
+    }
   }
   sum = wave_sum(sum);
   if (lane == 0) {
@@ -261,26 +289,56 @@ __global__ __launch_bounds__(kThreads) void accept_stats_kernel(SampledAcceptPar
   }
 }
 
-// The sum over a part of the row where the run of accepted proposals ends: of the residual or
-// of p. All threads of the workgroup, which all get it.
+// A row's parts as one; sums of one-hot rows are 1.
+__device__ __forceinline__ Stat join_parts(const Stat *s, int parts, double c32, const double *table) {
+  constexpr int kAhead = 8;
+  Stat r = {kNegInf, 0x7fffffff, 0.0};
+  for (int k0 = 0; k0 < parts; k0 += kAhead) {
+    Stat x[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) x[k] = s[min(k0 + k, parts - 1)];
+    float mx = r.max;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) mx = fmaxf(mx, x[k].max);
+    auto scaled = [&](const Stat &a) {
+      if (a.max == mx) return a.sum;
+      if (a.max == kNegInf || mx == __builtin_huge_valf()) return 0.0;
+      return a.sum * exp2_of(static_cast<double>(a.max) - static_cast<double>(mx), c32, table);
+    };
+    double sum = scaled(r);
+    int at = r.max == mx ? r.at : 0x7fffffff;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (k0 + k < parts) {
+        sum += scaled(x[k]);
+        if (x[k].max == mx) at = min(at, x[k].at);
+      }
+    r = Stat{mx, at, sum};
+  }
+  if (c32 == 0.0 || r.max == kNegInf) r.sum = 1.0;
+  return r;
+}
+
+// One piece of the row where the run of accepted proposals ends: tokens 8 t .. + 7 of part
+// `part` of the draw for thread t, and what the draw weighs them by.
 template <typename T>
-__device__ __forceinline__ double part_sum(const SampledAcceptParams &p, int b, int part, const Chain &ch, const Temper &tp,
-                           const Temper &tq, const double *table, double *seg) {
+__device__ __forceinline__ void draw_weights(const SampledAcceptParams &p, int b, int part, const Chain &ch,
+                                             double cp, double cq, const double *table, double (&w)[8]) {
   const int64_t row = static_cast<int64_t>(b) * p.w + ch.accepted;
-  const T *zp = static_cast<const T *>(p.target) + row * p.target_stride;
-  const bool left = ch.drawn == kLeft, drafted = left && p.draft;
-  const int begin = part * kPart;
-  Eight<T> x[kVec], y[kVec];
-  load_part<T>(x, zp, begin, p.vocab);
-  if (drafted) load_part<T>(y, static_cast<const T *>(p.draft) + row * p.draft_stride, begin, p.vocab);
+  const bool drafted = ch.drawn == kLeft && p.draft;
+  const int first = part * kDraw + static_cast<int>(threadIdx.x) * 8;
+  const Eight<T> x = load8<T>(static_cast<const T *>(p.target) + row * p.target_stride, first, p.vocab);
+  Eight<T> y = {};
+  if (drafted) y = load8<T>(static_cast<const T *>(p.draft) + row * p.draft_stride, first, p.vocab);
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    w[j] = residual(p, logit<T>(x, j), drafted ? logit<T>(y, j) : 0.f, first + j, ch, cp, cq, table);
+}
+// The sum over a part, for all threads.
+__device__ __forceinline__ double part_total(const double (&w)[8], double *seg) {
   double sum = 0.0;
 #pragma unroll
-  for (int v = 0; v < kVec; ++v)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int at = begin + (v * kThreads + static_cast<int>(threadIdx.x)) * 8 + j;
-      sum += residual(p, logit<T>(x[v], j), drafted ? logit<T>(y[v], j) : 0.f, at, ch, tp, tq, table);
-    }
+  for (int j = 0; j < 8; ++j) sum += w[j];
   sum = wave_sum(sum);
   __syncthreads();  // the call before has been read
   if (threadIdx.x % 64 == 0) seg[threadIdx.x / 64] = sum;
@@ -291,163 +349,59 @@ __device__ __forceinline__ double part_sum(const SampledAcceptParams &p, int b, 
   return total;
 }
 
-// The row's token number that the draw takes, from a part: its residuals in token order.
-// All threads of the workgroup; `before`: the sum of the parts before.
-template <typename T>
-__device__ __forceinline__ int pick(const SampledAcceptParams &p, int b, int part, double before, double target, const Chain &ch,
-                    const Temper &tp, const Temper &tq, const double *table, double *seg, int *answer) {
-  const int64_t row = static_cast<int64_t>(b) * p.w + ch.accepted;
-  const T *zp = static_cast<const T *>(p.target) + row * p.target_stride;
-  const T *zq = p.draft ? static_cast<const T *>(p.draft) + row * p.draft_stride : nullptr;
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, begin = part * kPart;
-  Eight<T> x[kVec], y[kVec] = {};
-  load_part<T>(x, zp, begin, p.vocab);
-  const bool drafted = ch.drawn == kLeft && zq;
-  if (drafted) load_part<T>(y, zq, begin, p.vocab);
-  // segments of 512 tokens: wave `wave` of piece v, in token order v * waves + wave
-#pragma unroll
-  for (int v = 0; v < kVec; ++v) {
-    double mine = 0.0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int at = begin + (v * kThreads + static_cast<int>(threadIdx.x)) * 8 + j;
-      mine += residual(p, logit<T>(x[v], j), drafted ? logit<T>(y[v], j) : 0.f, at, ch, tp, tq, table);
-    }
-    mine = wave_sum(mine);
-    if (lane == 0) seg[v * kWavesA + wave] = mine;
-  }
-  __syncthreads();
-  // the segment that passes the target; where rounding lets none, the last with a token
-  int found = 0;
-  double run = before, from = before;
-  for (int k = 0; k < kVec * kWavesA; ++k) {
-    const double s = seg[k];
-    if (s > 0.0) {
-      found = k;
-      from = run;
-      if (target < run + s) break;
-    }
-    run += s;
-  }
-  if (found % kWavesA == wave) {
-    Eight<T> xs = x[0], ys = y[0];
-#pragma unroll
-    for (int v = 1; v < kVec; ++v)
-      if (v == found / kWavesA) xs = x[v], ys = y[v];
-    const int first = begin + found * 512 + lane * 8;
-    double w[8], mine = 0.0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      w[j] = residual(p, logit<T>(xs, j), drafted ? logit<T>(ys, j) : 0.f, first + j, ch, tp, tq, table);
-      mine += w[j];
-    }
-    // inclusive sum of the lanes
-    double incl = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const uint64_t u = __builtin_bit_cast(uint64_t, incl);
-      const uint32_t lo = __shfl_up(static_cast<int>(u), d), hi = __shfl_up(static_cast<int>(u >> 32), d);
-      incl += lane >= d ? join64(lo, hi) : 0.0;
-    }
-    double at = from + (incl - mine);
-    int token = 0x7fffffff, last = -1;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      at += w[j];
-      if (w[j] > 0.0) {
-        last = first + j;
-        if (target < at) token = min(token, first + j);
-      }
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      token = min(token, __shfl_xor(token, d));
-      last = max(last, __shfl_xor(last, d));
-    }
-    if (lane == 0) *answer = token == 0x7fffffff ? last : token;
-  }
-  __syncthreads();
-  return *answer;
-}
-
-// The drawn token into the outputs, by thread 0.
-template <typename T>
-__device__ __forceinline__ void emit_drawn(const SampledAcceptParams &p, int b, int token, const Chain &ch, const Temper &tp,
-                           const double *table) {
-  const int64_t row = static_cast<int64_t>(b) * p.w + ch.accepted;
-  if (p.emitted) p.emitted[row] = token;
-  if (p.probs) {
-    const T *zp = static_cast<const T *>(p.target) + row * p.target_stride;
-    float z = to_f32<T>(zp[token]);
-    z = z == z ? z : kNegInf;
-    p.probs[row] = static_cast<float>(weight(z, token, ch.p, tp, table) / ch.p.sum);
-  }
-}
-
-// target: the share of the whole that the draw takes.
-__device__ __forceinline__ double share_of(const SampledAcceptParams &p, int b, double total) {
-  const float u = p.draw[b];
-  return (u >= 0.f && u < 1.f ? static_cast<double>(u) : 0.0) * total;
-}
-
 template <typename T>
 __global__ __launch_bounds__(kThreads) void accept_chain_kernel(SampledAcceptParams p) {
   __shared__ double table[32], seg[kWavesA];
   __shared__ Chain chain;
-  const int b = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
+  __shared__ Stat drafts[64];
+  __shared__ double draft_weight[64];
+  const int b = blockIdx.x / p.draw_parts, part = blockIdx.x % p.draw_parts;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  fill_table(table);
   bool bad_temp = false, bad_tested = false;
   const int m = tested_of(p, b, &bad_tested);
-  const Temper tp = temper(p.temperature, b, &bad_temp);
-  const Temper tq = p.draft ? temper(p.draft_temperature, b, &bad_temp) : Temper{0.0, true};
+  const double cp = temper(p.temperature, b, &bad_temp);
+  const double cq = p.draft ? temper(p.draft_temperature, b, &bad_temp) : 0.0;
+  // lane i of the first two waves: position i of the target and of the draft
+  const int64_t at_row = static_cast<int64_t>(b) * p.w + lane;
+  const bool mine = lane < p.w && (wave == 0 ? lane <= m : wave == 1 && p.draft && lane < m);
+  int y = 0;
+  float zy = kNegInf;
+  if (mine && lane < m) {
+    y = p.proposals[at_row];
+    const T *rows = static_cast<const T *>(wave == 0 ? p.target : p.draft);
+    if (y >= 0 && y < p.vocab) zy = to_f32<T>(rows[at_row * (wave == 0 ? p.target_stride : p.draft_stride) + y]);
+  }
+  const float u = wave == 0 && lane < p.w ? p.uniform[at_row] : 0.f;
+  fill_table(table);
+  Stat s = {kNegInf, 0, 1.0};
+  double wy = 0.0;
+  if (mine) {
+    s = join_parts(stats_of(p, wave, at_row), p.parts, wave == 0 ? cp : cq, table);
+    if (lane < m) wy = weight(no_nan(zy), y, s, wave == 0 ? cp : cq, table);
+  }
+  if (wave == 1) {
+    drafts[lane] = s;
+    draft_weight[lane] = wy;
+  }
+  __syncthreads();
   if (wave == 0) {
-    // lane i: position i
-    Stat sp = {kNegInf, 0, 0.0}, sq = {kNegInf, 0, 1.0};
-    int y = 0;
-    double py = 0.0;
-    bool ok = false, bad_number = false, bad_token = false;
-    if (lane < p.w && lane <= m) {
-      const int64_t row = static_cast<int64_t>(b) * p.w + lane;
-      const Stat *s = stats_of(p, 0, row);
-      sp = s[0];
-      for (int k = 1; k < p.parts; ++k) sp = join(sp, s[k], tp, table);
-      if (tp.greedy || sp.max == kNegInf) sp.sum = 1.0;
-      if (lane < m) {
-        if (p.draft) {
-          s = stats_of(p, 1, row);
-          sq = s[0];
-          for (int k = 1; k < p.parts; ++k) sq = join(sq, s[k], tq, table);
-          if (tq.greedy || sq.max == kNegInf) sq.sum = 1.0;
-        }
-        y = p.proposals[row];
-        bad_token = y < 0 || y >= p.vocab;
-        const float u = p.uniform[row];
-        bad_number = !(u >= 0.f && u < 1.f);
-        if (!bad_token) {
-          auto at = [&](const void *rows, int64_t stride) {
-            const float z = to_f32<T>(static_cast<const T *>(rows)[row * stride + y]);
-            return z == z ? z : kNegInf;
-          };
-          const double wp = weight(at(p.target, p.target_stride), y, sp, tp, table);
-          const double wq = p.draft ? weight(at(p.draft, p.draft_stride), y, sq, tq, table) : 1.0;
-          py = wp / sp.sum;
-          ok = !bad_number && static_cast<double>(u) * (wq / sq.sum) < py;
-        }
-      }
-    }
+    const bool checked = lane < m;
+    const bool bad_token = checked && (y < 0 || y >= p.vocab), bad_number = checked && !(u >= 0.f && u < 1.f);
+    const Stat sq = p.draft ? drafts[lane] : Stat{kNegInf, 0, 1.0};
+    const double wq = p.draft ? draft_weight[lane] : 1.0, py = wy / s.sum;
+    const bool ok = checked && !bad_token && !bad_number && static_cast<double>(u) * (wq / sq.sum) < py;
     const uint64_t miss = ~__ballot(ok);
     const int a = min(miss ? static_cast<int>(__builtin_ctzll(miss)) : 64, m);
     if (lane == min(a, p.w - 1)) {
-      chain.p = sp;
+      chain.p = s;
       chain.q = sq;
       chain.accepted = a;
       chain.y = bad_token ? -1 : y;
       chain.drawn = a == p.w ? kNothing : a == m ? kPlain : kLeft;
     }
     if (part == 0) {
-      const float u = p.draw[b];
-      const bool bad_draw = lane == 0 && a < p.w && !(u >= 0.f && u < 1.f);
+      const float v = p.draw[b];
+      const bool bad_draw = lane == 0 && a < p.w && !(v >= 0.f && v < 1.f);
       const bool reached = lane <= a;  // what lies behind the first rejected one does not count
       const uint32_t word = (bad_temp || bad_draw || (reached && bad_number) ? DAS_DEVERR_SAMPLE : 0) |
                             (bad_tested ? DAS_DEVERR_TESTED : 0) |
@@ -460,9 +414,8 @@ __global__ __launch_bounds__(kThreads) void accept_chain_kernel(SampledAcceptPar
         if (p.num_emitted) p.num_emitted[b] = keep;
       }
       if (lane < a) {
-        const int64_t row = static_cast<int64_t>(b) * p.w + lane;
-        if (p.emitted) p.emitted[row] = y;
-        if (p.probs) p.probs[row] = static_cast<float>(py);
+        if (p.emitted) p.emitted[at_row] = y;
+        if (p.probs) p.probs[at_row] = static_cast<float>(py);
       }
     }
   }
@@ -470,44 +423,118 @@ __global__ __launch_bounds__(kThreads) void accept_chain_kernel(SampledAcceptPar
   const Chain ch = chain;
   if (part == 0 && threadIdx.x == 0) *chain_of(p, b) = ch;
   if (ch.drawn == kNothing) return;
-  const double total = part_sum<T>(p, b, part, ch, tp, tq, table, seg);
+  double w[8];
+  draw_weights<T>(p, b, part, ch, cp, cq, table, w);
+  const double total = part_total(w, seg);
   if (threadIdx.x == 0) lefts_of(p, b)[part] = total;
 }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void accept_draw_kernel(SampledAcceptParams p) {
-  __shared__ double table[32], seg[kVec * kWavesA];
-  __shared__ int answer;
-  const int b = blockIdx.x;
+  __shared__ double table[32], seg[kWavesA], lefts[kAcceptMostDraws];
+  const int b = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   Chain ch = *chain_of(p, b);
+  for (int k = threadIdx.x; k < p.draw_parts; k += kThreads) lefts[k] = lefts_of(p, b)[k];
   if (ch.drawn == kNothing) return;
   bool bad;  // reported before
-  const Temper tp = temper(p.temperature, b, &bad);
-  const Temper tq = p.draft ? temper(p.draft_temperature, b, &bad) : Temper{0.0, true};
+  const double cp = temper(p.temperature, b, &bad);
+  const double cq = p.draft ? temper(p.draft_temperature, b, &bad) : 0.0;
+  const float number = p.draw[b];
   fill_table(table);
-  const double *lefts = lefts_of(p, b);
-  double total = 0.0;
-  for (int k = 0; k < p.parts; ++k) total += lefts[k];
-  const bool none = total == 0.0;  // p does not exceed q anywhere: a token of p
-  if (none) {
+  // the running sum over the parts: a lane's parts, then the lanes before
+  auto total_of = [&]() {
+    double sum = 0.0;
+    for (int k = lane; k < p.draw_parts; k += 64) sum += lefts[k];
+    return wave_sum(sum);
+  };
+  double total = total_of(), w[8];
+  if (total == 0.0) {  // p does not exceed q anywhere: a token of p
     ch.drawn = kPlain;
-    for (int k = 0; k < p.parts; ++k) total += part_sum<T>(p, b, k, ch, tp, tq, table, seg);
-  }
-  const double target = share_of(p, b, total);
-  int part = 0;
-  double before = 0.0, run = 0.0;
-  for (int k = 0; k < p.parts; ++k) {
-    const double w = none ? part_sum<T>(p, b, k, ch, tp, tq, table, seg) : lefts[k];
-    if (w > 0.0) {
-      part = k;
-      before = run;
-      if (target < run + w) break;
+    for (int k = 0; k < p.draw_parts; ++k) {
+      draw_weights<T>(p, b, k, ch, cp, cq, table, w);
+      const double sum = part_total(w, seg);
+      if (threadIdx.x == 0) lefts[k] = sum;
     }
-    run += w;
+    __syncthreads();
+    total = total_of();
   }
+  const double target = (number >= 0.f && number < 1.f ? static_cast<double>(number) : 0.0) * total;
+  // Inclusive sums of 64 values, one a lane.
+  auto scan = [&](double x) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const uint64_t v = __builtin_bit_cast(uint64_t, x);
+      const double o = join64(__shfl_up(static_cast<int>(v), d), __shfl_up(static_cast<int>(v >> 32), d));
+      x += lane >= d ? o : 0.0;
+    }
+    return x;
+  };
+  auto lane_of = [&](double x, int l) {
+    const uint64_t v = __builtin_bit_cast(uint64_t, x);
+    return join64(__builtin_amdgcn_readlane(static_cast<uint32_t>(v), l),
+                  __builtin_amdgcn_readlane(static_cast<uint32_t>(v >> 32), l));
+  };
+  // the part that passes the target; where rounding lets none, the last with a token
+  int part = 0;
+  double run = 0.0, before = 0.0;
+  for (int k0 = 0; k0 < p.draw_parts; k0 += 64) {
+    const double x = k0 + lane < p.draw_parts ? lefts[k0 + lane] : 0.0, incl = scan(x);
+    const uint64_t pass = __ballot(x > 0.0 && target < run + incl), some = __ballot(x > 0.0);
+    if (pass || some) {
+      const int l = pass ? static_cast<int>(__builtin_ctzll(pass)) : 63 - static_cast<int>(__builtin_clzll(some));
+      part = k0 + l;
+      before = run + (lane_of(incl, l) - lane_of(x, l));
+      if (pass) break;
+    }
+    run += lane_of(incl, 63);
+  }
+  draw_weights<T>(p, b, part, ch, cp, cq, table, w);
+  double sum = 0.0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum += w[j];
+  const double incl = scan(sum);
   __syncthreads();
-  const int token = min(max(pick<T>(p, b, part, before, target, ch, tp, tq, table, seg, &answer), 0), p.vocab - 1);
-  if (threadIdx.x == 0) emit_drawn<T>(p, b, token, ch, tp, table);
+  if (lane == 63) seg[wave] = incl;
+  __syncthreads();
+  // the wave whose 512 tokens pass the target, the same way
+  int found = 0;
+  run = before;
+  double from = before;
+#pragma unroll
+  for (int k = 0; k < kWavesA; ++k) {
+    const double x = seg[k];
+    if (x > 0.0 && !(target < from + seg[found] && seg[found] > 0.0)) {
+      found = k;
+      from = run;
+    }
+    run += x;
+  }
+  if (found != wave) return;
+  double at = from + (incl - sum);
+  const int first = part * kDraw + static_cast<int>(threadIdx.x) * 8;
+  int token = 0x7fffffff, last = -1;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    at += w[j];
+    if (w[j] > 0.0) {
+      last = first + j;
+      if (target < at) token = min(token, first + j);
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    token = min(token, __shfl_xor(token, d));
+    last = max(last, __shfl_xor(last, d));
+  }
+  if (lane == 0) {
+    token = min(max(token == 0x7fffffff ? last : token, 0), p.vocab - 1);
+    const int64_t row = static_cast<int64_t>(b) * p.w + ch.accepted;
+    if (p.emitted) p.emitted[row] = token;
+    if (p.probs) {
+      const float z = no_nan(to_f32<T>(static_cast<const T *>(p.target)[row * p.target_stride + token]));
+      p.probs[row] = static_cast<float>(weight(z, token, ch.p, cp, table) / ch.p.sum);
+    }
+  }
 }
 
 template <typename T>
@@ -515,7 +542,7 @@ hipError_t launch_typed(const SampledAcceptParams &p, hipStream_t s) {
   const int64_t rows = static_cast<int64_t>(p.batch) * p.w * (p.draft ? 2 : 1);
   hipError_t e = launch_kernel(accept_stats_kernel<T>, dim3(static_cast<unsigned>(rows * p.parts)), dim3(kThreads), s, p);
   if (e != hipSuccess) return e;
-  e = launch_kernel(accept_chain_kernel<T>, dim3(static_cast<unsigned>(p.batch) * p.parts), dim3(kThreads), s, p);
+  e = launch_kernel(accept_chain_kernel<T>, dim3(static_cast<unsigned>(p.batch) * p.draw_parts), dim3(kThreads), s, p);
   if (e != hipSuccess) return e;
   return launch_kernel(accept_draw_kernel<T>, dim3(p.batch), dim3(kThreads), s, p);
 }
