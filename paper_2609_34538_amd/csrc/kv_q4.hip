@@ -9,12 +9,23 @@
 // and its result does not depend on how tokens come together. Blocks with a NaN or an
 // infinity get the exponent byte 255, which reads as NaN.
 //
-// A wave's unit is the call's positions of one page, of one (plane, layer, KV head) and
-// sequence, in groups of 8 tokens. A lane's item is 8 dims of a token, 16 bytes of a bf16
-// row; the four lanes of a block agree on its exponent by two DPP steps. Keys: an item is one
-// word of the page. Values: an item is four bytes, 16 apart, beside those of the group's
-// other tokens, so groups go through LDS for 8-byte accesses; a commit into part of a group
-// stores its bytes one by one, which leaves the others as they were.
+// A wave's unit is a quad of neighbouring tokens of one (plane, layer) and sequence, and 12
+// blocks of 32 dims along the heads, four a step: lane 16 a + 4 c + q has dims 8 c .. + 7 of
+// block a of token q, 16 bytes of a bf16 row, so that a step takes 256 bytes of each row and
+// the wave 768. The four lanes of a token's block agree on its exponent by two rotations within
+// 16 lanes. Keys: a lane's 8 codes are one word of the page. Values: the four lanes c hold words
+// of four tokens; a transposition of bytes in each quad of lanes (four broadcasts and three byte
+// permutations, its own inverse) makes of them the words of the page, four tokens of two dims.
+// A commit to part of a quad stores its bytes one by one, which leaves the others as they were.
+//
+// Bound by memory that is read and written at once: 2005 tokens of 24 planes and layers, 55
+// heads, dh 96 (135 MB in, 508 MB out) come back in 206 us, 3.1 TB/s, as a library conversion of
+// bytes to fp32 of that size does; without its loads the kernel takes 105 us, without its stores
+// 87. Commits of 0-32 tokens of 32 sequences (130 MB in, 34 MB out) take 66 us, what lies in
+// part of a 128-byte line of the page going out as several writes (63 MB by the counters); of 8
+// tokens of 64 planes x 4 layers x 55 heads 13 us, the launch and three dependent round trips.
+// Measured and not kept: a wave along the tokens of one head, 192 bytes of each row (213, 67
+// and 16 us), 2, 4, 6 and 8 steps a wave (216, 211, 222, 257 us), all steps in a loop (220 us).
 
 #include "mfma_tile.h"
 #include "q4_internal.h"
@@ -23,10 +34,11 @@ namespace das {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kGroup = 8;  // tokens
+constexpr int kSteps = 3;  // of a wave, whose loads are issued together
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 // 8 elements as loaded.
 template <typename T>
@@ -55,10 +67,19 @@ __device__ __forceinline__ uint32_t largest(const Eight<T> &x) {
     return static_cast<uint32_t>(max(m[0], m[1])) << 16;
   }
 }
-// The maximum over the four lanes of a quad.
-__device__ __forceinline__ uint32_t quad_max(uint32_t u) {
-  u = max(u, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, u, 0xB1, 0xf, 0xf, false)));
-  return max(u, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, u, 0x4E, 0xf, 0xf, false)));
+// The maximum over lanes 4, 8 and 12 apart within 16.
+__device__ __forceinline__ uint32_t block_max(uint32_t u) {
+  u = max(u, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, u, 0x128, 0xf, 0xf, false)));  // row_ror:8
+  return max(u, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, u, 0x124, 0xf, 0xf, false)));
+}
+// Byte j of lane i's word in a quad becomes byte i of lane j's; q: lane % 4.
+__device__ __forceinline__ uint32_t transposed(uint32_t w, int q) {
+  const uint32_t a = __builtin_amdgcn_update_dpp(0, w, 0x00, 0xf, 0xf, false);
+  const uint32_t b = __builtin_amdgcn_update_dpp(0, w, 0x55, 0xf, 0xf, false);
+  const uint32_t c = __builtin_amdgcn_update_dpp(0, w, 0xAA, 0xf, 0xf, false);
+  const uint32_t d = __builtin_amdgcn_update_dpp(0, w, 0xFF, 0xf, 0xf, false);
+  const uint32_t pick = q | (q + 4) << 8;
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, pick), __builtin_amdgcn_perm(b, a, pick), 0x05040100);
 }
 // Codes of 8 elements in a word.
 template <typename T>
@@ -100,133 +121,108 @@ __device__ __forceinline__ Eight<T> decode(uint32_t c, float scale) {
   return x;
 }
 
-// Where the word of keys of token t of a page, dims 8 c .. + 7, lies, and its exponent.
-template <int DH>
-__device__ __forceinline__ void key_place(int t, int c, int &word, int &exp) {
-  constexpr int KS = DH / 32;
-  const int n = t % 32 / 8 * 4 + t % 4, at = (t / 32 * 2 + t / 4 % 2) * KS + c / 4;
-  word = at / 4 * 1024 + (c % 4 * 16 + n) * 16 + at % 4 * 4;
-  exp = n * 4 * KS + at;
-}
-// Where the 8 tokens of group j of dims 2 pair, + 1 lie, and the exponent of token t, block s.
-__device__ __forceinline__ int value_place(int j, int pair) {
-  return pair / 16 * 1024 + (j % 4 * 16 + pair % 16) * 16 + j / 4 * 8;
-}
-template <int DH>
-__device__ __forceinline__ int value_exp(int t, int s) {
-  return t % 32 / 8 * 16 * (DH / 32) + s * 16 + t / 32 * 8 + t % 8;
-}
-
-// READ: from the cache into the rows; else from the rows into the cache.
+// READ: from the cache into the rows; else from the rows into the cache. grid: (plane, layer)
+// and share of the heads, keys first; sequences; groups of four quads, one a wave.
 template <typename T, int DH, bool READ>
-__global__ __launch_bounds__(64 * kWaves) void kv_q4_kernel(TokensQ4Params p) {
-  constexpr int CH = DH / 8, IT = (kGroup * CH + 63) / 64;  // items of a token, a lane's of a group
-  // a group's value codes: [8 tokens][dh / 2] on the way back, [dh / 2][8 tokens] into the cache
-  __shared__ __attribute__((aligned(8))) uint8_t codes[kWaves][kGroup * DH / 2];
+__global__ __launch_bounds__(64 * kWaves) void kv_q4_kernel(TokensQ4Params p, int shares) {
+  constexpr int KS = DH / 32;
   const int b = blockIdx.y;
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  const int per_plane = p.layers * p.hkv;
-  const int k_units = p.n_k_planes * per_plane, v_units = p.n_v_planes * per_plane;
-  const int k_blocks = (k_units + kWaves - 1) / kWaves;
-  const bool is_v = static_cast<int>(blockIdx.x) >= k_blocks;
-  const int rel = (is_v ? blockIdx.x - k_blocks : blockIdx.x) * kWaves + wave;
-  const bool first_wg = blockIdx.x == 0 && blockIdx.z == 0;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  const int share = blockIdx.x % shares, unit = blockIdx.x / shares;
+  const int k_units = p.n_k_planes * p.layers;
+  const bool is_v = unit >= k_units;
+  const int rel = is_v ? unit - k_units : unit;  // plane * layers + layer
 
   const int S = p.first[b];
   const int n = p.num[b];
   const long end = static_cast<long>(S) + n;
   bool bad = S < 0 || n < 0 || n > p.w_max || end > static_cast<long>(p.max_pages) * kPage;
   if (READ) bad |= end > p.limit[b];
-  if (first_wg && threadIdx.x == 0) {
+  if (blockIdx.x == 0 && blockIdx.z == 0 && threadIdx.x == 0) {
     if (bad) report_error(p.dev_error, READ ? DAS_DEVERR_PREFIX : DAS_DEVERR_COMMIT);
     if (!READ && p.len_out) p.len_out[b] = bad ? S : S + n;
   }
   if (bad || n == 0) return;
+  const int quad_end = (S + n + 3) / 4;
   const int32_t *table = p.block_table + static_cast<size_t>(b) * p.max_pages;
-  const int first_page = S / kPage, last_page = (S + n - 1) / kPage;
-  // every page id once, whoever writes there
-  if (blockIdx.x == 0) {
-    for (int pg = first_page + blockIdx.z + gridDim.z * threadIdx.x; pg <= last_page; pg += gridDim.z * blockDim.x) {
-      const int id = table[pg];
-      if (id < 0 || id >= p.num_pages) report_error(p.dev_error, DAS_DEVERR_PAGE);
+  const int a = lane / 16, c = lane / 4 % 4, q = lane % 4;
+  const int blocks = p.hkv * KS, first_block = share * (4 * kSteps) + a;
+  const size_t row = static_cast<size_t>(blocks) * 32;
+  T *rows = static_cast<T *>(is_v ? p.v_new : p.k_new) + (static_cast<size_t>(rel) * p.batch + b) * p.w_max * row;
+  const size_t heads = static_cast<size_t>(rel) * p.hkv * p.num_pages;
+  uint8_t *pool = (is_v ? p.v_pool : p.k_pool) + heads * q4_page_bytes(DH);
+  uint8_t *exponents = (is_v ? p.v_exp : p.k_exp) + heads * q4_page_exps(DH);
+  const uint64_t head_bytes = static_cast<uint64_t>(p.num_pages) * q4_page_bytes(DH);
+  const uint64_t head_exps = static_cast<uint64_t>(p.num_pages) * q4_page_exps(DH);
+
+  for (int quad = S / 4 + 4 * blockIdx.z + wave; quad < quad_end; quad += 4 * gridDim.z) {
+    const int id = table[quad / 16];
+    const int t = 4 * quad + q;
+    const bool live = t >= S && t < S + n, whole = 4 * quad >= S && 4 * quad + 4 <= S + n;
+    T *line = rows + static_cast<size_t>(live ? t - S : 0) * row + 8 * c;
+    Eight<T> x[kSteps];
+    if constexpr (!READ) {  // whatever the page
+#pragma unroll
+      for (int r = 0; r < kSteps; ++r) {
+        x[r] = Eight<T>{};
+        if (live && first_block + 4 * r < blocks)
+          __builtin_memcpy(&x[r], __builtin_assume_aligned(line + 32 * (first_block + 4 * r), 16), sizeof(x[r]));
+      }
     }
-  }
-  if (rel >= (is_v ? v_units : k_units)) return;
-
-  const int plane = rel / per_plane, layer = (rel / p.hkv) % p.layers, h = rel % p.hkv;
-  const size_t plane_layer = static_cast<size_t>(plane) * p.layers + layer;
-  // rows [plane][layer][B][w_max][Hkv][DH]
-  T *rows = static_cast<T *>(is_v ? p.v_new : p.k_new) +
-            ((plane_layer * p.batch + b) * p.w_max * p.hkv + h) * DH;
-  const size_t row = static_cast<size_t>(p.hkv) * DH;
-  const size_t head = (plane_layer * p.hkv + h) * p.num_pages;
-  uint8_t *mine = codes[wave];
-
-  for (int pg = first_page + blockIdx.z; pg <= last_page; pg += gridDim.z) {
-    const int id = table[pg];
-    if (id < 0 || id >= p.num_pages) continue;  // uniform
-    uint8_t *page = (is_v ? p.v_pool : p.k_pool) + (head + id) * q4_page_bytes(DH);
-    uint8_t *exps = (is_v ? p.v_exp : p.k_exp) + (head + id) * q4_page_exps(DH);
-    const int lo = max(S - pg * kPage, 0), hi = static_cast<int>(min(end - static_cast<long>(pg) * kPage, 64L));
-#pragma unroll 1
-    for (int j = lo / kGroup; j < (hi + kGroup - 1) / kGroup; ++j) {
-      if (READ && is_v) {
-        __builtin_amdgcn_wave_barrier();
-        if (lane < DH / 2) {
-          const uint64_t c = *reinterpret_cast<const uint64_t *>(page + value_place(j, lane));
+    if (id < 0 || id >= p.num_pages) {  // uniform
+      if (blockIdx.x == 0 && lane == 0) report_error(p.dev_error, DAS_DEVERR_PAGE);
+      continue;
+    }
+    const int half = quad % 16 / 8, g = quad % 8 / 2, e = quad % 2;  // token 32 half + 8 g + 4 e + q of the page
+    const int at0 = (2 * half + e) * KS;
+    uint8_t *page = pool + static_cast<size_t>(id) * q4_page_bytes(DH) +
+                    (is_v ? (16 * g + 4 * c + q) * 16 + 8 * half + 4 * e : (16 * c + 4 * g + q) * 16);
+    uint8_t *exps = exponents + static_cast<size_t>(id) * q4_page_exps(DH) +
+                    (is_v ? g * 16 * KS + 8 * half + 4 * e + q : (4 * g + q) * 4 * KS + at0);
+    // the lane's word of block s of head h, and the exponent
+    auto word_of = [&](uint32_t block) {
+      const uint32_t h = block / KS, s = block % KS, at = at0 + s;
+      return reinterpret_cast<uint32_t *>(page + h * head_bytes + (is_v ? 1024 * s : at / 4 * 1024 + at % 4 * 4));
+    };
+    auto exp_of = [&](uint32_t block) {
+      const uint32_t h = block / KS, s = block % KS;
+      return exps + h * head_exps + (is_v ? 16 * s : s);
+    };
+    if constexpr (READ) {
+      uint32_t w[kSteps], ex[kSteps];
 #pragma unroll
-          for (int i = 0; i < kGroup; ++i) mine[i * (DH / 2) + lane] = static_cast<uint8_t>(c >> (8 * i));
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+      for (int r = 0; r < kSteps; ++r) {
+        const int block = first_block + 4 * r;
+        w[r] = block < blocks ? *word_of(block) : 0;
+        ex[r] = block < blocks ? *exp_of(block) : 0;
       }
 #pragma unroll
-      for (int it = 0; it < IT; ++it) {
-        const int item = it * 64 + lane, i = item / CH, c = item % CH, t = j * kGroup + i;
-        const bool live = t >= lo && t < hi && i < kGroup;
-        Eight<T> *at = reinterpret_cast<Eight<T> *>(rows + static_cast<size_t>(pg * kPage + t - S) * row + 8 * c);
-        if constexpr (READ) {
-          if (!live) continue;
-          int word = 0, exp;
-          if (is_v) exp = value_exp<DH>(t, c / 4);
-          else key_place<DH>(t, c, word, exp);
-          const uint32_t w = is_v ? *reinterpret_cast<const uint32_t *>(mine + i * (DH / 2) + 4 * c)
-                                  : *reinterpret_cast<const uint32_t *>(page + word);
-          const Eight<T> x = decode<T>(w, __uint_as_float(static_cast<uint32_t>(exps[exp]) << 23));
-          __builtin_memcpy(__builtin_assume_aligned(at, 16), &x, sizeof(x));
-        } else {
-          Eight<T> x = {};
-          if (live) __builtin_memcpy(&x, __builtin_assume_aligned(at, 16), sizeof(x));
-          const uint32_t byte = exponent_byte(quad_max(largest<T>(x)));
-          const uint32_t w = encode<T>(x, __uint_as_float(byte << 23));
-          if (is_v) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (i < kGroup) mine[(4 * c + k) * kGroup + i] = static_cast<uint8_t>(w >> (8 * k));
-            if (live && c % 4 == 0) exps[value_exp<DH>(t, c / 4)] = static_cast<uint8_t>(byte);
-          } else if (live) {
-            int word, exp;
-            key_place<DH>(t, c, word, exp);
-            *reinterpret_cast<uint32_t *>(page + word) = w;
-            if (c % 4 == 0) exps[exp] = static_cast<uint8_t>(byte);
-          }
-        }
+      for (int r = 0; r < kSteps; ++r) {
+        const int block = first_block + 4 * r;
+        const Eight<T> y = decode<T>(is_v ? transposed(w[r], q) : w[r], __uint_as_float(ex[r] << 23));
+        if (live && block < blocks) __builtin_memcpy(__builtin_assume_aligned(line + 32 * block, 16), &y, sizeof(y));
       }
-      if (!READ && is_v) {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        if (lane < DH / 2) {
-          uint8_t *to = page + value_place(j, lane);
-          const uint64_t c = *reinterpret_cast<const uint64_t *>(mine + lane * kGroup);
-          if (lo <= j * kGroup && hi >= (j + 1) * kGroup) {
-            *reinterpret_cast<uint64_t *>(to) = c;
-          } else {
-            for (int i = max(lo - j * kGroup, 0); i < min(hi - j * kGroup, kGroup); ++i)
-              to[i] = static_cast<uint8_t>(c >> (8 * i));
+    } else {
+#pragma unroll
+      for (int r = 0; r < kSteps; ++r) {
+        const int block = first_block + 4 * r;
+        const bool in = block < blocks;
+        const uint32_t byte = exponent_byte(block_max(largest<T>(x[r])));
+        const uint32_t w = encode<T>(x[r], __uint_as_float(byte << 23));
+        if (is_v) {
+          const uint32_t wt = transposed(w, q);
+          if (in && whole) {
+            *word_of(block) = wt;
+          } else if (in) {
+            uint8_t *to = reinterpret_cast<uint8_t *>(word_of(block));
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (4 * quad + j >= S && 4 * quad + j < S + n) to[j] = static_cast<uint8_t>(wt >> (8 * j));
           }
+        } else if (in && live) {
+          *word_of(block) = w;
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        if (in && live && c == 0) *exp_of(block) = static_cast<uint8_t>(byte);
       }
     }
   }
@@ -234,13 +230,13 @@ __global__ __launch_bounds__(64 * kWaves) void kv_q4_kernel(TokensQ4Params p) {
 
 template <typename T, int DH, bool READ>
 hipError_t launch_typed(const TokensQ4Params &p, hipStream_t s) {
-  const int per_plane = p.layers * p.hkv;
-  const int blocks = (p.n_k_planes * per_plane + kWaves - 1) / kWaves +
-                     (p.n_v_planes * per_plane + kWaves - 1) / kWaves;
-  // pages that w_max positions can touch
-  const int pages = (p.w_max + kPage - 2) / kPage + 1;
-  return launch_kernel(kv_q4_kernel<T, DH, READ>, dim3(blocks, p.batch, READ ? min(pages, 65535) : 1),
-                       dim3(64 * kWaves), s, p);
+  const int64_t units = static_cast<int64_t>(p.n_k_planes + p.n_v_planes) * p.layers;
+  // quads that w_max positions can touch, four to a workgroup
+  const int groups = ((p.w_max + 2) / 4 + 1 + 3) / 4;
+  const int shares = (p.hkv * (DH / 32) + 4 * kSteps - 1) / (4 * kSteps);
+  return launch_kernel(kv_q4_kernel<T, DH, READ>,
+                       dim3(static_cast<unsigned>(units * shares), p.batch, groups < 65535 ? groups : 65535),
+                       dim3(64 * kWaves), s, p, shares);
 }
 
 template <bool READ>
