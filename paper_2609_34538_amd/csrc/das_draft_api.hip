@@ -58,7 +58,19 @@ struct PlanQ4 {
 };
 
 // Cuts the units (sequence, KV head) of a call into chunks of equal length, one workgroup
-// each, by the table's width, in tiles of 64 tokens.
+// each, by the table's width, in tiles of 64 tokens. A chunk costs about 5 us beside its tiles
+// (1 us for four of them), and more than one a unit a second launch; without enough of them the
+// longest unit is what the call takes.
+//
+// RW == 1: three a compute unit of a batch, whose lengths differ, one a compute unit of a single
+// sequence; in chunks of at least 32 tiles where that leaves 384 of them, 16 where 256, 8
+// where 128 (us, 4 query heads a KV head, one token each, dh 128, up to 8191 tokens; in
+// parentheses with chunks of 8, 16, 32 and all tiles):
+//   32 units 11.4 (12.2 11.5 15.2 33), 64 units 16.1 (19 16.5 15.7 34), 128 units 23.6 (29 25 24
+//   36), 192 units 29.0 (39 32 29 36), 384 units 51 (69 58 54 59), 512 units 64 (86 73 67 70);
+//   55 units of one sequence, 8192 tokens, 32 rows, dh 96: 20.8 (28 23 22 44).
+// A unit is not cut at all below 16 tiles, and up to 65 where there are 192 of them (256 units,
+// up to 4096 tokens: 21.7; 23.7 with 24 tiles a chunk, 24.3 with 32).
 das_status plan_attn(const das_cache_q4 *cache, const das_batch *b, int hq, int w, PlanQ4 *plan) {
   const das_cache *c = &cache->base;
   if (hq < 1 || hq % c->num_kv_heads != 0) return DAS_ERR_SHAPE;
@@ -73,11 +85,18 @@ das_status plan_attn(const das_cache_q4 *cache, const das_batch *b, int hq, int 
   const long long tiles = 1LL + b->max_pages_per_seq;
   const int rw = q4_row_waves(plan->rows, c->head_dim, es);
   const long long wgs = units * n_rg;  // of one chunk per unit
-  const bool one = rw == 1 && (tiles <= 16 || 4 * wgs >= 3 * kNumCUs);
-  const long long target = rw == 1 && b->batch == 1 ? kNumCUs : 2 * kNumCUs;
-  const long long least = rw == 1 ? (wgs * ((tiles + 3) / 4) <= kNumCUs ? 4 : 8) : rw == 2 ? 2 : 4;
-  long long ns = one ? 1 : std::max<long long>(1, target / wgs);
-  const long long ct = std::max<long long>((tiles + ns - 1) / ns, least);
+  const auto enough = [&](long long ct, long long n) { return wgs * ((tiles + ct - 1) / ct) >= n; };
+  long long ns, least;
+  if (rw == 1) {
+    const bool one = tiles <= 16 || (tiles <= 65 && 4 * wgs >= 3 * kNumCUs);
+    ns = one ? 1 : std::min<long long>((b->batch == 1 ? 1 : 3) * kNumCUs / wgs, 64);
+    least = enough(32, 384) ? 32 : enough(16, 256) ? 16 : enough(8, 128) ? 8 : 4;
+  } else {
+    ns = 2 * kNumCUs / wgs;
+    least = rw == 2 ? 2 : 4;
+  }
+  ns = std::max<long long>(ns, 1);
+  const long long ct = std::max((tiles + ns - 1) / ns, least);
   ns = (tiles + ct - 1) / ct;
   if (units * n_rg * ns * 256 > 0xffffffffLL) return DAS_ERR_SHAPE;
   plan->chunk_tiles = static_cast<int>(ct);
