@@ -5,11 +5,11 @@
 // max(p - q, 0), one after the last tested proposal a token of p, by a second random number:
 // every emitted token then is a draw from p, whatever q is.
 //
-// Weights are w = exp((z - max) / T) in 64 bits, so that a token is another one only where
-// the random number lies within 2^-40 of a border, and sums of equal weights are exact in any
-// order. Residuals are w_p Z_q - w_q Z_p: exactly 0 where both are equal with equal sums;
-// below 2^-40 of p they count as 0, so that rounding leaves no token that p does not exceed q
-// at.
+// Weights are w = exp((z - max) / T) in 64 bits, right to 2^-43.5, and their sums Z to 2^-41.5 (a
+// row's, where each weight may be off by that) or better, so that a token is another one only
+// where the random number lies within 2^-40 of a border. Residuals are w_p Z_q - w_q Z_p: exactly
+// 0 where both are equal with equal sums; below 2^-40 of p they count as 0, so that rounding
+// leaves no token that p does not exceed q at (2 x 2^-41.5 + 2 x 2^-43.5 < 2^-40).
 //
 // Three kernels: the largest logit and the sum of weights of every part of every row; per
 // sequence the run of accepted proposals, and of every part of the row where it ends the sum
@@ -49,47 +49,77 @@ __device__ __forceinline__ double temper(const float *temperature, int b, bool *
   return !ok || T == 0.f ? 0.0 : 32.0 * 1.4426950408889634 / static_cast<double>(T);
 }
 
-// 2^(d c32 / 32) for d <= 0, d c32 >= -32000, in 64 bits: 2^(k / 32 + f / 32), |f| <= 1/2, with
-// 2^(j / 32) from a table of 32 entries, which lie in different banks, and the series of e^(f ln
-// 2 / 32) to f^5 (rest below 2^-48). 1 exactly at d = 0.
-__device__ __forceinline__ double exp2_near(double d, double c32, const double *table) {
-  const double big = __builtin_fma(d, c32, 0x1.8p52);
-  const int k = static_cast<int>(__builtin_bit_cast(uint64_t, big));
-  const double f = __builtin_fma(d, c32, -(big - 0x1.8p52));
-  // (ln 2 / 32)^n / n!
-  double q = 3.9737099845494154e-11;
-  q = __builtin_fma(q, f, 9.172562701824643e-09);
-  q = __builtin_fma(q, f, 1.6938509724371819e-06);
-  q = __builtin_fma(q, f, 2.3459619820224677e-04);
-  q = __builtin_fma(q, f, 2.166084939249829e-02);
-  const double a = table[k & 31];
-  return __builtin_amdgcn_ldexp(__builtin_fma(a * f, q, a), k >> 5);
+// Powers of two in 64 bits, as products a e: a from a table of N entries, 2^(j / N) with j << lg(2^20
+// / N) taken from their upper halves, where the exponent is in units of 1 << 20: adding the
+// numerator, shifted the same way, leaves its quotient by N, rounded down, in the exponent.
+constexpr int kCoarse = 32, kFine = 256;
+template <int N>
+struct Powers {
+  static constexpr int SHIFT = N == kCoarse ? 15 : 12;
+  u32x2 at[N];
+  __device__ __forceinline__ double of(uint32_t k) const {
+    u32x2 t = at[k % N];
+    t[1] += k << SHIFT;
+    return __builtin_bit_cast(double, t);
+  }
+  __device__ __forceinline__ void fill() {  // by all threads, of which there are at least N
+    static_assert(N << SHIFT == 1 << 20, "an octave");
+    if (threadIdx.x < N) {
+      // from the series of e^x - 1 for a 16th of the exponent, doubled four times
+      const double x = threadIdx.x * (0.69314718055994531 / N / 16.0);
+      double q = 1.0 / 40320.0;
+      q = __builtin_fma(q, x, 1.0 / 5040.0);
+      q = __builtin_fma(q, x, 1.0 / 720.0);
+      q = __builtin_fma(q, x, 1.0 / 120.0);
+      q = __builtin_fma(q, x, 1.0 / 24.0);
+      q = __builtin_fma(q, x, 1.0 / 6.0);
+      q = __builtin_fma(q, x, 0.5);
+      q = __builtin_fma(q, x, 1.0);
+      double e = q * x;
+      for (int i = 0; i < 4; ++i) e = __builtin_fma(e, e, 2.0 * e);
+      u32x2 t = __builtin_bit_cast(u32x2, 1.0 + e);
+      t[1] -= threadIdx.x << SHIFT;
+      at[threadIdx.x] = t;
+    }
+    __syncthreads();
+  }
+};
+
+// 2^(d c32 / 32) for d <= 0, d c32 >= -32000: of k + f = d c32, |f| <= 1/2, 2^(k / 32) from the
+// table (kCoarse entries lie in different banks), and 2^(f / 32) by the polynomial 1 + f r(f) of
+// degree 4 whose largest relative error is least, 2^-43.5. 1 exactly at d = 0.
+template <int N>
+__device__ __forceinline__ double exp2_near(double d, double c32, const Powers<N> &table) {
+  constexpr double kRound = 0x1.8p52;  // leaves a sum with it rounded to an integer, in its lower half
+  const double big = __builtin_fma(d, c32, kRound), f = __builtin_fma(d, c32, -(big - kRound));
+  double r = 9.172534833359138e-09;
+  r = __builtin_fma(r, f, 1.6938633790138636e-06);
+  r = __builtin_fma(r, f, 2.3459619821480828e-04);
+  r = __builtin_fma(r, f, 2.166084939172456e-02);
+  return table.of(static_cast<uint32_t>(__builtin_bit_cast(uint64_t, big)) * (N / kCoarse)) * __builtin_fma(r, f, 1.0);
 }
 // The same for any d <= 0; what is under 2^-1000 becomes that.
-__device__ __forceinline__ double exp2_of(double d, double c32, const double *table) {
+template <int N>
+__device__ __forceinline__ double exp2_of(double d, double c32, const Powers<N> &table) {
   return exp2_near(d * c32 < -32000.0 ? -32000.0 / c32 : d, c32, table);
 }
-__device__ __forceinline__ void fill_table(double *table) {
-  if (threadIdx.x < 32) {
-    // 2^(j / 32) from the series of e^x - 1 for a 16th of the exponent, doubled four times
-    const double x = threadIdx.x * (0.69314718055994531 / 32.0 / 16.0);
-    double q = 1.0 / 40320.0;
-    q = __builtin_fma(q, x, 1.0 / 5040.0);
-    q = __builtin_fma(q, x, 1.0 / 720.0);
-    q = __builtin_fma(q, x, 1.0 / 120.0);
-    q = __builtin_fma(q, x, 1.0 / 24.0);
-    q = __builtin_fma(q, x, 1.0 / 6.0);
-    q = __builtin_fma(q, x, 0.5);
-    q = __builtin_fma(q, x, 1.0);
-    double e = q * x;
-    for (int i = 0; i < 4; ++i) e = __builtin_fma(e, e, 2.0 * e);
-    table[threadIdx.x] = 1.0 + e;
-  }
-  __syncthreads();
+// Of a sum with it: the integer part in the lower 20 bits of the upper half (modulo 2^19), the rest
+// in units of 2^-32 in the lower half.
+constexpr double kFixed = 0x1.8p20;
+// -2^(n / 256) as a product a e, of n + kFixed, |n| < 2^18: 2^-41.5 of it is what n's rounding costs
+// at most, 2^-45 the polynomial in its rest (relative error, exactly 1 at 0, the least of degree 3).
+__device__ __forceinline__ void fixed_power(double n, const Powers<kFine> &table, double &a, double &e) {
+  const u32x2 w = __builtin_bit_cast(u32x2, n);
+  const double f = w[0];
+  e = 0x1.c747fdca05451p-125;
+  e = __builtin_fma(e, f, 0x1.ebfbca05b01afp-83);
+  e = __builtin_fma(e, f, 0x1.62e42ff08b09bp-41);
+  e = __builtin_fma(e, f, 1.0);
+  a = table.of(w[1]);
 }
 
 // The weight of logit z at index j of a row.
-__device__ __forceinline__ double weight(float z, int j, const Stat &r, double c32, const double *table) {
+__device__ __forceinline__ double weight(float z, int j, const Stat &r, double c32, const Powers<kCoarse> &table) {
   if (c32 == 0.0 || r.max == kNegInf) return j == r.at ? 1.0 : 0.0;
   if (r.max == __builtin_huge_valf()) return z == r.max ? 1.0 : 0.0;
   const double w = exp2_of(static_cast<double>(z) - static_cast<double>(r.max), c32, table);
@@ -97,7 +127,7 @@ __device__ __forceinline__ double weight(float z, int j, const Stat &r, double c
 }
 // What a draw weighs token `at` by, from the target's and the draft's logits.
 __device__ __forceinline__ double residual(const SampledAcceptParams &p, float zp, float zq, int at, const Chain &ch,
-                                           double cp, double cq, const double *table) {
+                                           double cp, double cq, const Powers<kCoarse> &table) {
   if (at >= p.vocab) return 0.0;
   const double w = weight(zp, at, ch.p, cp, table);
   if (ch.drawn != kLeft) return w;
@@ -201,9 +231,13 @@ constexpr int kDraw = kThreads * 8;                 // tokens of a part of the d
 static_assert(kDraw == kAcceptDraw && sizeof(Stat) == kAcceptStatBytes && sizeof(Chain) == kAcceptChainBytes,
               "the workspace's layout");
 
+// The sums' arithmetic bounds it: 11 operations a logit beside the unpacking and the maximum (1024
+// rows of 65536 bf16 logits twice, 268 MB: 61 us; with 20 operations 74 us, and 64 us with as
+// many registers as the compiler takes by itself, which is 4 waves a SIMD instead of 6).
 template <typename T>
-__global__ __launch_bounds__(kThreads) void accept_stats_kernel(SampledAcceptParams p) {
-  __shared__ double table[32], part_sum[kWavesA];
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) void accept_stats_kernel(SampledAcceptParams p) {
+  __shared__ Powers<kFine> table;
+  __shared__ double part_sum[kWavesA];
   __shared__ float part_max[kWavesA];
   __shared__ int part_at[kWavesA];
   const int part = blockIdx.x % p.parts;
@@ -220,7 +254,7 @@ __global__ __launch_bounds__(kThreads) void accept_stats_kernel(SampledAcceptPar
   const int begin = part * kAcceptPart + static_cast<int>(threadIdx.x) * 8;
 #pragma unroll
   for (int v = 0; v < kVec; ++v) x[v] = load8<T>(src, begin + v * kThreads * 8, p.vocab);
-  fill_table(table);
+  table.fill();
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   float mx = kNegInf;
 #pragma unroll
@@ -232,7 +266,7 @@ __global__ __launch_bounds__(kThreads) void accept_stats_kernel(SampledAcceptPar
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < kWavesA; ++k) mx = fmaxf(mx, part_max[k]);
-  double sum = 0.0;
+  double sum = 0.0, largest = 1.0;  // what the largest logit weighs in the sum
   int at = 0x7fffffff;
   if (c32 == 0.0 || mx == kNegInf) {
 #pragma unroll
@@ -248,15 +282,23 @@ __global__ __launch_bounds__(kThreads) void accept_stats_kernel(SampledAcceptPar
       for (int j = 0; j < 8; ++j) sum += logit<T>(x[v], j) == mx ? 1.0 : 0.0;
   } else if (const float low = static_cast<float>(static_cast<double>(mx) - 28000.0 / c32);
              low > -3e38f && (static_cast<double>(mx) - static_cast<double>(low)) * c32 < 32000.0 &&
-             (static_cast<double>(mx) - static_cast<double>(low)) * c32 > 24000.0) {
+             (static_cast<double>(mx) - static_cast<double>(low)) * c32 > 24000.0 &&
+             fabs(static_cast<double>(mx) * c32) < 0x1p30) {
     // Logits under `low` weigh nothing (2^-875, give or take fp32's rounding of it); as that they,
-    // NaN and -inf need no more tests.
-    const double top = mx;
+    // NaN and -inf need no more tests. The weights are taken relative to the power of two under
+    // the largest, which saves the difference of each logit and the largest, and their sum is
+    // brought to be relative to the largest afterwards.
+    const double step = 8.0 * c32, base = kFixed - 256.0 * floor(static_cast<double>(mx) * step / 256.0), least = low;
+    double a, e;
 #pragma unroll
     for (int v = 0; v < kVec; ++v)
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        sum += exp2_near(static_cast<double>(fmaxf(raw_logit<T>(x[v], j), low)) - top, c32, table);
+      for (int j = 0; j < 8; ++j) {
+        fixed_power(__builtin_fma(fmax(static_cast<double>(raw_logit<T>(x[v], j)), least), step, base), table, a, e);
+        sum = __builtin_fma(a, e, sum);
+      }
+    fixed_power(__builtin_fma(static_cast<double>(mx), step, base), table, a, e);
+    largest = a * e;  // both have the sign of a
   } else {  // so hot that every finite logit counts, or so cold that fp32 has no such `low`
     const double top = mx;
 #pragma unroll 1
@@ -285,12 +327,13 @@ __global__ __launch_bounds__(kThreads) void accept_stats_kernel(SampledAcceptPar
       r.sum += part_sum[k];
       r.at = min(r.at, part_at[k]);
     }
+    r.sum /= largest;
     stats_of(p, side, row)[part] = r;
   }
 }
 
 // A row's parts as one; sums of one-hot rows are 1.
-__device__ __forceinline__ Stat join_parts(const Stat *s, int parts, double c32, const double *table) {
+__device__ __forceinline__ Stat join_parts(const Stat *s, int parts, double c32, const Powers<kCoarse> &table) {
   constexpr int kAhead = 8;
   Stat r = {kNegInf, 0x7fffffff, 0.0};
   for (int k0 = 0; k0 < parts; k0 += kAhead) {
@@ -323,7 +366,7 @@ __device__ __forceinline__ Stat join_parts(const Stat *s, int parts, double c32,
 // `part` of the draw for thread t, and what the draw weighs them by.
 template <typename T>
 __device__ __forceinline__ void draw_weights(const SampledAcceptParams &p, int b, int part, const Chain &ch,
-                                             double cp, double cq, const double *table, double (&w)[8]) {
+                                             double cp, double cq, const Powers<kCoarse> &table, double (&w)[8]) {
   const int64_t row = static_cast<int64_t>(b) * p.w + ch.accepted;
   const bool drafted = ch.drawn == kLeft && p.draft;
   const int first = part * kDraw + static_cast<int>(threadIdx.x) * 8;
@@ -351,7 +394,8 @@ __device__ __forceinline__ double part_total(const double (&w)[8], double *seg) 
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void accept_chain_kernel(SampledAcceptParams p) {
-  __shared__ double table[32], seg[kWavesA];
+  __shared__ Powers<kCoarse> table;
+  __shared__ double seg[kWavesA];
   __shared__ Chain chain;
   __shared__ Stat drafts[64];
   __shared__ double draft_weight[64];
@@ -372,7 +416,7 @@ __global__ __launch_bounds__(kThreads) void accept_chain_kernel(SampledAcceptPar
     if (y >= 0 && y < p.vocab) zy = to_f32<T>(rows[at_row * (wave == 0 ? p.target_stride : p.draft_stride) + y]);
   }
   const float u = wave == 0 && lane < p.w ? p.uniform[at_row] : 0.f;
-  fill_table(table);
+  table.fill();
   Stat s = {kNegInf, 0, 1.0};
   double wy = 0.0;
   if (mine) {
@@ -431,7 +475,8 @@ __global__ __launch_bounds__(kThreads) void accept_chain_kernel(SampledAcceptPar
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void accept_draw_kernel(SampledAcceptParams p) {
-  __shared__ double table[32], seg[kWavesA], lefts[kAcceptMostDraws];
+  __shared__ Powers<kCoarse> table;
+  __shared__ double seg[kWavesA], lefts[kAcceptMostDraws];
   const int b = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   Chain ch = *chain_of(p, b);
   for (int k = threadIdx.x; k < p.draw_parts; k += kThreads) lefts[k] = lefts_of(p, b)[k];
@@ -440,7 +485,7 @@ __global__ __launch_bounds__(kThreads) void accept_draw_kernel(SampledAcceptPara
   const double cp = temper(p.temperature, b, &bad);
   const double cq = p.draft ? temper(p.draft_temperature, b, &bad) : 0.0;
   const float number = p.draw[b];
-  fill_table(table);
+  table.fill();
   // the running sum over the parts: a lane's parts, then the lanes before
   auto total_of = [&]() {
     double sum = 0.0;
