@@ -594,7 +594,7 @@ das_status das_kv_append_q4(const das_cache_q4 *cache, const das_batch *batch, c
  *          (DAS_DEVERR_PAGE).
  *
  * w_max in 1..DAS_MAX_READ, batch * w_max * Hkv * head_dim < 2^46. k_out and v_out are
- * 16-byte aligned and must not overlap the cache or each other.
+ * 16-byte aligned and overlap neither the cache nor each other (DAS_ERR_SHAPE).
  */
 das_status das_kv_read_q4(const das_cache_q4 *cache, const das_batch *batch, const int32_t *first,
                           const int32_t *num, int32_t w_max, void *k_out, void *v_out,
@@ -687,8 +687,8 @@ das_status das_qk_rope(const das_rope *rope, int32_t batch, int32_t block_len, c
  *
  * Rows past what is checked (and the row after it) are not read. batch in 1..65535, block_len
  * in 1..DAS_MAX_BLOCK, vocab in 1..DAS_MAX_VOCAB. Logits are aligned to their type, the other
- * arrays to 4 bytes; outputs must not overlap the inputs or each other. Entries of emitted and
- * probs past num_emitted[b] are left alone. Equal calls give equal bits.
+ * arrays to 4 bytes; outputs overlap neither the inputs nor each other (DAS_ERR_SHAPE). Entries
+ * of emitted and probs past num_emitted[b] are left alone. Equal calls give equal bits.
  */
 size_t das_sampled_accept_workspace_bytes(int32_t batch, int32_t block_len, int32_t vocab);
 das_status das_sampled_accept(int32_t batch, int32_t block_len, int32_t vocab, int32_t dtype,

@@ -138,13 +138,14 @@ das_status tokens_params(const das_cache_q4 *cache, const das_batch *batch, cons
   return DAS_OK;
 }
 
-// Bytes from the first to the last element of [B][w][heads][dh] at these distances, and
-// whether there are none between its rows.
+// An array, its bytes from the first to the last element, and whether there are none between
+// its rows.
 struct Span {
   const void *at;
   uint64_t bytes;
-  bool dense;
+  bool dense = true;
 };
+// That of [B][w][heads][dh] at these distances; false where they are none.
 bool span_of(const void *at, int batch, int w, int heads, int dh, int64_t sb, int64_t st, int es, Span *out) {
   const int64_t row = static_cast<int64_t>(heads) * dh;
   constexpr int64_t kMost = INT64_MAX >> 4;
@@ -283,6 +284,16 @@ das_status das_kv_read_q4(const das_cache_q4 *cache, const das_batch *batch, con
   if (per * std::max(c->num_k_planes, c->num_v_planes) >= 0x1p62) return DAS_ERR_SHAPE;
   const uint64_t k_bytes = static_cast<uint64_t>(per) * c->num_k_planes, v_bytes = static_cast<uint64_t>(per) * c->num_v_planes;
   if (overlap(k_out, k_bytes, v_out, v_bytes)) return DAS_ERR_SHAPE;
+  const double heads = static_cast<double>(c->num_layers) * c->num_kv_heads * c->num_pages;
+  const auto bytes_of = [&](int planes, int of_page) {
+    return static_cast<uint64_t>(std::min(heads * planes * of_page, 0x1p62));
+  };
+  const Span held[] = {{c->k_pool, bytes_of(c->num_k_planes, q4_page_bytes(c->head_dim))},
+                       {c->v_pool, bytes_of(c->num_v_planes, q4_page_bytes(c->head_dim))},
+                       {cache->k_exp, bytes_of(c->num_k_planes, q4_page_exps(c->head_dim))},
+                       {cache->v_exp, bytes_of(c->num_v_planes, q4_page_exps(c->head_dim))}};
+  for (const Span &h : held)
+    if (overlap(k_out, k_bytes, h.at, h.bytes) || overlap(v_out, v_bytes, h.at, h.bytes)) return DAS_ERR_SHAPE;
   p.first = first;
   p.limit = batch->prefix_len;
   p.num = num;
@@ -410,6 +421,19 @@ das_status das_sampled_accept(int32_t batch, int32_t block_len, int32_t vocab, i
     return DAS_ERR_SHAPE;
   if (!workspace || workspace_bytes < accept_workspace(batch, block_len, vocab) || !aligned(workspace, 256))
     return DAS_ERR_WORKSPACE;
+  // every workgroup of a sequence reads its inputs, one of them writes its results
+  const uint64_t seqs = 4ull * batch, all = 4ull * rows;
+  const Span in[] = {{proposals, all},         {uniform, all}, {draw, seqs}, {temperature, seqs},
+                     {draft_temperature, seqs}, {tested, seqs},
+                     {target_logits, ((rows - 1) * target_stride + vocab) * es},
+                     {draft_logits, ((rows - 1) * draft_stride + vocab) * es}};
+  const Span out[] = {{accepted, seqs}, {num_keep, seqs}, {num_emitted, seqs}, {emitted, all}, {probs, all}};
+  for (const Span &o : out) {
+    for (const Span &i : in)
+      if (overlap(o.at, o.bytes, i.at, i.bytes)) return DAS_ERR_SHAPE;
+    for (const Span *other = out; other != &o; ++other)
+      if (overlap(o.at, o.bytes, other->at, other->bytes)) return DAS_ERR_SHAPE;
+  }
   SampledAcceptParams p;
   p.proposals = proposals;
   p.target = target_logits;

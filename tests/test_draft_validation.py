@@ -172,6 +172,29 @@ def test_accept_refusals(kw, status):
     assert LIB.das_sampled_accept(*{**ACCEPT, **kw}.values(), None) == status
 
 
+APART = dict(ACCEPT, y=FAKE * 2, zp=FAKE * 3, zq=FAKE * 4, T=FAKE * 5, Tq=FAKE * 6, m=FAKE * 7, u=FAKE * 8, v=FAKE * 9,
+             acc=FAKE * 10, keep=FAKE * 11, emit=FAKE * 12, n=FAKE * 13, pr=FAKE * 14)
+
+
+@pytest.mark.parametrize("out", ["acc", "keep", "emit", "n", "pr"])
+@pytest.mark.parametrize("other,at", [("y", 20), ("u", 20), ("v", 4), ("T", 4), ("Tq", 4), ("m", 4), ("zp", 5 * 400 + 396),
+                                      ("zq", 5 * 400 + 396), ("acc", 4), ("keep", 4), ("emit", 20), ("n", 4), ("pr", 20)])
+def test_results_of_the_verification_overlap_nothing(out, other, at):
+    if out != other:
+        for where in (0, at):  # the first element and the last of the other
+            assert LIB.das_sampled_accept(*{**APART, out: APART[other] + where}.values(), None) == SHAPE
+
+
+@pytest.mark.parametrize("held", ["k_pool", "v_pool", "k_exp", "v_exp"])
+def test_read_back_does_not_overlap_the_cache(held):
+    at = dict(k_pool=FAKE * 16, v_pool=FAKE * 32, k_exp=FAKE * 48, v_exp=FAKE * 64)
+    planes = 2 if held[0] == "k" else 1
+    last = planes * 2 * 8 * 50 * (32 * 96 if held.endswith("pool") else 2 * 96) - 16
+    for where in (0, last):
+        assert _read(_cache(**at), _batch(), k=at[held] + where, v=FAKE * 80) == SHAPE
+        assert _read(_cache(**at), _batch(), v=at[held] + where, k=FAKE * 80) == SHAPE
+
+
 def _tensors():
     cache = das.Quant4Cache.empty(2, 2, 5, 64, 2, {1: 0, 2: 1}, {2: 0}, device="cpu")
     batch = das.Batch(torch.zeros(3, dtype=torch.int32), torch.zeros((3, 2), dtype=torch.int32))

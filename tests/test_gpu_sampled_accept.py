@@ -95,7 +95,7 @@ class Call:
             n = len(tokens)
             assert got["accepted"][b] == a and got["num_keep"][b] == n and got["num_emitted"][b] == n, b
             assert got["emitted"][b].tolist() == tokens + [-9] * (w - n), b
-            # one rounding to fp32 of a value good to 2^-44
+            # one rounding to fp32 of a value good to 2^-40
             assert (np.abs(got["probs"][b, :n] - probs) <= 2.0 ** -24 * np.array(probs) + 2.0 ** -149).all(), b
             assert (got["probs"][b, n:] == -9).all()
         assert int(self.err) == error
@@ -137,6 +137,19 @@ def test_temperatures_and_tested(dtype):
     got = Call(z, d, y, T, Tq, tested).check()
     assert got["accepted"][1] == 0 and got["accepted"].max() >= 2
     Call(z, None, z.float().argmax(-1).int(), T, None, tested).check()
+
+
+@pytest.mark.parametrize("offset", [1.0e6, 1.1e6, 1.3e6, -1.0e6, -1.3e6, 2.0e9])
+def test_large_logits_at_a_low_temperature(offset):
+    """Logits times 32 log2(e) / T on both sides of 2^30, where weights are taken in another way;
+    in steps of a sixteenth and more, with parts of a row apart by more than the range."""
+    B, w, V = 3, 4, 20000
+    z, d = _logits(6, B, w, V, F32, gain=0.5)
+    z[:, :, 9000:], d[:, :, 9000:] = z[:, :, 9000:] - 0.3 * abs(offset), d[:, :, 9000:] - 0.3 * abs(offset)
+    z[1], d[1] = z[1].flip(-1), d[1].flip(-1)
+    z, d, T = z + offset, d + offset, torch.full((B,), 0.05 if abs(offset) < 1e9 else 200.0, device=DEV)
+    Call(z, d, _drawn(1, d, float(T[0])), T, T).check()
+    Call(z, None, z.argmax(-1).int(), T).check()
 
 
 def test_rows_apart_and_off_alignment():
