@@ -332,14 +332,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) v
   }
 }
 
-// A row's parts as one; sums of one-hot rows are 1.
-__device__ __forceinline__ Stat join_parts(const Stat *s, int parts, double c32, const Powers<kCoarse> &table) {
-  constexpr int kAhead = 8;
+// A row's parts as one; sums of one-hot rows are 1. `x`: the first kAhead of them (the last, where
+// there are fewer), as load_parts has them.
+constexpr int kAhead = 8;
+__device__ __forceinline__ void load_parts(Stat (&x)[kAhead], const Stat *s, int from, int parts) {
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) x[k] = s[min(from + k, parts - 1)];
+}
+__device__ __forceinline__ Stat join_parts(Stat (&x)[kAhead], const Stat *s, int parts, double c32,
+                                           const Powers<kCoarse> &table) {
   Stat r = {kNegInf, 0x7fffffff, 0.0};
   for (int k0 = 0; k0 < parts; k0 += kAhead) {
-    Stat x[kAhead];
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) x[k] = s[min(k0 + k, parts - 1)];
+    if (k0) load_parts(x, s, k0, parts);
     float mx = r.max;
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) mx = fmaxf(mx, x[k].max);
@@ -401,26 +405,33 @@ __global__ __launch_bounds__(kThreads) void accept_chain_kernel(SampledAcceptPar
   __shared__ double draft_weight[64];
   const int b = blockIdx.x / p.draw_parts, part = blockIdx.x % p.draw_parts;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  // all that needs no other result first, in one round trip: lane i of the first two waves has
+  // position i of the target and of the draft
+  const int64_t at_row = static_cast<int64_t>(b) * p.w + lane;
+  const bool sided = lane < p.w && (wave == 0 || (wave == 1 && p.draft));
+  Stat parts[kAhead];
+  int y = 0;
+  float u = 0.f;
+  if (sided) {
+    y = p.proposals[at_row];
+    u = p.uniform[at_row];
+    load_parts(parts, stats_of(p, wave, at_row), 0, p.parts);  // those that nobody asked for are not used
+  }
   bool bad_temp = false, bad_tested = false;
   const int m = tested_of(p, b, &bad_tested);
   const double cp = temper(p.temperature, b, &bad_temp);
   const double cq = p.draft ? temper(p.draft_temperature, b, &bad_temp) : 0.0;
-  // lane i of the first two waves: position i of the target and of the draft
-  const int64_t at_row = static_cast<int64_t>(b) * p.w + lane;
-  const bool mine = lane < p.w && (wave == 0 ? lane <= m : wave == 1 && p.draft && lane < m);
-  int y = 0;
+  const bool mine = sided && (wave == 0 ? lane <= m : lane < m);
   float zy = kNegInf;
   if (mine && lane < m) {
-    y = p.proposals[at_row];
     const T *rows = static_cast<const T *>(wave == 0 ? p.target : p.draft);
     if (y >= 0 && y < p.vocab) zy = to_f32<T>(rows[at_row * (wave == 0 ? p.target_stride : p.draft_stride) + y]);
   }
-  const float u = wave == 0 && lane < p.w ? p.uniform[at_row] : 0.f;
   table.fill();
   Stat s = {kNegInf, 0, 1.0};
   double wy = 0.0;
   if (mine) {
-    s = join_parts(stats_of(p, wave, at_row), p.parts, wave == 0 ? cp : cq, table);
+    s = join_parts(parts, stats_of(p, wave, at_row), p.parts, wave == 0 ? cp : cq, table);
     if (lane < m) wy = weight(no_nan(zy), y, s, wave == 0 ? cp : cq, table);
   }
   if (wave == 1) {
