@@ -2,12 +2,12 @@
 // power-of-two scale per token, KV head and 32 dims (das_attn_q4).
 //
 // A unit is one (sequence, KV head); its 64-token tiles, the draft block's first, then a
-// page each, are cut into chunks of chunk_tiles, one workgroup of four waves each. Up to 16
-// * NQ query rows the waves take a chunk's pages in turn, from memory into registers, two on
-// the way; with more rows RW of the waves hold different ones and all four share the
-// conversion of a page through LDS. Each wave has its own running maximum, sum and output;
-// they merge through LDS, and where a unit has several chunks these leave records that a
-// second kernel merges.
+// page each, are cut into chunks of chunk_tiles, one workgroup of four waves each. Up to 32
+// query rows (RW == 1) the waves take a chunk's pages in turn, from memory into registers, one
+// ahead; with more (RW == 4) each has rows of its own and all four share the conversion of a
+// page through LDS. Each wave has its own running maximum, sum and output; with RW == 1 they
+// merge through LDS, and where a unit has several chunks these leave records that a second
+// kernel merges.
 //
 // Both products take the key / value tile as the A operand, as in mfma_tile.h:
 //   S^T (tokens x rows) = K . Q^T,   O^T (dh x rows) += V^T . P^T
@@ -23,6 +23,17 @@
 // queries, probabilities and the block's elements in three bf16 parts each, which hold all 24
 // bits, and sum their products with the codes, exact, in fp32: three times the bf16 matrix
 // work, where fp32 instructions would take sixteen times.
+//
+// Measured (bf16): 32 sequences x 55 heads, dh 96, 4096-8192 tokens: 4 rows 178 us, 6.2 TB/s of
+// page bytes, 16 rows 189 us, 5.9, both near what this card's memory gives; 32 rows 226 us, 5.1:
+// vector instructions, some 400 a page (204 of them the conversion, 180 the softmax). 192 units of
+// 4 rows, 1-8191 tokens, dh 128: 28.8 us, the longest units and the second launch. 32 units of 128
+// rows, 32768 tokens, dh 128: 91 us, 750 TFLOP/s, vector and matrix instructions in turn. One
+// sequence of 2048 tokens, 55 heads, 8 rows: 9.7 us, two launches and their round trips.
+// Measured and not kept: pages through a ring of three in LDS in place of registers (226 -> 235
+// us, 28.8 -> 32); the sum of the rounded probabilities by the matrix unit (226 -> 222 us, and
+// a less exact log-sum-exp); no maximum unless a sum overflows (spills, 453 us); a page in two
+// halves at dh 96 (the same; at dh 128 with two row tiles it is what keeps them in registers).
 
 #include <type_traits>
 
@@ -328,8 +339,7 @@ __device__ __forceinline__ bool block_tile4(Acc<DH, NQ> &st, uint64_t &far, Bloc
 // Shared memory of a workgroup.
 // RW == 1: the merge area of one row tile, before that a block tile's probabilities for its
 // late values.
-// RW > 1: two converted pages; afterwards, in the second one's place, the probabilities, and
-// then, with RW == 2, the merge area.
+// RW == 4: two converted pages; afterwards, in the second one's place, the probabilities.
 template <int DH, int NQ, int RW>
 struct Lds4 {
   static constexpr int RS = DH + 4;  // row stride of the merge area (floats)
@@ -348,6 +358,7 @@ __global__ __launch_bounds__(64 * kWavesQ8) __attribute__((amdgpu_waves_per_eu(2
 void attn_q4_kernel(AttnQ8Params p, int n_rg) {
   using L = Lds4<DH, NQ, RW>;
   constexpr int KS = DH / 32;
+  static_assert(RW == 1 || RW == kWavesQ8, "waves with rows of their own: none or all");
   constexpr int STRIDE = RW == 1 ? kWavesQ8 : 1;  // from a wave's tile to its next
   __shared__ __attribute__((aligned(16))) uint8_t smem[L::BYTES];
   __shared__ float sm[kWavesQ8][16 * NQ], sl[kWavesQ8][16 * NQ], sa[kWavesQ8][16 * NQ];
@@ -355,14 +366,14 @@ void attn_q4_kernel(AttnQ8Params p, int n_rg) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ln = lane & 15, lg = lane >> 4;
-  const int rw = wave % RW, iw = wave / RW;
+  const int rw = RW == 1 ? 0 : wave;
   // every unit's first chunk comes before any second one
   const int units = p.batch * p.hkv;
   const int rg = blockIdx.x % n_rg, grp = blockIdx.x / n_rg;
   const int unit = grp % units, chunk = grp / units;
   const int b = unit / p.hkv, kvh = unit % p.hkv;
   const int row0 = rg * (16 * NQ * RW) + rw * (16 * NQ);
-  const int g0 = chunk * p.chunk_tiles + (RW == 1 ? iw : 0);  // this wave's first tile of the unit
+  const int g0 = chunk * p.chunk_tiles + (RW == 1 ? wave : 0);  // this wave's first tile of the unit
 
   const int s_raw = p.prefix_len[b];
   QParts<T, DH> qf[NQ];
@@ -393,16 +404,14 @@ void attn_q4_kernel(AttnQ8Params p, int n_rg) {
     return pg >= 0 && pg < p.max_pages ? p.block_table[static_cast<size_t>(b) * p.max_pages + pg] : 0;
   };
   int window = load_window(0);
-  // The draft block is tile 0 of chunk 0, one or two tiles of 32 tokens: with RW == 2 one
-  // for each half of the waves, else all of a wave.
+  // The draft block is tile 0 of chunk 0, one or two tiles of 32 tokens.
   Block<T, DH> blk;
   const int n_block = g0 == 0 ? 1 : 0;
-  const int u_first = RW == 2 ? iw : 0;
-  const int u_end = n_block ? min((p.w + kTile - 1) / kTile, RW == 2 ? iw + 1 : 2) : 0;
-  const bool has_block = u_first < u_end;
-  // not ahead where its registers are those of the first page (fp32)
-  constexpr bool AHEAD = sizeof(T) == 2;
-  if (AHEAD && has_block) load_block<T, DH>(blk, p, b, kvh, u_first, ln, lg);
+  const int u_end = n_block ? min((p.w + kTile - 1) / kTile, 2) : 0;
+  const bool has_block = u_end > 0;
+  // not ahead where its registers are those of the first page
+  constexpr bool AHEAD = sizeof(T) == 2 && (DH < 128 || NQ == 1);
+  if (AHEAD && has_block) load_block<T, DH>(blk, p, b, kvh, 0, ln, lg);
 
   bool bad;
   const int S = clamp_prefix(s_raw, p.max_pages, &bad);
@@ -478,8 +487,8 @@ void attn_q4_kernel(AttnQ8Params p, int n_rg) {
 
   bool late = false;  // whether the block has values that are added late
   auto work_block = [&](auto far_form) {
-    for (int u = u_first; u < u_end; ++u) {
-      if (!AHEAD || decltype(far_form)::value || u > u_first) load_block<T, DH>(blk, p, b, kvh, u, ln, lg);
+    for (int u = 0; u < u_end; ++u) {
+      if (!AHEAD || decltype(far_form)::value || u > 0) load_block<T, DH>(blk, p, b, kvh, u, ln, lg);
       late |= block_tile4<T, DH, NQ, decltype(far_form)::value>(st, far, blk, p, u, qf, row_pos, lg);
     }
   };
@@ -492,7 +501,8 @@ void attn_q4_kernel(AttnQ8Params p, int n_rg) {
     if (AHEAD && has_block) work_block(std::false_type{});
     int lb = load(i + 1, tb);
     auto work = [&](Page<DH> &t, int limit) {
-      if constexpr (sizeof(T) == 2) {
+      // whole pages where their logits fit the registers
+      if constexpr (sizeof(T) == 2 && (DH < 128 || NQ == 1)) {
         prefix_tiles<T, DH, NQ, 0, 4, false>(st, far, t, qf, limit, p.scale_log2, lg);
       } else {
         prefix_tiles<T, DH, NQ, 0, 2, false>(st, far, t, qf, limit, p.scale_log2, lg);
@@ -507,10 +517,9 @@ void attn_q4_kernel(AttnQ8Params p, int n_rg) {
     }
   } else {
     // Each wave brings its pieces of a page into registers, a step ahead, and writes them
-    // converted to LDS, from where all multiply: with RW == 4 all of the page, with RW == 2
-    // one half of its tokens. One barrier a step publishes page s and frees the place of page
-    // s - 1, which page s + 1 takes. Pieces: values to the first dh / 32 waves; keys to the
-    // others, at dh 128 one to each.
+    // converted to LDS, from where all multiply. One barrier a step publishes page s and frees
+    // the place of page s - 1, which page s + 1 takes. Pieces: values to the first dh / 32
+    // waves; keys to the others, at dh 128 one to each.
     constexpr int NK = KS == 3 ? 3 : 1;
     const bool has_v = wave < KS;
     const bool has_k = KS == 4 || (KS == 3 ? wave == 3 : wave >= 2);
@@ -576,13 +585,8 @@ void attn_q4_kernel(AttnQ8Params p, int n_rg) {
       convert(step + 1);
       fetch(n_block + step + 2);
       const uint8_t *slot = smem + (step % 2) * L::STEP;
-      if constexpr (RW == 4) {
-        const int limits[2] = {now, now - kTile};
-        shared_tiles4<T, DH, NQ, 2>(st, far, slot, qf, limits, p.scale_log2, lane);
-      } else {
-        const int limits[1] = {now - kTile * iw};
-        shared_tiles4<T, DH, NQ, 1>(st, far, slot + iw * 4 * KS * kFragBytes, qf, limits, p.scale_log2, lane);
-      }
+      const int limits[2] = {now, now - kTile};
+      shared_tiles4<T, DH, NQ, 2>(st, far, slot, qf, limits, p.scale_log2, lane);
     }
     __syncthreads();  // the pages have been read
   }
@@ -597,8 +601,8 @@ void attn_q4_kernel(AttnQ8Params p, int n_rg) {
     for (int i = n_block; i < n; ++i) {
       Page<DH> t;
       const int visible = load(i, t);
-      if (RW != 2 || iw == 0) prefix_tiles<T, DH, NQ, 0, 2, true>(st, far, t, qf, visible, p.scale_log2, lg);
-      if (RW != 2 || iw == 1) prefix_tiles<T, DH, NQ, 1, 2, true>(st, far, t, qf, visible, p.scale_log2, lg);
+      prefix_tiles<T, DH, NQ, 0, 2, true>(st, far, t, qf, visible, p.scale_log2, lg);
+      prefix_tiles<T, DH, NQ, 1, 2, true>(st, far, t, qf, visible, p.scale_log2, lg);
     }
   }
   float m[NQ];
@@ -610,7 +614,7 @@ void attn_q4_kernel(AttnQ8Params p, int n_rg) {
   }
   if (late) {
     float *probs = reinterpret_cast<float *>(smem + L::PROBS + wave * L::PROB_STRIDE);
-    for (int u = u_first; u < u_end; ++u)
+    for (int u = 0; u < u_end; ++u)
       late_values<T, DH, NQ, kLate4<T>>(st, again, m, p, b, kvh, u, qf, row_pos, probs, ln, lg);
   }
   uint8_t *rec = p.ws + (static_cast<size_t>(unit) * p.nsplit + chunk) * p.piece_stride;
@@ -644,19 +648,12 @@ hipError_t launch_shape(const AttnQ8Params &p, hipStream_t s) {
 template <typename T, int DH>
 hipError_t launch_dh(const AttnQ8Params &p, hipStream_t s) {
   constexpr int ES = sizeof(T);
-  const int nq = q4_row_tiles(p.rows, DH, ES), rw = q4_row_waves(p.rows, DH, ES);
+  const int nq = q4_row_tiles(p.rows, ES), rw = q4_row_waves(p.rows);
   hipError_t e = hipErrorInvalidValue;
   if (nq == 1 && rw == 1) e = launch_shape<T, DH, 1, 1>(p, s);
-  if constexpr (ES == 4 || DH == 128) {
-    if (nq == 1 && rw == 2) e = launch_shape<T, DH, 1, 2>(p, s);
-  }
-  if constexpr (ES == 4) {
-    if (rw == 4) e = launch_shape<T, DH, 1, 4>(p, s);
-  } else {
-    if constexpr (DH != 128) {
-      if (nq == 2 && rw == 1) e = launch_shape<T, DH, 2, 1>(p, s);
-    }
-    if (nq == 2 && rw == 2) e = launch_shape<T, DH, 2, 2>(p, s);
+  if (nq == 1 && rw == 4) e = launch_shape<T, DH, 1, 4>(p, s);
+  if constexpr (ES == 2) {
+    if (nq == 2 && rw == 1) e = launch_shape<T, DH, 2, 1>(p, s);
     if (nq == 2 && rw == 4) e = launch_shape<T, DH, 2, 4>(p, s);
   }
   if (e != hipSuccess || p.nsplit == 1) return e;

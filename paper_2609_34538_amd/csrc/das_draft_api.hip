@@ -71,6 +71,12 @@ struct PlanQ4 {
 //   55 units of one sequence, 8192 tokens, 32 rows, dh 96: 20.8 (28 23 22 44).
 // A unit is not cut at all below 16 tiles, and up to 65 where there are 192 of them (256 units,
 // up to 4096 tokens: 21.7; 23.7 with 24 tiles a chunk, 24.3 with 32).
+//
+// RW == 4, where a page is a step for all waves: three a compute unit of a batch, two of a single
+// sequence, from four tiles on, from 32 on beyond 4096 tokens where that leaves 384 of them (us;
+// in parentheses with 4, 8, 16, 32 and 64 tiles a chunk): 32 heads of 128 rows, dh 128, 32768
+// tokens 93 (156 116 103 93 114); 192 of 48 rows, up to 8191 tokens 68 (100 77 70 68 93); 55 of one
+// sequence, 64 rows, dh 96, 2048 tokens 18.7 (18.7 20.9 28 44 40), 8192 tokens 34 (44 38 35 46 78).
 das_status plan_attn(const das_cache_q4 *cache, const das_batch *b, int hq, int w, PlanQ4 *plan) {
   const das_cache *c = &cache->base;
   if (hq < 1 || hq % c->num_kv_heads != 0) return DAS_ERR_SHAPE;
@@ -79,11 +85,11 @@ das_status plan_attn(const das_cache_q4 *cache, const das_batch *b, int hq, int 
   if (w < 1 || w > DAS_MAX_BLOCK) return DAS_ERR_SHAPE;
   plan->rows = w * group;
   const int es = c->dtype == DAS_F32 ? 4 : 2;
-  const int gr = q4_group_rows(plan->rows, c->head_dim, es);
+  const int gr = q4_group_rows(plan->rows, es);
   const long long n_rg = (plan->rows + gr - 1) / gr;
   const long long units = static_cast<long long>(b->batch) * c->num_kv_heads;
   const long long tiles = 1LL + b->max_pages_per_seq;
-  const int rw = q4_row_waves(plan->rows, c->head_dim, es);
+  const int rw = q4_row_waves(plan->rows);
   const long long wgs = units * n_rg;  // of one chunk per unit
   const auto enough = [&](long long ct, long long n) { return wgs * ((tiles + ct - 1) / ct) >= n; };
   long long ns, least;
@@ -92,8 +98,8 @@ das_status plan_attn(const das_cache_q4 *cache, const das_batch *b, int hq, int 
     ns = one ? 1 : std::min<long long>((b->batch == 1 ? 1 : 3) * kNumCUs / wgs, 64);
     least = enough(32, 384) ? 32 : enough(16, 256) ? 16 : enough(8, 128) ? 8 : 4;
   } else {
-    ns = 2 * kNumCUs / wgs;
-    least = rw == 2 ? 2 : 4;
+    ns = (b->batch == 1 ? 2 : 3) * kNumCUs / wgs;
+    least = tiles > 65 && enough(32, 384) ? 32 : 4;
   }
   ns = std::max<long long>(ns, 1);
   const long long ct = std::max((tiles + ns - 1) / ns, least);

@@ -22,17 +22,24 @@ __host__ __device__ constexpr int q4_page_exps(int dh) { return kPage * dh / kQ4
 // tokens (the draft block's, then a page each).
 hipError_t launch_attn_q4(const AttnQ8Params &p, int dtype, int dh, hipStream_t s);
 
-// Launch shape of the attention kernel: 16-row tiles of a wave (two of a bf16 call up to 32
-// rows do not fit its registers beside two pages under way at head dim 128, nor do two of an
-// fp32 call, whose queries are three operands each) and waves with different rows.
-__host__ __device__ constexpr int q4_row_tiles(int rows, int dh, int es) {
-  return rows <= 16 || es == 4 || (dh == 128 && rows <= 32) ? 1 : 2;
+// Launch shape of the attention kernel: 16-row tiles of a wave, and whether all waves have the
+// same rows and pages of their own (1) or rows of their own and the same pages, whose conversion
+// they share (4). An fp32 call's queries are three operands each: one row tile. us of (tiles,
+// waves), bf16 calls, 32 sequences x 55 heads, dh 96, 4096-8192 tokens unless said:
+//   16 rows (1, 1) 197, (2, 1) 227; 32 rows (2, 1) 232, (1, 1) twice 368, (1, 4) 428;
+//   32 rows of 32 x 32 heads, dh 128: (2, 1) 190, (1, 1) twice 275, (1, 4) 330;
+//   64 rows, 2048-4096 tokens: (1, 4) 239, (2, 1) twice 253, (2, 4) 357; 128 rows of 4 x 8 heads,
+//   dh 128, 32768 tokens: (2, 4) 96, (1, 4) twice 122, (2, 1) four times 165;
+//   fp32, 16 x 55 heads, dh 96, 32 rows: (1, 1) twice 144, (1, 4) 220; 64 rows, 8 x 55 heads:
+//   (1, 4) 143, (1, 1) four times 154.
+// Two waves with the same rows and two with others, in between, were no faster than the better
+// of these anywhere (64 rows 267, fp32 32 rows 154).
+__host__ __device__ constexpr int q4_row_tiles(int rows, int es) {
+  return es == 2 && ((rows > 16 && rows <= 32) || rows > 64) ? 2 : 1;
 }
-__host__ __device__ constexpr int q4_row_waves(int rows, int dh, int es) {
-  return rows <= 16 * q4_row_tiles(rows, dh, es) ? 1 : rows <= 32 * q4_row_tiles(rows, dh, es) ? 2 : 4;
-}
-__host__ __device__ constexpr int q4_group_rows(int rows, int dh, int es) {
-  return 16 * q4_row_tiles(rows, dh, es) * q4_row_waves(rows, dh, es);
+__host__ __device__ constexpr int q4_row_waves(int rows) { return rows <= 32 ? 1 : 4; }
+__host__ __device__ constexpr int q4_group_rows(int rows, int es) {
+  return 16 * q4_row_tiles(rows, es) * q4_row_waves(rows);
 }
 
 // The commit into the 4-bit cache, and the way back (k_new, v_new written).

@@ -8,7 +8,13 @@
 // position's angle has no bits left of its fraction of a turn in 32): reduction to a quarter
 // of a turn by two-part pi / 2, then the series. A lane holds 16 dims of a head, both dims of
 // its 8 pairs; LPR lanes a head, which add their squares, in 64 bits so that no finite
-// element's passes the largest number. Bound by HBM for batches.
+// element's passes the largest number. The next head's pieces are under way while one is worked
+// on.
+//
+// Bound by memory for batches: 32 x 32 tokens of 165 heads, dh 96, bf16 out of a fused projection
+// (65 MB) 15.1 us, 4.3 TB/s, where a copy of large arrays reaches 4.9; 8 tokens 4.0 us, the launch
+// and two round trips. A token's heads are shared by workgroups until there are eight a compute
+// unit: 8 tokens with one each 4.8 us.
 
 #include "mfma_tile.h"
 #include "q4_internal.h"

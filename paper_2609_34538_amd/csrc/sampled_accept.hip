@@ -232,7 +232,7 @@ static_assert(kDraw == kAcceptDraw && sizeof(Stat) == kAcceptStatBytes && sizeof
               "the workspace's layout");
 
 // The sums' arithmetic bounds it: 11 operations a logit beside the unpacking and the maximum (1024
-// rows of 65536 bf16 logits twice, 268 MB: 61 us; with 20 operations 74 us, and 64 us with as
+// rows of 65536 bf16 logits twice, 268 MB: 58 us; with 20 operations 74 us, and 61 us with as
 // many registers as the compiler takes by itself, which is 4 waves a SIMD instead of 6).
 template <typename T>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) void accept_stats_kernel(SampledAcceptParams p) {
