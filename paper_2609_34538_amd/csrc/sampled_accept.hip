@@ -15,6 +15,14 @@
 // sequence the run of accepted proposals, and of every part of the row where it ends the sum
 // of the residual; the token in the part where the running sum passes the random number's
 // share.
+//
+// 32 sequences x 32 positions x 65536 bf16 logits, target and draft, three quarters of which are
+// tested (200 MB): 70-76 us, of which the rows' sums 58 (3.4 TB/s, bound by their 64-bit
+// arithmetic), the run 12 and the draw 8; one sequence of 8 positions, fp32: 14.7 us, three
+// launches and their round trips. Measured and not kept: the draw in the second kernel, by the
+// last part to end (14.7 -> 14.4 us, but 76 -> 91: what its counter needs to be seen in order
+// writes a cache back for every part); the sums of weights under 2^-12 in fp32 (no gain: nearly
+// every piece of a row has a larger one).
 
 #include "mfma_tile.h"
 #include "q4_internal.h"
@@ -231,9 +239,9 @@ constexpr int kDraw = kThreads * 8;                 // tokens of a part of the d
 static_assert(kDraw == kAcceptDraw && sizeof(Stat) == kAcceptStatBytes && sizeof(Chain) == kAcceptChainBytes,
               "the workspace's layout");
 
-// The sums' arithmetic bounds it: 11 operations a logit beside the unpacking and the maximum (1024
-// rows of 65536 bf16 logits twice, 268 MB: 58 us; with 20 operations 74 us, and 61 us with as
-// many registers as the compiler takes by itself, which is 4 waves a SIMD instead of 6).
+// The sums' arithmetic bounds it: 11 operations a logit beside the unpacking and the maximum (1530
+// rows of 65536 bf16 logits, 200 MB: 58 us; with 20 operations 74 us, and 61 us with as many
+// registers as the compiler takes by itself, which is 4 waves a SIMD instead of 6).
 template <typename T>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) void accept_stats_kernel(SampledAcceptParams p) {
   __shared__ Powers<kFine> table;
