@@ -117,6 +117,52 @@ def test_ragged_batches_match_the_oracle(case):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dh", [64, 96, 128])
+@pytest.mark.parametrize("group,w", [(1, 16), (1, 17), (2, 16), (3, 11), (1, 64), (5, 13), (8, 16), (8, 17)])
+def test_rows_around_the_launch_shapes(dtype, dh, group, w):
+    """16, 17, 32, 33, 64, 65, 128 and 136 query rows a KV head; chunks of one and several."""
+    lens = [1500, 63, 0]
+    cache, batch, table = random_cache(7, dtype, 3, 2, dh, lens, spread=1)
+    q, kb, vb = _block(11, dtype, 3, w, 2 * group, 2, dh)
+    out, lse = _run(cache, batch, q, kb, vb)
+    _check(cache, batch, table, lens, q, kb, vb, out, lse)
+
+
+@pytest.mark.parametrize("w", [4, 20, 32, 50])
+def test_wide_heads_far_logits_and_late_values(w):
+    """Head dim 128: infinities in block values reach who sees them, and rows whose logits are
+    far give the value of the largest."""
+    lens = [400]
+    cache, batch, table = random_cache(9, BF16, 1, 2, 128, lens)
+    q, kb, vb = _block(3, BF16, 1, w, 2, 2, 128)
+    clean = das.attn_policy_q4(cache, batch, 0, 1, 1, q, kb, vb)
+    vb[0, 3, 1, 100] = float("inf")
+    out = das.attn_policy_q4(cache, batch, 0, 1, 1, q, kb, vb)
+    assert torch.isinf(out[0, 3:, 1, 100]).all()
+    out[0, 3:, 1, 100] = clean[0, 3:, 1, 100]
+    assert torch.equal(out, clean)
+    vb[0, 3, 1, 100] = 0
+    cache.k_exp.copy_(torch.where(cache.k_exp == 255, 255, 127 + 30))
+    kb.zero_()  # the largest logit is a cached token's, at 2^30 and more
+    out = das.attn_policy_q4(cache, batch, 0, 1, 1, q, kb, vb)
+    host = HostCache(cache)
+    k, v = (host.rows(n, 0, 0, table[0], lens[0]) for n in ("k", "v"))
+    for h in range(2):
+        x = q[0, :, h].double().cpu().numpy() @ k[:, h].T / np.sqrt(128)
+        top = np.sort(x, -1)[:, -2:]
+        # fp32 sums of 128 exact products: 2^-17 of their sizes' sum at most
+        err = 2.0 ** -16 * (np.abs(q[0, :, h].double().cpu().numpy()) @ np.abs(k[:, h]).T).max(-1) / np.sqrt(128)
+        sure = top[:, 1] - top[:, 0] > 2 * err + 60
+        assert sure.sum() > w // 2
+        best = v[x.argmax(-1), h]
+        got = out[0, :, h].double().cpu().numpy()
+        # one probability of 1, what is under 2^-39 of the row's largest may be lost in a record,
+        # whose elements have 11 bits, and a rounding to bf16
+        tol = (2.0 ** -8 + 2.0 ** -11) * np.abs(best) + 2.0 ** -38 * np.abs(best).max(-1, keepdims=True)
+        assert (np.abs(got - best) <= tol)[sure].all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_plane_layer_and_policy(dtype):
     """Keys of depth 2 and values of depth 3 at layer 1 are the ones that are read."""
     lens = [130, 40]
