@@ -15,7 +15,11 @@
 // (65 MB) 15.1-16.1 us, 4.0-4.3 TB/s, where a copy of large arrays reaches 4.9; 8 tokens 4.2 us,
 // the launch and two round trips. A token's heads are shared by workgroups until there are eight a
 // compute unit: 64 tokens 4.4 us, with one workgroup each 8.4, 256 tokens 8.2 and 10.6; 1024
-// tokens with three each 16.2, six 18.7.
+// tokens with three each 16.2, six 18.7. Where half of a workgroup or more would be idle, it takes
+// several tokens, from four a compute unit on: 17955 tokens of 15 heads, dh 64, 18.9 us, with one
+// each 27.8, of 6 heads 11.3 and 27.5; 2048 tokens 4.7 and 5.8; 768 tokens 4.1 and 4.0.
+
+#include <algorithm>
 
 #include "mfma_tile.h"
 #include "q4_internal.h"
@@ -24,7 +28,6 @@ namespace das {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxPairs = 64;
 
 // cos and sin of t in 64 bits, |t| up to 2^31 (the largest position times a frequency of 1).
 __device__ __forceinline__ void turn(double t, float &c, float &s) {
@@ -114,13 +117,17 @@ __device__ __forceinline__ void store8(T *dst, const float *f) {
   __builtin_memcpy(__builtin_assume_aligned(dst, 16), &x, sizeof(x));
 }
 
-template <typename T, int DH>
-__global__ __launch_bounds__(kThreads) void qk_rope_kernel(RopeParams p) {
+// PACKED: per_wg tokens a workgroup, one head a slot; else one, a share of its heads.
+template <typename T, int DH, bool PACKED>
+__global__ __launch_bounds__(kThreads) void qk_rope_kernel(RopeParams p, int per_wg) {
   constexpr int LPR = DH == 64 ? 4 : 8, ROWS = kThreads / LPR;  // lanes of a head, heads at once
-  __shared__ float cs[kMaxPairs], sn[kMaxPairs];
-  const int64_t token = blockIdx.x;
+  __shared__ float cs[kThreads], sn[kThreads];
+  const int heads = p.hq + p.hkv + (p.v ? p.hkv : 0), pairs = p.rotary / 2;
+  const int slot = threadIdx.x / LPR;
+  const int local = PACKED ? slot / heads : 0;  // the token of the workgroup's
+  const int64_t tokens = static_cast<int64_t>(p.batch) * p.w, first_token = static_cast<int64_t>(blockIdx.x) * per_wg;
+  const int64_t token = min(first_token + local, tokens - 1);
   const int b = token / p.w, i = token % p.w;
-  const int heads = p.hq + p.hkv + (p.v ? p.hkv : 0);
   const int lane = threadIdx.x % LPR;
   const bool in_head = lane < DH / 16;
   // the lane's 8-dim pieces; half-split pairs lie rotary / 2 apart, interleaved ones side by side
@@ -149,26 +156,31 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(RopeParams p) {
     }
   };
   const int per = (heads + gridDim.y - 1) / gridDim.y;
-  const int h_end = min(heads, static_cast<int>(blockIdx.y + 1) * per);
-  int h = blockIdx.y * per + threadIdx.x / LPR;
+  int h = PACKED ? slot - local * heads : blockIdx.y * per + slot;
+  const int h_end = PACKED ? (local < per_wg && first_token + local < tokens ? heads : 0)
+                           : min(heads, static_cast<int>(blockIdx.y + 1) * per);
   Row row;
   if (h < h_end) load(h, row);
-  if (threadIdx.x < p.rotary / 2) {
-    const double pos = p.each ? static_cast<double>(p.positions[token])
-                              : static_cast<double>(p.positions[b]) + static_cast<double>(i);
-    turn(pos * static_cast<double>(p.inv_freq[threadIdx.x]), cs[threadIdx.x], sn[threadIdx.x]);
+  if (static_cast<int>(threadIdx.x) < per_wg * pairs) {
+    const int pair = PACKED ? threadIdx.x % pairs : threadIdx.x;
+    const int64_t at = PACKED ? min(first_token + threadIdx.x / pairs, tokens - 1) : token;
+    const int of = PACKED ? static_cast<int>(at / p.w) : b, place = PACKED ? static_cast<int>(at % p.w) : i;
+    const double pos = p.each ? static_cast<double>(p.positions[at])
+                              : static_cast<double>(p.positions[of]) + static_cast<double>(place);
+    turn(pos * static_cast<double>(p.inv_freq[pair]), cs[threadIdx.x], sn[threadIdx.x]);
   }
   __syncthreads();
+  const int local_pairs = PACKED ? min(local, per_wg - 1) * pairs : 0;
   float c[8], s[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    c[j] = turns ? cs[8 * lane + j] : 1.f;
-    s[j] = turns ? sn[8 * lane + j] : 0.f;
+    c[j] = turns ? cs[local_pairs + 8 * lane + j] : 1.f;
+    s[j] = turns ? sn[local_pairs + 8 * lane + j] : 0.f;
   }
   // the same number of rounds for all lanes of a head; its lanes have the same h
-  for (; h < h_end; h += ROWS) {
+  for (; h < h_end; h += PACKED ? heads : ROWS) {
     Row next;
-    if (h + ROWS < h_end) load(h + ROWS, next);
+    if (!PACKED && h + ROWS < h_end) load(h + ROWS, next);
     const bool is_q = h < p.hq, is_v = h >= p.hq + p.hkv;
     const int at = is_q ? h : is_v ? h - p.hq - p.hkv : h - p.hq;
     const int n = is_q ? p.hq : p.hkv;
@@ -237,11 +249,15 @@ hipError_t launch_dh(const RopeParams &p, hipStream_t s) {
   constexpr int ROWS = kThreads / (DH == 64 ? 4 : 8);
   const int heads = p.hq + p.hkv + (p.v ? p.hkv : 0);
   const int64_t tokens = static_cast<int64_t>(p.batch) * p.w;
+  const int pack = std::min(ROWS / heads, p.rotary ? kThreads / (p.rotary / 2) : ROWS);
+  if (pack >= 2 && tokens >= 4 * kNumCUs)
+    return launch_kernel(qk_rope_kernel<T, DH, true>, dim3(static_cast<unsigned>((tokens + pack - 1) / pack)),
+                         dim3(kThreads), s, p, pack);
   const int rounds = (heads + ROWS - 1) / ROWS;
   // eight workgroups a compute unit, where there are heads for them
   const int64_t want = (8 * kNumCUs + tokens - 1) / tokens;
   const int split = static_cast<int>(want < rounds ? want : rounds);
-  return launch_kernel(qk_rope_kernel<T, DH>, dim3(static_cast<unsigned>(tokens), split), dim3(kThreads), s, p);
+  return launch_kernel(qk_rope_kernel<T, DH, false>, dim3(static_cast<unsigned>(tokens), split), dim3(kThreads), s, p, 1);
 }
 
 template <typename T>

@@ -67,6 +67,15 @@ CASES = [  # dtype, B, w, hq, hkv, dh, rotary, interleaved, norm, fused
     (F32, 3, 2, 40, 10, 128, 128, True, False, True),
     (F32, 2, 1, 3, 3, 96, 80, False, True, True),
     (F32, 1, 3000, 2, 1, 64, 64, False, True, True),
+    # several tokens a workgroup, the last one not full
+    (BF16, 1, 1031, 1, 1, 64, 64, False, True, False),
+    (BF16, 41, 53, 5, 5, 64, 64, True, True, True),
+    (BF16, 700, 3, 6, 2, 96, 96, False, True, True),
+    (BF16, 19, 61, 8, 4, 128, 48, False, False, True),
+    (BF16, 1100, 1, 3, 1, 96, 0, False, True, True),
+    (BF16, 3, 399, 8, 4, 128, 128, True, True, True),
+    (F32, 2, 1025, 4, 1, 64, 16, False, True, True),
+    (F32, 5, 251, 10, 3, 128, 128, True, True, True),
 ]
 
 
