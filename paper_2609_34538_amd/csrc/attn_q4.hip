@@ -25,11 +25,11 @@
 // work, where fp32 instructions would take sixteen times.
 //
 // Measured (bf16): 32 sequences x 55 heads, dh 96, 4096-8192 tokens: 4 rows 178 us, 6.2 TB/s of
-// page bytes, 16 rows 189 us, 5.9, both near what this card's memory gives; 32 rows 226 us, 5.1:
+// page bytes, 16 rows 189 us, 5.9, both near what this card's memory gives; 32 rows 224 us, 5.1:
 // vector instructions, some 400 a page (204 of them the conversion, 180 the softmax). 192 units of
-// 4 rows, 1-8191 tokens, dh 128: 28.8 us, the longest units and the second launch. 32 units of 128
-// rows, 32768 tokens, dh 128: 91 us, 750 TFLOP/s, vector and matrix instructions in turn. One
-// sequence of 2048 tokens, 55 heads, 8 rows: 9.7 us, two launches and their round trips.
+// 4 rows, 1-8191 tokens, dh 128: 26.6 us, the longest units and the second launch. 32 units of 128
+// rows, 32768 tokens, dh 128: 90 us, 760 TFLOP/s, vector and matrix instructions in turn. One
+// sequence of 2048 tokens, 55 heads, 8 rows: 9.4 us, two launches and their round trips.
 // Measured and not kept: pages through a ring of three in LDS in place of registers (226 -> 235
 // us, 28.8 -> 32); the sum of the rounded probabilities by the matrix unit (226 -> 222 us, and
 // a less exact log-sum-exp); no maximum unless a sum overflows (spills, 453 us); a page in two
@@ -141,10 +141,11 @@ __device__ __forceinline__ void prob_operands(const f32x4 &a, const f32x4 &b, u3
 }
 
 // E / 2 tiles of 32 tokens of a page, from tile T0 on, through both products.
-// `limit`: visible tokens of the page.
-template <typename T, int DH, int NQ, int T0, int E, bool FAR>
+// `limit`: visible tokens of the page; keys_taken is called when t's keys are.
+template <typename T, int DH, int NQ, int T0, int E, bool FAR, typename Then>
 __device__ __forceinline__ void prefix_tiles(Acc<DH, NQ> &st, uint64_t &far, Page<DH> &t,
-                                             const QParts<T, DH> (&qf)[NQ], int limit, float scale, int lg) {
+                                             const QParts<T, DH> (&qf)[NQ], int limit, float scale, int lg,
+                                             Then keys_taken) {
   constexpr int KS = DH / 32;
   f32x4 s[NQ][E];
 #pragma unroll
@@ -162,6 +163,7 @@ __device__ __forceinline__ void prefix_tiles(Acc<DH, NQ> &st, uint64_t &far, Pag
 #pragma unroll
         for (int qt = 0; qt < NQ; ++qt) s[qt][e] = mfma16x16x32(a, qf[qt].x[k][i], s[qt][e]);
     }
+  keys_taken();
   const int none[NQ] = {};
   int limits[E / 2];
 #pragma unroll
@@ -451,17 +453,12 @@ void attn_q4_kernel(AttnQ8Params p, int n_rg) {
     return ok ? min(kTokens, S - kTokens * (g0 + STRIDE * i - 1)) : 0;
   };
 
-  // The wave's i-th tile into registers. Past the last tile the loads go to empty buffers:
-  // they are always issued, so that the compiler can count them, and waits for one page leave
-  // the next under way.
-  auto load = [&](int i, Page<DH> &t) {
-    size_t at;
-    const int visible = locate(i, at);
-    const int bytes = i < n ? q4_page_bytes(DH) : 0, exps = i < n ? q4_page_exps(DH) : 0;
-    const auto rk = buffer_of(p.k_layer + at * q4_page_bytes(DH), bytes);
-    const auto rv = buffer_of(p.v_layer + at * q4_page_bytes(DH), bytes);
-    const auto rke = buffer_of(p.k_exp + at * q4_page_exps(DH), exps);
-    const auto rve = buffer_of(p.v_exp + at * q4_page_exps(DH), exps);
+  // The keys and the values of the wave's i-th tile into registers. Past the last tile the loads
+  // go to empty buffers: they are always issued, so that the compiler can count them, and waits
+  // for some leave the others under way.
+  auto load_keys = [&](int i, size_t at, Page<DH> &t) {
+    const auto rk = buffer_of(p.k_layer + at * q4_page_bytes(DH), i < n ? q4_page_bytes(DH) : 0);
+    const auto rke = buffer_of(p.k_exp + at * q4_page_exps(DH), i < n ? q4_page_exps(DH) : 0);
     if constexpr (KS == 2) {
       const u32x2 e = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rke, ln * 4 * KS, 0, kCached));
       t.ke[0] = e[0], t.ke[1] = e[1];
@@ -476,12 +473,22 @@ void attn_q4_kernel(AttnQ8Params p, int n_rg) {
 #pragma unroll
     for (int k = 0; k < KS; ++k)
       t.k[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, 16 * lane, 1024 * k, kNonTemporal));
+  };
+  auto load_values = [&](int i, size_t at, Page<DH> &t) {
+    const auto rv = buffer_of(p.v_layer + at * q4_page_bytes(DH), i < n ? q4_page_bytes(DH) : 0);
+    const auto rve = buffer_of(p.v_exp + at * q4_page_exps(DH), i < n ? q4_page_exps(DH) : 0);
 #pragma unroll
     for (int k = 0; k < KS; ++k)
       t.ve[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rve, lg * 16 * KS, 16 * k, kCached));
 #pragma unroll
     for (int k = 0; k < KS; ++k)
       t.v[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, 16 * lane, 1024 * k, kNonTemporal));
+  };
+  auto load = [&](int i, Page<DH> &t) {
+    size_t at;
+    const int visible = locate(i, at);
+    load_keys(i, at, t);
+    load_values(i, at, t);
     return visible;
   };
 
@@ -493,27 +500,50 @@ void attn_q4_kernel(AttnQ8Params p, int n_rg) {
     }
   };
   if constexpr (RW == 1) {
-    // two pages in flight, the first before the block's tile is worked on
-    Page<DH> ta, tb;
-    int i = n_block;
     if (!AHEAD && has_block) work_block(std::false_type{});
-    int la = load(i, ta);
-    if (AHEAD && has_block) work_block(std::false_type{});
-    int lb = load(i + 1, tb);
-    auto work = [&](Page<DH> &t, int limit) {
-      // whole pages where their logits fit the registers
-      if constexpr (sizeof(T) == 2 && (DH < 128 || NQ == 1)) {
-        prefix_tiles<T, DH, NQ, 0, 4, false>(st, far, t, qf, limit, p.scale_log2, lg);
-      } else {
-        prefix_tiles<T, DH, NQ, 0, 2, false>(st, far, t, qf, limit, p.scale_log2, lg);
-        prefix_tiles<T, DH, NQ, 1, 2, false>(st, far, t, qf, limit, p.scale_log2, lg);
+    constexpr bool WHOLE = sizeof(T) == 2 && (DH < 128 || NQ == 1);  // a page's logits fit the registers
+    if constexpr (WHOLE && (DH > 64 || NQ == 2)) {
+      // The next page's keys are asked for when the page's have been taken, its values likewise.
+      // Two pages in turn, as below, are slower (192 units of 4 rows, dh 128: 28.7 against 26.6
+      // us; 32 rows, dh 96: 224.7 against 223.4; at dh 64 97 against 95 with 32 rows, but 79
+      // against 83 with 16), three waves a SIMD in the registers that are free without the block
+      // ahead slower too (28.7; 243).
+      Page<DH> t;
+      int limit = load(n_block, t);
+      if (AHEAD && has_block) work_block(std::false_type{});
+#pragma unroll 1
+      for (int i = n_block; i < n; ++i) {
+        size_t at;
+        int next = 0;
+        prefix_tiles<T, DH, NQ, 0, 4, false>(st, far, t, qf, limit, p.scale_log2, lg, [&] {
+          next = locate(i + 1, at);
+          load_keys(i + 1, at, t);
+        });
+        load_values(i + 1, at, t);
+        limit = next;
       }
-    };
-    for (; i < n; i += 2) {
-      work(ta, la);
-      la = load(i + 2, ta);
-      if (i + 1 < n) work(tb, lb);
-      lb = load(i + 3, tb);
+    } else {
+      // Two pages in flight (with one page's registers as above fp32 calls take 78 us for 75, 32
+      // rows of dh 128 179 for 170).
+      Page<DH> ta, tb;
+      int i = n_block;
+      int la = load(i, ta);
+      if (AHEAD && has_block) work_block(std::false_type{});
+      int lb = load(i + 1, tb);
+      auto work = [&](Page<DH> &t, int limit) {
+        if constexpr (WHOLE) {
+          prefix_tiles<T, DH, NQ, 0, 4, false>(st, far, t, qf, limit, p.scale_log2, lg, [] {});
+        } else {
+          prefix_tiles<T, DH, NQ, 0, 2, false>(st, far, t, qf, limit, p.scale_log2, lg, [] {});
+          prefix_tiles<T, DH, NQ, 1, 2, false>(st, far, t, qf, limit, p.scale_log2, lg, [] {});
+        }
+      };
+      for (; i < n; i += 2) {
+        work(ta, la);
+        la = load(i + 2, ta);
+        if (i + 1 < n) work(tb, lb);
+        lb = load(i + 3, tb);
+      }
     }
   } else {
     // Each wave brings its pieces of a page into registers, a step ahead, and writes them
@@ -601,8 +631,8 @@ void attn_q4_kernel(AttnQ8Params p, int n_rg) {
     for (int i = n_block; i < n; ++i) {
       Page<DH> t;
       const int visible = load(i, t);
-      prefix_tiles<T, DH, NQ, 0, 2, true>(st, far, t, qf, visible, p.scale_log2, lg);
-      prefix_tiles<T, DH, NQ, 1, 2, true>(st, far, t, qf, visible, p.scale_log2, lg);
+      prefix_tiles<T, DH, NQ, 0, 2, true>(st, far, t, qf, visible, p.scale_log2, lg, [] {});
+      prefix_tiles<T, DH, NQ, 1, 2, true>(st, far, t, qf, visible, p.scale_log2, lg, [] {});
     }
   }
   float m[NQ];
