@@ -66,11 +66,11 @@ struct PlanQ4 {
 // sequence; in chunks of at least 32 tiles where that leaves 384 of them, 16 where 256, 8
 // where 128 (us, 4 query heads a KV head, one token each, dh 128, up to 8191 tokens; in
 // parentheses with chunks of 8, 16, 32 and all tiles):
-//   32 units 11.4 (12.2 11.5 15.2 33), 64 units 16.1 (19 16.5 15.7 34), 128 units 23.6 (29 25 24
-//   36), 192 units 29.0 (39 32 29 36), 384 units 51 (69 58 54 59), 512 units 64 (86 73 67 70);
-//   55 units of one sequence, 8192 tokens, 32 rows, dh 96: 20.8 (28 23 22 44).
-// A unit is not cut at all below 16 tiles, and up to 65 where there are 192 of them (256 units,
-// up to 4096 tokens: 21.7; 23.7 with 24 tiles a chunk, 24.3 with 32).
+//   32 units 11.1 (11.5 11.0 14.5 32), 64 units 15.0 (17 15.0 15.2 32), 128 units 22.3 (27 23 22
+//   34), 192 units 27.2 (35 30 27 35), 384 units 51 (63 54 51 56), 512 units 65 (80 69 65 67);
+//   55 units of one sequence, 8192 tokens, 32 rows, dh 96: 21.0-22.5 (27 22 21 43).
+// A unit is not cut at all below 16 tiles, and up to 65 where there are 192 of them (192 units of
+// 4096 tokens: 23.7; 26.2 with 16 tiles a chunk, 28.1 with 24, 25.7 with 32).
 //
 // RW == 4, where a page is a step for all waves: three a compute unit of a batch, two of a single
 // sequence, from four tiles on, from 32 on beyond 4096 tokens where that leaves 384 of them (us;
