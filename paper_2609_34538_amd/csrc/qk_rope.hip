@@ -16,8 +16,10 @@
 // the launch and two round trips. A token's heads are shared by workgroups until there are eight a
 // compute unit: 64 tokens 4.4 us, with one workgroup each 8.4, 256 tokens 8.2 and 10.6; 1024
 // tokens with three each 16.2, six 18.7. Where half of a workgroup or more would be idle, it takes
-// several tokens, from four a compute unit on: 17955 tokens of 15 heads, dh 64, 18.9 us, with one
-// each 27.8, of 6 heads 11.3 and 27.5; 2048 tokens 4.7 and 5.8; 768 tokens 4.1 and 4.0.
+// several tokens, from four a compute unit on: 17955 tokens of 15 heads, dh 64, 17.0 us, with one
+// each 27.8, of 6 heads 9.7 and 27.5; 2048 tokens 4.5 and 5.8; 768 tokens 4.1 and 4.0. Measured and
+// not kept: several tokens in several rounds, where a token's last round is half empty (1024
+// tokens of 24 heads, dh 128, 5.1 -> 6.3 us, 2048 of 40 heads 11.4 -> 12.9).
 
 #include <algorithm>
 
@@ -124,10 +126,8 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(RopeParams p, int per
   __shared__ float cs[kThreads], sn[kThreads];
   const int heads = p.hq + p.hkv + (p.v ? p.hkv : 0), pairs = p.rotary / 2;
   const int slot = threadIdx.x / LPR;
-  const int local = PACKED ? slot / heads : 0;  // the token of the workgroup's
-  const int64_t tokens = static_cast<int64_t>(p.batch) * p.w, first_token = static_cast<int64_t>(blockIdx.x) * per_wg;
-  const int64_t token = min(first_token + local, tokens - 1);
-  const int b = token / p.w, i = token % p.w;
+  const int tokens = p.batch * p.w, token0 = blockIdx.x * per_wg;
+  const float per_head = 1.f / static_cast<float>(heads);
   const int lane = threadIdx.x % LPR;
   const bool in_head = lane < DH / 16;
   // the lane's 8-dim pieces; half-split pairs lie rotary / 2 apart, interleaved ones side by side
@@ -140,51 +140,64 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(RopeParams p, int per
   struct Row {
     Eight<T> a, b, wa, wb;
   };
-  auto load = [&](int h, Row &r) {
-    if (h >= heads || !in_head) return;
+  const int per = (heads + gridDim.y - 1) / gridDim.y;
+  const int begin = PACKED ? slot : blockIdx.y * per + slot;
+  const int end = PACKED ? min(per_wg, tokens - token0) * heads : min(heads, static_cast<int>(blockIdx.y + 1) * per);
+  // the token of the workgroup's that row r is of
+  auto local_of = [&](int r) { return PACKED ? static_cast<int>((static_cast<float>(r) + 0.5f) * per_head) : 0; };
+  const int b0 = token0 / p.w, i0 = token0 - b0 * p.w;
+  auto load = [&](int r, Row &row) {
+    if (r >= end || !in_head) return;
+    const int local = local_of(r), h = r - local * heads;
+    int b = b0, i = i0 + local;
+    if (PACKED && i >= p.w) {
+      const int over = i / p.w;
+      b += over;
+      i -= over * p.w;
+    }
     const bool is_q = h < p.hq, is_v = h >= p.hq + p.hkv;
     const int at = is_q ? h : is_v ? h - p.hq - p.hkv : h - p.hq;
     const T *src = static_cast<const T *>(is_q ? p.q : is_v ? p.v : p.k) +
                    b * (is_q ? p.q_batch : is_v ? p.v_batch : p.k_batch) +
                    i * (is_q ? p.q_token : is_v ? p.v_token : p.k_token) + static_cast<int64_t>(at) * DH;
-    r.a = load8<T>(src + first);
-    r.b = load8<T>(src + second);
+    row.a = load8<T>(src + first);
+    row.b = load8<T>(src + second);
     const T *w = static_cast<const T *>(is_q ? p.q_weight : p.k_weight);
     if (w && !is_v) {
-      r.wa = load8<T>(w + first);
-      r.wb = load8<T>(w + second);
+      row.wa = load8<T>(w + first);
+      row.wb = load8<T>(w + second);
     }
   };
-  const int per = (heads + gridDim.y - 1) / gridDim.y;
-  int h = PACKED ? slot - local * heads : blockIdx.y * per + slot;
-  const int h_end = PACKED ? (local < per_wg && first_token + local < tokens ? heads : 0)
-                           : min(heads, static_cast<int>(blockIdx.y + 1) * per);
+  int r = begin;
   Row row;
-  if (h < h_end) load(h, row);
+  load(r, row);
   if (static_cast<int>(threadIdx.x) < per_wg * pairs) {
-    const int pair = PACKED ? threadIdx.x % pairs : threadIdx.x;
-    const int64_t at = PACKED ? min(first_token + threadIdx.x / pairs, tokens - 1) : token;
-    const int of = PACKED ? static_cast<int>(at / p.w) : b, place = PACKED ? static_cast<int>(at % p.w) : i;
-    const double pos = p.each ? static_cast<double>(p.positions[at])
-                              : static_cast<double>(p.positions[of]) + static_cast<double>(place);
+    const int local = PACKED ? threadIdx.x / pairs : 0, pair = threadIdx.x - local * pairs;
+    const int token = min(token0 + local, tokens - 1), b = token / p.w;
+    const double pos = p.each ? static_cast<double>(p.positions[token])
+                              : static_cast<double>(p.positions[b]) + static_cast<double>(token - b * p.w);
     turn(pos * static_cast<double>(p.inv_freq[pair]), cs[threadIdx.x], sn[threadIdx.x]);
   }
   __syncthreads();
-  const int local_pairs = PACKED ? min(local, per_wg - 1) * pairs : 0;
   float c[8], s[8];
+  auto angles = [&](int local) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    c[j] = turns ? cs[local_pairs + 8 * lane + j] : 1.f;
-    s[j] = turns ? sn[local_pairs + 8 * lane + j] : 0.f;
-  }
-  // the same number of rounds for all lanes of a head; its lanes have the same h
-  for (; h < h_end; h += PACKED ? heads : ROWS) {
+    for (int j = 0; j < 8; ++j) {
+      c[j] = turns ? cs[local * pairs + 8 * lane + j] : 1.f;
+      s[j] = turns ? sn[local * pairs + 8 * lane + j] : 0.f;
+    }
+  };
+  if (!PACKED) angles(0);
+  // the same number of rounds for all lanes of a head; its lanes have the same r
+  for (; r < end; r += ROWS) {
     Row next;
-    if (!PACKED && h + ROWS < h_end) load(h + ROWS, next);
+    if (!PACKED) load(r + ROWS, next);
+    const int local = local_of(r), h = r - local * heads;
+    if (PACKED) angles(local);
     const bool is_q = h < p.hq, is_v = h >= p.hq + p.hkv;
     const int at = is_q ? h : is_v ? h - p.hq - p.hkv : h - p.hq;
     const int n = is_q ? p.hq : p.hkv;
-    T *dst = static_cast<T *>(is_q ? p.q_out : is_v ? p.v_out : p.k_out) + (token * n + at) * DH;
+    T *dst = static_cast<T *>(is_q ? p.q_out : is_v ? p.v_out : p.k_out) + (static_cast<int64_t>(token0 + local) * n + at) * DH;
     if (is_v) {
       if (in_head) {
         __builtin_memcpy(__builtin_assume_aligned(dst + first, 16), &row.a, sizeof(row.a));
@@ -249,7 +262,7 @@ hipError_t launch_dh(const RopeParams &p, hipStream_t s) {
   constexpr int ROWS = kThreads / (DH == 64 ? 4 : 8);
   const int heads = p.hq + p.hkv + (p.v ? p.hkv : 0);
   const int64_t tokens = static_cast<int64_t>(p.batch) * p.w;
-  const int pack = std::min(ROWS / heads, p.rotary ? kThreads / (p.rotary / 2) : ROWS);
+  const int pack = std::min({ROWS / heads, 8, p.rotary ? kThreads / (p.rotary / 2) : 8});
   if (pack >= 2 && tokens >= 4 * kNumCUs)
     return launch_kernel(qk_rope_kernel<T, DH, true>, dim3(static_cast<unsigned>((tokens + pack - 1) / pack)),
                          dim3(kThreads), s, p, pack);
