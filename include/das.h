@@ -665,7 +665,8 @@ das_status das_qk_rope(const das_rope *rope, int32_t batch, int32_t block_len, c
  * - from p of position a_b where a_b = m_b < w,
  * and with a_b = w none is. The token drawn is the first in index order at which the running
  * sum passes draw[b] times the whole. Weights are 64-bit exponentials relative to the row's
- * largest.
+ * largest: a logit more than 745.1 temperatures below it weighs nothing, and its token is neither
+ * accepted nor drawn, with numbers of 0 either.
  *
  *   proposals    device [B][w] int32. One that is checked and lies outside the vocabulary is
  *                rejected, with the whole of p as the residual but for q

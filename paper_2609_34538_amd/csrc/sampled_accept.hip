@@ -96,7 +96,8 @@ struct Powers {
 // 2^(d c32 / 32) for d <= 0, d c32 >= -32000: of k + f = d c32, |f| <= 1/2, 2^(k / 32) from the
 // table (kCoarse entries lie in different banks), and 2^(f / 32) by the polynomial 1 + f r(f) of
 // degree 4 whose largest relative error is least, 2^-43.5. 1 exactly at d = 0.
-template <int N>
+// Times 2^UP, with which d c32 may go down to -32 (1022 + UP).
+template <int UP = 0, int N>
 __device__ __forceinline__ double exp2_near(double d, double c32, const Powers<N> &table) {
   constexpr double kRound = 0x1.8p52;  // leaves a sum with it rounded to an integer, in its lower half
   const double big = __builtin_fma(d, c32, kRound), f = __builtin_fma(d, c32, -(big - kRound));
@@ -104,9 +105,10 @@ __device__ __forceinline__ double exp2_near(double d, double c32, const Powers<N
   r = __builtin_fma(r, f, 1.6938633790138636e-06);
   r = __builtin_fma(r, f, 2.3459619821480828e-04);
   r = __builtin_fma(r, f, 2.166084939172456e-02);
-  return table.of(static_cast<uint32_t>(__builtin_bit_cast(uint64_t, big)) * (N / kCoarse)) * __builtin_fma(r, f, 1.0);
+  const uint32_t k = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, big)) * (N / kCoarse) + UP * N;
+  return table.of(k) * __builtin_fma(r, f, 1.0);
 }
-// The same for any d <= 0; what is under 2^-1000 becomes that.
+// The same for any d <= 0; what is under 2^-1000 becomes that, which no sum notices.
 template <int N>
 __device__ __forceinline__ double exp2_of(double d, double c32, const Powers<N> &table) {
   return exp2_near(d * c32 < -32000.0 ? -32000.0 / c32 : d, c32, table);
@@ -126,12 +128,16 @@ __device__ __forceinline__ void fixed_power(double n, const Powers<kFine> &table
   a = table.of(w[1]);
 }
 
-// The weight of logit z at index j of a row.
+// The weight of logit z at index j of a row, times kOne: with that, all that an exponential in 64
+// bits holds are normal numbers. Under 2^-1075, half of its smallest, a weight is 0, so that no
+// random number of 0 accepts or draws its token.
+constexpr int kUp = 128;
+constexpr double kOne = 0x1p128, kLeast = -32.0 * 1075.0;
 __device__ __forceinline__ double weight(float z, int j, const Stat &r, double c32, const Powers<kCoarse> &table) {
-  if (c32 == 0.0 || r.max == kNegInf) return j == r.at ? 1.0 : 0.0;
-  if (r.max == __builtin_huge_valf()) return z == r.max ? 1.0 : 0.0;
-  const double w = exp2_of(static_cast<double>(z) - static_cast<double>(r.max), c32, table);
-  return z > kNegInf ? w : 0.0;
+  if (c32 == 0.0 || r.max == kNegInf) return j == r.at ? kOne : 0.0;
+  if (r.max == __builtin_huge_valf()) return z == r.max ? kOne : 0.0;
+  const double d = static_cast<double>(z) - static_cast<double>(r.max), w = exp2_near<kUp>(d, c32, table);
+  return d * c32 >= kLeast ? w : 0.0;
 }
 // What a draw weighs token `at` by, from the target's and the draft's logits.
 __device__ __forceinline__ double residual(const SampledAcceptParams &p, float zp, float zq, int at, const Chain &ch,
@@ -139,7 +145,7 @@ __device__ __forceinline__ double residual(const SampledAcceptParams &p, float z
   if (at >= p.vocab) return 0.0;
   const double w = weight(zp, at, ch.p, cp, table);
   if (ch.drawn != kLeft) return w;
-  const double wq = p.draft ? weight(zq, at, ch.q, cq, table) : at == ch.y ? 1.0 : 0.0;
+  const double wq = p.draft ? weight(zq, at, ch.q, cq, table) : at == ch.y ? kOne : 0.0;
   const double a = w * ch.q.sum, d = a - wq * ch.p.sum;
   return d > kNone * a ? d : 0.0;
 }
@@ -451,7 +457,7 @@ __global__ __launch_bounds__(kThreads) void accept_chain_kernel(SampledAcceptPar
     const bool checked = lane < m;
     const bool bad_token = checked && (y < 0 || y >= p.vocab), bad_number = checked && !(u >= 0.f && u < 1.f);
     const Stat sq = p.draft ? drafts[lane] : Stat{kNegInf, 0, 1.0};
-    const double wq = p.draft ? draft_weight[lane] : 1.0, py = wy / s.sum;
+    const double wq = p.draft ? draft_weight[lane] : kOne, py = wy / s.sum;  // times kOne
     const bool ok = checked && !bad_token && !bad_number && static_cast<double>(u) * (wq / sq.sum) < py;
     const uint64_t miss = ~__ballot(ok);
     const int a = min(miss ? static_cast<int>(__builtin_ctzll(miss)) : 64, m);
@@ -478,7 +484,7 @@ __global__ __launch_bounds__(kThreads) void accept_chain_kernel(SampledAcceptPar
       }
       if (lane < a) {
         if (p.emitted) p.emitted[at_row] = y;
-        if (p.probs) p.probs[at_row] = static_cast<float>(py);
+        if (p.probs) p.probs[at_row] = static_cast<float>(py / kOne);
       }
     }
   }
@@ -596,7 +602,7 @@ __global__ __launch_bounds__(kThreads) void accept_draw_kernel(SampledAcceptPara
     if (p.emitted) p.emitted[row] = token;
     if (p.probs) {
       const float z = no_nan(to_f32<T>(static_cast<const T *>(p.target)[row * p.target_stride + token]));
-      p.probs[row] = static_cast<float>(weight(z, token, ch.p, cp, table) / ch.p.sum);
+      p.probs[row] = static_cast<float>(weight(z, token, ch.p, cp, table) / ch.p.sum / kOne);
     }
   }
 }
