@@ -5,11 +5,15 @@
 // max(p - q, 0), one after the last tested proposal a token of p, by a second random number:
 // every emitted token then is a draw from p, whatever q is.
 //
-// Weights are w = exp((z - max) / T) in 64 bits, right to 2^-43.5, and their sums Z to 2^-41.5 (a
-// row's, where each weight may be off by that) or better, so that a token is another one only
-// where the random number lies within 2^-40 of a border. Residuals are w_p Z_q - w_q Z_p: exactly
-// 0 where both are equal with equal sums; below 2^-40 of p they count as 0, so that rounding
-// leaves no token that p does not exceed q at (2 x 2^-41.5 + 2 x 2^-43.5 < 2^-40).
+// Weights are w = exp((z - max) / T) in 64 bits, right to 2^-50 and what the rounding of their
+// exponent costs, 2^-52.4 an octave below the largest. Sums Z of a row are right to 2^-41.2: each
+// weight by the rounding of its exponent to 2^-41.5, by its polynomial to 2^-45, as the one of the
+// largest that they are divided by, and by the sums' and the temperature's roundings to 2^-45.2.
+// So a token is another one only where the random number lies within 2^-40 of a border, in a draw
+// from a residual 2^-40 of p's whole. Residuals are w_p Z_q - w_q Z_p: exactly 0 where both are
+// equal with equal sums; below 2^-40 of p they count as 0, so that rounding leaves no token that p
+// does not exceed q at (2 x 2^-41.2 + 2 x 2^-45.9 < 2^-40 for weights down to 2^-64; what is
+// under that matters where nothing else is left).
 //
 // Three kernels: the largest logit and the sum of weights of every part of every row; per
 // sequence the run of accepted proposals, and of every part of the row where it ends the sum
@@ -94,17 +98,19 @@ struct Powers {
 };
 
 // 2^(d c32 / 32) for d <= 0, d c32 >= -32000: of k + f = d c32, |f| <= 1/2, 2^(k / 32) from the
-// table (kCoarse entries lie in different banks), and 2^(f / 32) by the polynomial 1 + f r(f) of
-// degree 4 whose largest relative error is least, 2^-43.5. 1 exactly at d = 0.
+// table (kCoarse entries lie in different banks), and 2^(f / 32) by 1 + f r(f), r the polynomial
+// that agrees with (2^(f / 32) - 1) / f at the five Chebyshev points: 2^-52.6 of it. 1 exactly at
+// d = 0.
 // Times 2^UP, with which d c32 may go down to -32 (1022 + UP).
 template <int UP = 0, int N>
 __device__ __forceinline__ double exp2_near(double d, double c32, const Powers<N> &table) {
   constexpr double kRound = 0x1.8p52;  // leaves a sum with it rounded to an integer, in its lower half
   const double big = __builtin_fma(d, c32, kRound), f = __builtin_fma(d, c32, -(big - kRound));
-  double r = 9.172534833359138e-09;
-  r = __builtin_fma(r, f, 1.6938633790138636e-06);
-  r = __builtin_fma(r, f, 2.3459619821480828e-04);
-  r = __builtin_fma(r, f, 2.166084939172456e-02);
+  double r = 3.9737238568525983e-11;
+  r = __builtin_fma(r, f, 9.172607532092245e-09);
+  r = __builtin_fma(r, f, 1.6938509724285119e-06);
+  r = __builtin_fma(r, f, 2.345961981994449e-04);
+  r = __builtin_fma(r, f, 2.166084939249829e-02);
   const uint32_t k = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, big)) * (N / kCoarse) + UP * N;
   return table.of(k) * __builtin_fma(r, f, 1.0);
 }
@@ -302,7 +308,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) v
     // NaN and -inf need no more tests. The weights are taken relative to the power of two under
     // the largest, which saves the difference of each logit and the largest, and their sum is
     // brought to be relative to the largest afterwards.
-    const double step = 8.0 * c32, base = kFixed - 256.0 * floor(static_cast<double>(mx) * step / 256.0), least = low;
+    const double step = 8.0 * c32, top = static_cast<double>(mx) * step, whole = 256.0 * floor(top / 256.0);
+    const double base = kFixed - whole, least = low;
     double a, e;
 #pragma unroll
     for (int v = 0; v < kVec; ++v)
@@ -311,8 +318,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) v
         fixed_power(__builtin_fma(fmax(static_cast<double>(raw_logit<T>(x[v], j)), least), step, base), table, a, e);
         sum = __builtin_fma(a, e, sum);
       }
-    fixed_power(__builtin_fma(static_cast<double>(mx), step, base), table, a, e);
+    // with what the rounding of its exponent leaves: every weight of the row is relative to it
+    const double n = __builtin_fma(static_cast<double>(mx), step, base);
+    const double rest = (top - whole - (n - kFixed)) + __builtin_fma(static_cast<double>(mx), step, -top);
+    fixed_power(n, table, a, e);
     largest = a * e;  // both have the sign of a
+    largest = __builtin_fma(largest, rest * (0.69314718055994531 / 256.0), largest);
   } else {  // so hot that every finite logit counts, or so cold that fp32 has no such `low`
     const double top = mx;
 #pragma unroll 1
