@@ -566,7 +566,8 @@ das_status das_attn_q4(const das_cache_q4 *cache, const das_batch *batch, int32_
 /*
  * das_kv_append into a 4-bit cache. Arguments as for das_kv_append, with k_new and v_new in
  * base.dtype; len_out must share no element with batch->prefix_len or num_new
- * (DAS_ERR_SHAPE).
+ * (DAS_ERR_SHAPE). The grid is one workgroup of 256 per (plane, layer) and 12 blocks of a
+ * token's heads: these must be fewer than 2^24 (DAS_ERR_SHAPE), in das_kv_read_q4 too.
  *
  * A block gets the smallest exponent e in -120..125 with |x| <= 7 * 2^e for its 32 elements,
  * so that none is further from its code than half the distance of the largest two (4 and 6).

@@ -118,13 +118,10 @@ das_status tokens_params(const das_cache_q4 *cache, const das_batch *batch, cons
   const das_cache *c = &cache->base;
   if (!k_rows || !v_rows) return DAS_ERR_NULL;
   if (!aligned(k_rows, 16) || !aligned(v_rows, 16)) return DAS_ERR_ALIGN;
-  // the grid: one wave per (plane, layer, KV head), four per workgroup, keys and values in
-  // separate workgroups; at most 2^32 - 1 work-items along x
-  const long long per_plane = static_cast<long long>(c->num_layers) * c->num_kv_heads;
-  constexpr long long kMost = 1 << 26;  // units that such a grid holds; the products fit 64 bits
-  if (per_plane > kMost || c->num_k_planes > kMost || c->num_v_planes > kMost) return DAS_ERR_SHAPE;
-  const long long blocks = (c->num_k_planes * per_plane + 3) / 4 + (c->num_v_planes * per_plane + 3) / 4;
-  if (blocks * 256 > 0xffffffffLL) return DAS_ERR_SHAPE;
+  // the grid: workgroups of 256 per (plane, layer) and share of its heads, at most 2^32 - 1
+  // work-items along x
+  const int64_t units = (static_cast<int64_t>(c->num_k_planes) + c->num_v_planes) * c->num_layers;
+  if (units > 0xffffffffLL / 256 / q4_head_shares(c->num_kv_heads, c->head_dim)) return DAS_ERR_SHAPE;
   p->k_new = const_cast<void *>(k_rows);
   p->v_new = const_cast<void *>(v_rows);
   p->k_pool = static_cast<uint8_t *>(c->k_pool);

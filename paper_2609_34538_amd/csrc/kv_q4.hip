@@ -34,7 +34,7 @@ namespace das {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kSteps = 3;  // of a wave, whose loads are issued together
+constexpr int kSteps = kQ4Steps;  // of a wave, whose loads are issued together
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -233,7 +233,7 @@ hipError_t launch_typed(const TokensQ4Params &p, hipStream_t s) {
   const int64_t units = static_cast<int64_t>(p.n_k_planes + p.n_v_planes) * p.layers;
   // quads that w_max positions can touch, four to a workgroup
   const int groups = ((p.w_max + 2) / 4 + 1 + 3) / 4;
-  const int shares = (p.hkv * (DH / 32) + 4 * kSteps - 1) / (4 * kSteps);
+  const int shares = q4_head_shares(p.hkv, DH);
   return launch_kernel(kv_q4_kernel<T, DH, READ>,
                        dim3(static_cast<unsigned>(units * shares), p.batch, groups < 65535 ? groups : 65535),
                        dim3(64 * kWaves), s, p, shares);

@@ -42,6 +42,13 @@ __host__ __device__ constexpr int q4_group_rows(int rows, int es) {
   return 16 * q4_row_tiles(rows, es) * q4_row_waves(rows);
 }
 
+// Workgroups of the commit and of the way back that share a (plane, layer)'s heads: a wave takes
+// kQ4Steps times four neighbouring blocks of each of its tokens. Units (plane, layer) times
+// shares are a grid's width.
+constexpr int kQ4Steps = 3;
+__host__ __device__ constexpr int q4_head_shares(int hkv, int dh) {
+  return (hkv * (dh / kQ4Block) + 4 * kQ4Steps - 1) / (4 * kQ4Steps);
+}
 // The commit into the 4-bit cache, and the way back (k_new, v_new written).
 struct TokensQ4Params {
   void *k_new;             // [nK][L][B][w_max][Hkv][dh]
