@@ -64,8 +64,13 @@ __device__ __forceinline__ uint32_t upper(float a, float b) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
 }
 __device__ __forceinline__ float truncated(float a) { return __uint_as_float(__float_as_uint(a) & 0xffff0000u); }
-// Eight fp32 as three bf16 each, by truncation: 8 bits a part, exact. FINITE: all are.
-template <bool FINITE>
+// Eight fp32 as three bf16 each, by truncation: 8 bits a part, exact.
+// KEYS: an infinity is in the first part alone; of a NaN the second is one, whatever its upper
+// bits are. QUERIES: parts that would be 0 are 2^-40 of the element instead, which no fp32 sum
+// notices, so that the products of an infinite key with them are infinities and not NaN (but with
+// a query of 0, or under 2^-93).
+enum Split { FINITE, KEYS, QUERIES };
+template <Split KIND>
 __device__ __forceinline__ void split3(const float (&a)[8], u32x4 (&part)[3]) {
   float x[8];
 #pragma unroll
@@ -73,12 +78,16 @@ __device__ __forceinline__ void split3(const float (&a)[8], u32x4 (&part)[3]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     x[j] = a[j] - truncated(a[j]);
-    if (!FINITE) x[j] = fabsf(a[j]) < __builtin_huge_valf() ? x[j] : 0.f;
+    if (KIND == KEYS) x[j] = fabsf(a[j]) == __builtin_huge_valf() ? 0.f : x[j];
+    if (KIND == QUERIES) x[j] = x[j] == 0.f ? a[j] * 0x1p-40f : x[j];
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) part[1][j] = upper(x[2 * j], x[2 * j + 1]);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] -= truncated(x[j]);
+  for (int j = 0; j < 8; ++j) {
+    x[j] -= truncated(x[j]);
+    if (KIND == QUERIES) x[j] = x[j] == 0.f ? a[j] * 0x1p-40f : x[j];
+  }
 #pragma unroll
   for (int j = 0; j < 4; ++j) part[2][j] = upper(x[2 * j], x[2 * j + 1]);
 }
@@ -136,7 +145,7 @@ __device__ __forceinline__ void prob_operands(const f32x4 &a, const f32x4 &b, u3
     pf[0] = u32x4{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])};
   } else {
     const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-    split3<true>(x, pf);
+    split3<FINITE>(x, pf);
   }
 }
 
@@ -260,7 +269,7 @@ __device__ __forceinline__ void block_logits(f32x4 (&s)[NQ][2], const Block<T, D
         float x[8];
         u32x4 a[3];
         eight_floats(t.k[e][k][0], t.k[e][k][1], x);
-        split3<false>(x, a);
+        split3<KEYS>(x, a);
 #pragma unroll
         for (int sum = 3; sum >= 0; --sum)
 #pragma unroll
@@ -325,7 +334,7 @@ __device__ __forceinline__ bool block_tile4(Acc<DH, NQ> &st, uint64_t &far, Bloc
         u32x4 a[3];
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(t.v[k][j][h]);
-        split3<true>(x, a);
+        split3<FINITE>(x, a);
 #pragma unroll
         for (int sum = 3; sum >= 0; --sum)
 #pragma unroll
@@ -396,7 +405,7 @@ void attn_q4_kernel(AttnQ8Params p, int n_rg) {
       } else {
         float x[8];
         eight_floats(src[0], src[1], x);
-        split3<false>(x, qf[qt].x[k]);
+        split3<QUERIES>(x, qf[qt].x[k]);
       }
     }
   }
