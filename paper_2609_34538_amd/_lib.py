@@ -859,6 +859,8 @@ class Quant4Cache:
               num_depths: int, k_plane: Dict[int, int], v_plane: Dict[int, int],
               dtype: torch.dtype = torch.bfloat16, device="cuda") -> "Quant4Cache":
         """An empty cache with planes for the depths that k_plane and v_plane name."""
+        if head_dim % BLOCK_DIMS:
+            raise ValueError(f"head_dim must be a multiple of {BLOCK_DIMS}")
         nk, nv, s = max(k_plane.values()) + 1, max(v_plane.values()) + 1, head_dim // BLOCK_DIMS
         at, u8 = (num_layers, num_kv_heads, num_pages), torch.uint8
         return cls(torch.zeros((nk, *at, s, 64, 16), dtype=u8, device=device),
