@@ -545,13 +545,14 @@ typedef struct das_cache_q4 {
  *
  * Numerics: cached elements are exact in the products' types. bf16 calls round probabilities
  * to bf16 for cached values, and to twice its bits for block values; fp32 calls take every
- * factor with its 24 bits, as far as they are 2^-133 or more. Accumulation and softmax statistics are fp32, for logits of any
- * finite size; sums are divided last, so that values whose sum over the positions passes the
- * largest fp32 give infinities. Block values that are infinite or NaN reach only the rows that
- * see them; a position whose logit is -infinity has no weight (in fp32 calls an infinite key
- * times a query of less than 2^-93 is NaN). Sequences that are cut into parts are joined from the parts' results, in bf16
- * calls from fp16 relative to each row's largest: what is under 2^-39 of it in its part is
- * lost. lse as for das_attn_policy.
+ * factor with its 24 bits, as far as they are 2^-133 or more. Accumulation and softmax
+ * statistics are fp32, for logits of any finite size; sums are divided last, so that values
+ * whose sum over the positions passes the largest fp32 give infinities. Block values that are
+ * infinite or NaN reach only the rows that see them; a position whose logit is -infinity has
+ * no weight (in fp32 calls an infinite key times a query of less than 2^-93 is NaN). Sequences
+ * that are cut into parts are joined from the parts' results, in bf16 calls from fp16 relative
+ * to each row's largest: what is under 2^-39 of it in its part is lost. lse as for
+ * das_attn_policy.
  *
  * das_attn_q4_workspace_bytes returns 0 for arguments that das_attn_q4 rejects; the
  * workspace is 256-byte aligned, needs no init, and calls that run concurrently need

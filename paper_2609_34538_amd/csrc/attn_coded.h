@@ -18,7 +18,8 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = 32;
 constexpr int kTilesPerPage = kPage / kTile;
-constexpr int kWavesQ8 = 4;// Probabilities are held relative to a reference that a row's logits may pass by
+constexpr int kWavesQ8 = 4;
+// Probabilities are held relative to a reference that a row's logits may pass by
 // kSlack binary orders before it moves; bf16 calls hold them times 2^kProbShift, so
 // that the largest fit fp16 and those down to 2^-23 of the reference are normal there. Plain
 // sums, and all of fp32 calls', are relative to the reference plus kSlack: no probability is

@@ -679,7 +679,8 @@ void attn_q8_kernel(AttnQ8Params p, int n_rg) {
       else write_output_row<T, DH>(p, b, kvh, row, lg, st.o[qt], m[qt], st.l[qt]);
     }
     return;
-  }  merge_waves<T, DH, NQ, RW>(p, st, m, part, sm, sl, sa, rec, nsb, rg, b, kvh, wave, ln, lg);
+  }
+  merge_waves<T, DH, NQ, RW>(p, st, m, part, sm, sl, sa, rec, nsb, rg, b, kvh, wave, ln, lg);
 }
 
 template <typename T, int DH>

@@ -18,12 +18,14 @@
 // permutations, its own inverse) makes of them the words of the page, four tokens of two dims.
 // A commit to part of a quad stores its bytes one by one, which leaves the others as they were.
 //
-// Bound by memory that is read and written at once: 2005 tokens of 24 planes and layers, 55
-// heads, dh 96 (135 MB in, 508 MB out) come back in 206 us, 3.1 TB/s, as a library conversion of
-// bytes to fp32 of that size does; without its loads the kernel takes 105 us, without its stores
-// 87. Commits of 0-32 tokens of 32 sequences (130 MB in, 34 MB out) take 66 us, what lies in
-// part of a 128-byte line of the page going out as several writes (63 MB by the counters); of 8
-// tokens of 64 planes x 4 layers x 55 heads 13 us, the launch and three dependent round trips.
+// 2005 tokens of 24 planes and layers, 55 heads, dh 96 (135 MB in, 508 MB out) come back in 206 us,
+// 3.1 TB/s, where a copy of large arrays reaches 4.9 (131 us; fp32, 1.15 GB, 357 us for 235). Without
+// its loads the kernel takes 105 us, without its stores 87, which is nearly the whole together:
+// they do not overlap, and neither is at the memory's rate, since a load takes 4-byte words of the
+// pages' 16-byte pieces, whose others other quads and heads come for. Commits of 0-32 tokens of 32
+// sequences (130 MB in, 34 MB out) take 66 us, what lies in part of a 128-byte line of the page
+// going out as several writes (63 MB by the counters); of 8 tokens of 64 planes x 4 layers x 55
+// heads 13 us, the launch and three dependent round trips.
 // Measured and not kept: a wave along the tokens of one head, 192 bytes of each row (213, 67
 // and 16 us), 2, 4, 6 and 8 steps a wave (216, 211, 222, 257 us), all steps in a loop (220 us).
 

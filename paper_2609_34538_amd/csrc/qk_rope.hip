@@ -12,7 +12,7 @@
 // on.
 //
 // Bound by memory for batches: 32 x 32 tokens of 165 heads, dh 96, bf16 out of a fused projection
-// (65 MB) 15.1-16.1 us, 4.0-4.3 TB/s, where a copy of large arrays reaches 4.9; 8 tokens 4.2 us,
+// (65 MB) 14.8-16.1 us, 4.0-4.4 TB/s, where a copy of large arrays reaches 4.9; 8 tokens 3.7-5.2 us,
 // the launch and two round trips. A token's heads are shared by workgroups until there are eight a
 // compute unit: 64 tokens 4.4 us, with one workgroup each 8.4, 256 tokens 8.2 and 10.6; 1024
 // tokens with three each 16.2, six 18.7. Where half of a workgroup or more would be idle, it takes

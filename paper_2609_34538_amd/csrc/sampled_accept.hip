@@ -21,9 +21,9 @@
 // share.
 //
 // 32 sequences x 32 positions x 65536 bf16 logits, target and draft, three quarters of which are
-// tested (200 MB): 70-76 us, of which the rows' sums 58 (3.4 TB/s, bound by their 64-bit
-// arithmetic), the run 12 and the draw 8; one sequence of 8 positions, fp32: 14.7 us, three
-// launches and their round trips. Measured and not kept: the draw in the second kernel, by the
+// tested (200 MB): 69-78 us, of which the rows' sums 58 (3.4 TB/s, bound by their 64-bit
+// arithmetic), the run 12 and the draw 8, 43 with a greedy draft; one sequence of 8 positions, fp32:
+// 12-19 us, three launches and their round trips. Measured and not kept: the draw in the second kernel, by the
 // last part to end (14.7 -> 14.4 us, but 76 -> 91: what its counter needs to be seen in order
 // writes a cache back for every part); the sums of weights under 2^-12 in fp32 (no gain: nearly
 // every piece of a row has a larger one).
@@ -255,7 +255,8 @@ static_assert(kDraw == kAcceptDraw && sizeof(Stat) == kAcceptStatBytes && sizeof
 // rows of 65536 bf16 logits, 200 MB: 58 us; with 20 operations 74 us, and 61 us with as many
 // registers as the compiler takes by itself, which is 4 waves a SIMD instead of 6).
 template <typename T>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) void accept_stats_kernel(SampledAcceptParams p) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6)))
+void accept_stats_kernel(SampledAcceptParams p) {
   __shared__ Powers<kFine> table;
   __shared__ double part_sum[kWavesA];
   __shared__ float part_max[kWavesA];
